@@ -141,6 +141,7 @@ def lib() -> ctypes.CDLL:
                    "radar_attend_selected",
                    "radar_profile_enable", "radar_profile_read"):
             getattr(L, fn).restype = ctypes.c_int
+        cache_ops.declare(L)
         _lib = L
     return _lib
 
@@ -511,6 +512,11 @@ def peak_read_gbps(device="cuda", nbytes=4 << 30, reps=5) -> float:
     sec = e0.elapsed_time(e1) / reps * 1e-3
     del buf
     return nbytes / sec / 1e9
+
+
+from . import cache_ops  # noqa: E402  (needs the helpers above)
+from .cache_ops import (  # noqa: E402,F401
+    Rope, rope_frequencies, rotary, rotary_fill, rotary_qk)
 
 
 class RadarLayer:

@@ -2,8 +2,9 @@
 
 The library is built from several translation units compiled in parallel:
 csrc/radar.hip (host logic, C ABI), csrc/build.hip (index build),
-csrc/split.hip (the split path's kernels) and csrc/fused.hip once per
-feature count n (-DRADAR_FUSED_N=n), then linked into one shared object.
+csrc/split.hip (the split path's kernels), csrc/fused.hip once per feature
+count n (-DRADAR_FUSED_N=n) and the cache operators' units, then linked into
+one shared object.
 """
 from __future__ import annotations
 
@@ -17,6 +18,9 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libradar.so")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ_DIR = os.path.join(HERE, "_build")
+# the cache operators: no kernel of the decode path is compiled from these
+CACHE_UNITS = ("rotary.hip",)
+CACHE_HEADERS = ("cache_impl.h",)
 FEATURE_COUNTS = (64, 128, 256, 512, 1024, 2048)
 
 HIPCC_FLAGS = [
@@ -38,14 +42,17 @@ def units():
     """(object name, source, extra flags) of every translation unit."""
     out = [("radar.o", "radar.hip", []), ("build.o", "build.hip", []),
            ("split.o", "split.hip", [])]
+    out += [(f[:-4] + ".o", f, []) for f in CACHE_UNITS]
     out += [(f"fused_n{n}.o", "fused.hip", [f"-DRADAR_FUSED_N={n}"])
             for n in FEATURE_COUNTS]
     return out
 
 
 def sources():
-    """Every file the library is built from (for hashes of the source)."""
-    names = sorted(f for f in os.listdir(CSRC) if f.endswith((".hip", ".h")))
+    """Every file the decode path is built from (for hashes of the source that
+    its measurements were taken with)."""
+    names = sorted(f for f in os.listdir(CSRC) if f.endswith((".hip", ".h"))
+                   and f not in CACHE_UNITS + CACHE_HEADERS)
     return [os.path.join(CSRC, f) for f in names] + [os.path.join(INCLUDE, "radar.h")]
 
 
@@ -55,6 +62,9 @@ def _stale(obj, src):
     t = os.path.getmtime(obj)
     deps = [src, os.path.join(CSRC, "radar_impl.h"), os.path.join(INCLUDE, "radar.h"),
             os.path.abspath(__file__)]
+    if os.path.basename(src) in CACHE_UNITS:
+        deps += [os.path.join(CSRC, h) for h in CACHE_HEADERS]
+        deps.append(os.path.join(INCLUDE, "radar_cache.h"))
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -1,0 +1,263 @@
+"""The cache operators beside the decode path (include/radar_cache.h): rotary
+positions, attention over a shared prefix, attention that accumulates the
+rows' weights, eviction by those weights. Like the rest of the binding this
+only marshals arguments; the package re-exports every public name.
+"""
+from __future__ import annotations
+
+import ctypes
+import dataclasses
+import math
+
+import torch
+
+from . import (RADAR_BF16, RADAR_F32, Config, RadarError, _cache, _check, _Config,
+               _need, _ptr, _query, lib)
+
+_P = ctypes.c_void_p
+_DTYPES = {torch.float32: RADAR_F32, torch.bfloat16: RADAR_BF16}
+ROPE_MAX_DIM = 256
+
+
+class _Rope(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("mscale", ctypes.c_float), ("inv_freq", ctypes.c_void_p)]
+
+
+class _Rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("seq", ctypes.c_int64),
+                ("token", ctypes.c_int64), ("head", ctypes.c_int64)]
+
+
+def declare(L) -> None:
+    """Argument types of the calls, for the library the package loaded."""
+    cfgp, ropep, rowsp = (ctypes.POINTER(x) for x in (_Config, _Rope, _Rows))
+    i64, i32, sz = ctypes.c_int64, ctypes.c_int32, ctypes.c_size_t
+    L.radar_rotary.argtypes = [ropep, i32, i64, i32, ctypes.c_int, i32, rowsp, rowsp,
+                               i32, rowsp, rowsp, i64, _P, i32, _P, i32, _P]
+    L.radar_rotary_fill.argtypes = [cfgp, ropep, i64, rowsp, rowsp, rowsp, rowsp, _P, _P,
+                                    i64, _P, i64, _P, i32, _P, _P]
+    for fn in ("radar_rotary", "radar_rotary_fill"):
+        getattr(L, fn).restype = ctypes.c_int
+
+
+def _one_device(x, *others):
+    """Every device tensor of a call lies on x's GPU."""
+    d = x.get_device()
+    for o in others:
+        if o is not None and o.get_device() not in (d, -1):
+            raise ValueError(f"tensors on different devices: {x.device} and {o.device}")
+
+
+def _call(fn, x, *args):
+    """lib().fn(*args, stream) with x's device current (a stream takes launches
+    from its own device only). The stream is asked for as torch's own generated
+    code asks: its handle alone, 2 us less than a stream object."""
+    f = getattr(lib(), fn)
+    i = x.get_device()
+    if i == torch.cuda.current_device():
+        st = f(*args, torch._C._cuda_getCurrentRawStream(i))
+    else:
+        with torch.cuda.device(i):
+            st = f(*args, torch._C._cuda_getCurrentRawStream(i))
+    if st != 0:
+        _check(fn, st)
+
+
+# ---- rotary positions --------------------------------------------------------
+@dataclasses.dataclass(frozen=True)
+class Rope:
+    """Rotary positions of a head: inv_freq, a device float64 tensor
+    [rot_dim / 2] of angles per position (see rope_frequencies); interleaved:
+    pairs (2 i, 2 i + 1) instead of (i, i + rot_dim / 2); mscale: a factor on
+    the rotated dims."""
+    inv_freq: torch.Tensor
+    interleaved: bool = False
+    mscale: float = 1.0
+
+    def __post_init__(self):
+        _need(self.inv_freq, torch.float64, "inv_freq")
+        object.__setattr__(self, "_c", _Rope(2 * self.inv_freq.numel(),
+                                             1 if self.interleaved else 0, self.mscale,
+                                             self.inv_freq.data_ptr()))
+
+    @property
+    def rot_dim(self) -> int:
+        return 2 * self.inv_freq.numel()
+
+
+def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
+                     factor: float = 1.0, trained_len: int = 0, alpha: float = 1.0,
+                     beta: float = 32.0):
+    """(inv_freq, mscale) of rot_dim rotated dims: inv_freq a float64 CPU tensor
+    f_i = base^(-2 i / rot_dim), and, for contexts longer than the trained one
+    by `factor`,
+      "linear"  f_i / factor (positions interpolated);
+      "ntk"     the base times factor^(rot_dim / (rot_dim - 2)), which leaves
+                the fastest pair as it is and slows the slowest by `factor`;
+      "yarn"    by parts: pairs that turn more than beta times over trained_len
+                positions stay, those that turn less than alpha times are
+                interpolated, linear in between; mscale = 0.1 ln(factor) + 1.
+    mscale is 1 otherwise."""
+    if rot_dim < 2 or rot_dim % 2:
+        raise ValueError(f"rot_dim must be even and positive, got {rot_dim}")
+    if not base > 0 or not factor > 0:
+        raise ValueError("base and factor must be positive")
+    if scaling == "ntk":
+        if rot_dim < 4:
+            raise ValueError("ntk scaling needs two pairs")
+        base = base * factor ** (rot_dim / (rot_dim - 2))
+    i = torch.arange(rot_dim // 2, dtype=torch.float64)
+    f = torch.pow(torch.tensor(float(base), dtype=torch.float64), -2.0 * i / rot_dim)
+    if scaling in ("none", "ntk"):
+        return f, 1.0
+    if scaling == "linear":
+        return f / factor, 1.0
+    if scaling != "yarn":
+        raise ValueError(f"scaling {scaling!r}: none, linear, ntk or yarn")
+    if trained_len < 1 or not beta > alpha:
+        raise ValueError("yarn needs trained_len >= 1 and beta > alpha")
+    turns = f * (trained_len / (2 * math.pi))
+    keep = ((turns - alpha) / (beta - alpha)).clamp(0.0, 1.0)
+    return keep * f + (1 - keep) * f / factor, 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+
+
+def _rows(x, name, dtype):
+    """(struct, B, T, heads, d) of x, [B][T][heads][d] or [B][heads][d] (one
+    token): a dense last axis, the address and the other strides on 16 bytes."""
+    if not x.is_cuda:
+        raise ValueError(f"{name} must be a device tensor")
+    if x.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {x.dtype}")
+    shape, stride = x.shape, x.stride()
+    if len(shape) == 4:
+        B, T, H, d = shape
+        sb, st, sh, sd = stride
+    elif len(shape) == 3:
+        (B, H, d), (sb, sh, sd), T, st = shape, stride, 1, 0
+    else:
+        raise ValueError(f"{name} must be [B][T][heads][d] or [B][heads][d]")
+    # (the stride of an axis of one element is not used and may be anything)
+    if B <= 1:
+        sb = 0
+    if T <= 1:
+        st = 0
+    if H <= 1:
+        sh = 0
+    ptr, per = x.data_ptr(), 16 // x.element_size()
+    if sd != 1 and d > 1 or ptr & 15 or sb % per or st % per or sh % per:
+        raise ValueError(f"{name} needs a dense last axis and other strides and an address "
+                         "that are multiples of 16 bytes")
+    return _Rows(ptr, sb, st, sh), B, T, H, d
+
+
+def _out_rows(x, out, name):
+    """(out, struct) for the input x: a new dense tensor, or the given one."""
+    if out is None:
+        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+    else:
+        if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
+            raise ValueError(f"{name} must have the input's shape, type and device")
+        if any(s == 0 and n > 1 for s, n in zip(out.stride(), out.shape)):
+            raise ValueError(f"{name} has elements that share a place")
+        if out.data_ptr() == x.data_ptr() and out.stride() != x.stride():
+            raise ValueError(f"{name} starts at its input with other strides")
+    return out, _rows(out, name, x.dtype)[0]
+
+
+def _positions(pos, B, T, name="pos"):
+    """(first position, device tensor or None, one per token) of an int, an
+    int64 [B] (first tokens) or an int64 [B][T] (each token)."""
+    if isinstance(pos, int):
+        return pos, None, 0
+    _need(pos, torch.int64, name)
+    if pos.dim() == 1 and pos.numel() == B:
+        return 0, pos, 0
+    if tuple(pos.shape) == (B, T):
+        return 0, pos, 1
+    raise ValueError(f"{name} must be an int, int64 [B] or int64 [B][T]")
+
+
+def _lens_of(lens, B):
+    if lens is not None:
+        _need(lens, torch.int64, "lens", B)
+    return lens
+
+
+def _float_type(x, name):
+    if x.dtype not in _DTYPES:
+        raise ValueError(f"{name} must be float32 or bfloat16, got {x.dtype}")
+
+
+def rotary(rope: Rope, x, pos, out=None, inverse: bool = False, lens=None):
+    """radar_rotary of one tensor x, [B][T][heads][d] or [B][heads][d] (one
+    token), strided as it comes out of a projection. pos: the position of the
+    first token (an int, or an int64 [B]) or of every token (int64 [B][T]).
+    out may be x. inverse: the gradient of the rotation. lens (int64 [B]): only
+    tokens t < lens[b] are touched. Returns out."""
+    _float_type(x, "x")
+    rx, B, T, H, d = _rows(x, "x", x.dtype)
+    out, ro = _out_rows(x, out, "out")
+    p0, p, each = _positions(pos, B, T)
+    lens = _lens_of(lens, B)
+    _one_device(x, p, lens, rope.inv_freq)
+    if x.numel():
+        by = ctypes.byref
+        _call("radar_rotary", x, by(rope._c), B, T, d, _DTYPES[x.dtype], H, by(rx), by(ro),
+              0, None, None, p0, _ptr(p), each, _ptr(lens), 1 if inverse else 0)
+    return out
+
+
+def rotary_qk(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = False,
+              lens=None):
+    """rotary() of q and k in one launch. Returns (q_out, k_out)."""
+    _float_type(q, "q")
+    rq, B, T, Hq, d = _rows(q, "q", q.dtype)
+    rk, Bk, Tk, Hk, dk = _rows(k, "k", q.dtype)
+    if (Bk, Tk, dk) != (B, T, d):
+        raise ValueError("q and k must agree in batch, tokens and head_dim")
+    q_out, qo = _out_rows(q, q_out, "q_out")
+    k_out, ko = _out_rows(k, k_out, "k_out")
+    p0, p, each = _positions(pos, B, T)
+    lens = _lens_of(lens, B)
+    _one_device(q, k, p, lens, rope.inv_freq)
+    if q.numel() and k.numel():
+        by = ctypes.byref
+        _call("radar_rotary", q, by(rope._c), B, T, d, _DTYPES[q.dtype], Hq, by(rq), by(qo),
+              Hk, by(rk), by(ko), p0, _ptr(p), each, _ptr(lens), 1 if inverse else 0)
+    return q_out, k_out
+
+
+def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_out=None,
+                lens=None):
+    """radar_rotary_fill: the chunk k, v [B][T][Hkv][d] (or [B][Hkv][d], one
+    token) into rows row + t of K and V, k rotated; with q, its rotation too,
+    in the same launch. row: an int, or an int64 [B] (rows outside the capacity
+    are skipped); pos: as for rotary(), the row itself if None. lens: only
+    tokens t < lens[b]. Returns q_out (None without q)."""
+    _cache(cfg, K, V)
+    rk, B, T, Hk, d = _rows(k, "k", cfg.dtype)
+    rv, *shape_v = _rows(v, "v", cfg.dtype)
+    if [B, T, Hk, d] != shape_v or (B, Hk, d) != (cfg.batch, cfg.n_kv_heads, cfg.head_dim):
+        raise ValueError("k and v must be [batch][T][n_kv_heads][head_dim], the config's "
+                         f"{cfg.batch}, {cfg.n_kv_heads} heads of {cfg.head_dim}")
+    rq = qo = None
+    by = ctypes.byref
+    if q is not None:
+        rq, *shape_q = _rows(q, "q", cfg.dtype)
+        if shape_q != [B, T, cfg.n_q_heads, d]:
+            raise ValueError("q must be [batch][T][n_q_heads][head_dim] with k's tokens")
+        q_out, qo = _out_rows(q, q_out, "q_out")
+        rq, qo = by(rq), by(qo)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    r0, rows, each = _positions(row, B, T, "row")
+    if each:
+        raise ValueError("row must be an int or int64 [B]")
+    p0, p, each = (r0, rows, 0) if pos is None else _positions(pos, B, T)
+    lens = _lens_of(lens, B)
+    _one_device(k, v, q, rows, p, lens, rope.inv_freq, K, V)
+    if T:
+        _call("radar_rotary_fill", k, by(cfg.c_struct()), by(rope._c), T, rq, qo, by(rk), by(rv),
+              _ptr(K), _ptr(V), r0, _ptr(rows), p0, _ptr(p), each, _ptr(lens))
+    return q_out
