@@ -19,8 +19,8 @@ LIB = os.path.join(HERE, "libradar.so")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ_DIR = os.path.join(HERE, "_build")
 # the cache operators: no kernel of the decode path is compiled from these
-CACHE_UNITS = ("rotary.hip",)
-CACHE_HEADERS = ("cache_impl.h",)
+CACHE_UNITS = ("rotary.hip", "prefix.hip", "attend.hip")
+CACHE_HEADERS = ("cache_impl.h", "attend_impl.h")
 FEATURE_COUNTS = (64, 128, 256, 512, 1024, 2048)
 
 HIPCC_FLAGS = [
@@ -42,7 +42,10 @@ def units():
     """(object name, source, extra flags) of every translation unit."""
     out = [("radar.o", "radar.hip", []), ("build.o", "build.hip", []),
            ("split.o", "split.hip", [])]
-    out += [(f[:-4] + ".o", f, []) for f in CACHE_UNITS]
+    out += [(f[:-4] + ".o", f, []) for f in CACHE_UNITS if f != "attend.hip"]
+    out += [(f"attend_{n}_{d}.o", "attend.hip",
+             [f"-DRADAR_ATTEND_F32={f32}", f"-DRADAR_ATTEND_D={d}"])
+            for f32, n in ((0, "bf16"), (1, "f32")) for d in (64, 128)]
     out += [(f"fused_n{n}.o", "fused.hip", [f"-DRADAR_FUSED_N={n}"])
             for n in FEATURE_COUNTS]
     return out

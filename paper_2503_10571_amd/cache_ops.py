@@ -37,7 +37,16 @@ def declare(L) -> None:
                                i32, rowsp, rowsp, i64, _P, i32, _P, i32, _P]
     L.radar_rotary_fill.argtypes = [cfgp, ropep, i64, rowsp, rowsp, rowsp, rowsp, _P, _P,
                                     i64, _P, i64, _P, i32, _P, _P]
-    for fn in ("radar_rotary", "radar_rotary_fill"):
+    L.radar_attend_prefix.argtypes = [cfgp, _P, _P, _P, i64, i64, _P, _P, i64, _P, _P, _P,
+                                      sz, _P]
+    L.radar_attend_accumulate.argtypes = [cfgp, _P, _P, _P, _P, i64, _P, _P, _P, sz, _P]
+    L.radar_attend_prefix_workspace_bytes.argtypes = [cfgp, i64, i64]
+    L.radar_attend_accumulate_workspace_bytes.argtypes = [cfgp, i64]
+    for fn in ("radar_attend_prefix_workspace_bytes",
+               "radar_attend_accumulate_workspace_bytes"):
+        getattr(L, fn).restype = sz
+    for fn in ("radar_rotary", "radar_rotary_fill", "radar_attend_prefix",
+               "radar_attend_accumulate"):
         getattr(L, fn).restype = ctypes.c_int
 
 
@@ -261,3 +270,92 @@ def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_ou
         _call("radar_rotary_fill", k, by(cfg.c_struct()), by(rope._c), T, rq, qo, by(rk), by(rv),
               _ptr(K), _ptr(V), r0, _ptr(rows), p0, _ptr(p), each, _ptr(lens))
     return q_out
+
+
+# ---- attention over a shared prefix, and with accumulated weights --------------
+def attend_prefix_workspace_bytes(cfg: Config, prefix_len: int, t: int) -> int:
+    """Scratch for every call with this config, at most this prefix_len and t."""
+    return int(lib().radar_attend_prefix_workspace_bytes(ctypes.byref(cfg.c_struct()),
+                                                         prefix_len, t))
+
+
+def attend_accumulate_workspace_bytes(cfg: Config, t: int) -> int:
+    """Scratch for every call with this config and at most this t."""
+    return int(lib().radar_attend_accumulate_workspace_bytes(ctypes.byref(cfg.c_struct()), t))
+
+
+def _workspace(given, nbytes, device):
+    """The given workspace, or a new one (none where the size is 0: the call
+    refuses its arguments)."""
+    if given is not None:
+        _need(given, torch.uint8, "workspace")
+        return given, given.numel()
+    if nbytes == 0:
+        return None, 0
+    return torch.empty(nbytes, dtype=torch.uint8, device=device), nbytes
+
+
+def _attended(cfg, q, out, lens):
+    _query(cfg, q)
+    if out is None:
+        out = torch.empty_like(q)
+    else:
+        _need(out, cfg.dtype, "out", cfg.batch * cfg.n_q_heads * cfg.head_dim)
+    return out, _lens_of(lens, cfg.batch)
+
+
+def attend_prefix(cfg: Config, q, Kp, Vp, prefix_len: int, K=None, V=None, t: int = 0,
+                  out=None, lens=None, workspace=None):
+    """radar_attend_prefix: exact attention of every sequence's query (q
+    [B][Hq][d]) over rows [0, prefix_len) of Kp, Vp [Hkv][rows][d], which the
+    batch shares, and rows [0, t) (or [0, lens[b])) of its own K, V (None with
+    t = 0). Returns out."""
+    out, lens = _attended(cfg, q, out, lens)
+    prefix_cap = 0
+    if prefix_len > 0:
+        for x, name in ((Kp, "Kp"), (Vp, "Vp")):
+            if x is None or x.dim() != 3 or x.shape[0] != cfg.n_kv_heads or x.shape[2] != cfg.head_dim:
+                raise ValueError(f"{name} must be [n_kv_heads][rows][head_dim]")
+            _need(x, cfg.dtype, name, host_ok=True)
+        prefix_cap = Kp.shape[1]
+        if Vp.shape[1] != prefix_cap:
+            raise ValueError("Kp and Vp must hold the same number of rows")
+    if t > 0 or K is not None:
+        if K is None or V is None:
+            raise ValueError("K and V are needed with t > 0")
+        _cache(cfg, K, V)
+    _one_device(q, Kp, Vp, K, V, out, lens, workspace)
+    c = ctypes.byref(cfg.c_struct())
+    need = lib().radar_attend_prefix_workspace_bytes(c, prefix_len, t) if workspace is None else 0
+    workspace, n = _workspace(workspace, need, q.device)
+    _call("radar_attend_prefix", q, c, _ptr(q), _ptr(Kp), _ptr(Vp), prefix_len, prefix_cap,
+          _ptr(K), _ptr(V), t, _ptr(lens), _ptr(out), _ptr(workspace), n)
+    return out
+
+
+def _mass(cfg, mass):
+    _need(mass, torch.float32, "mass", cfg.batch * cfg.n_kv_heads * cfg.capacity)
+
+
+def new_mass(cfg: Config, device) -> torch.Tensor:
+    """The weights of the rows of an empty cache, [B][Hkv][capacity] fp32."""
+    return torch.zeros(cfg.batch, cfg.n_kv_heads, cfg.capacity, dtype=torch.float32,
+                       device=device)
+
+
+def attend_accumulate(cfg: Config, q, K, V, mass, t: int, out=None, lens=None,
+                      workspace=None):
+    """radar_attend_accumulate: exact attention over rows [0, t) (or
+    [0, lens[b])) of K and V; the softmax weight of every row, summed over the
+    query heads of its kv head, is added to mass [B][Hkv][capacity] (fp32).
+    Returns out."""
+    out, lens = _attended(cfg, q, out, lens)
+    _cache(cfg, K, V)
+    _mass(cfg, mass)
+    _one_device(q, K, V, mass, out, lens, workspace)
+    c = ctypes.byref(cfg.c_struct())
+    need = lib().radar_attend_accumulate_workspace_bytes(c, t) if workspace is None else 0
+    workspace, n = _workspace(workspace, need, q.device)
+    _call("radar_attend_accumulate", q, c, _ptr(q), _ptr(K), _ptr(V), _ptr(mass), t,
+          _ptr(lens), _ptr(out), _ptr(workspace), n)
+    return out
