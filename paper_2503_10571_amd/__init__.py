@@ -517,7 +517,8 @@ def peak_read_gbps(device="cuda", nbytes=4 << 30, reps=5) -> float:
 from . import cache_ops  # noqa: E402  (needs the helpers above)
 from .cache_ops import (  # noqa: E402,F401
     Rope, attend_accumulate, attend_accumulate_workspace_bytes, attend_prefix,
-    attend_prefix_workspace_bytes, new_mass, rope_frequencies, rotary, rotary_fill, rotary_qk)
+    attend_prefix_workspace_bytes, evict, evict_workspace_bytes, new_mass,
+    rope_frequencies, rotary, rotary_fill, rotary_qk)
 
 
 class RadarLayer:

@@ -42,11 +42,13 @@ def declare(L) -> None:
     L.radar_attend_accumulate.argtypes = [cfgp, _P, _P, _P, _P, i64, _P, _P, _P, sz, _P]
     L.radar_attend_prefix_workspace_bytes.argtypes = [cfgp, i64, i64]
     L.radar_attend_accumulate_workspace_bytes.argtypes = [cfgp, i64]
+    L.radar_evict.argtypes = [cfgp, _P, _P, _P, i64, _P, i64, i64, _P, _P, _P, sz, _P]
+    L.radar_evict_workspace_bytes.argtypes = [cfgp, i64, i64, i64]
     for fn in ("radar_attend_prefix_workspace_bytes",
-               "radar_attend_accumulate_workspace_bytes"):
+               "radar_attend_accumulate_workspace_bytes", "radar_evict_workspace_bytes"):
         getattr(L, fn).restype = sz
     for fn in ("radar_rotary", "radar_rotary_fill", "radar_attend_prefix",
-               "radar_attend_accumulate"):
+               "radar_attend_accumulate", "radar_evict"):
         getattr(L, fn).restype = ctypes.c_int
 
 
@@ -359,3 +361,38 @@ def attend_accumulate(cfg: Config, q, K, V, mass, t: int, out=None, lens=None,
     _call("radar_attend_accumulate", q, c, _ptr(q), _ptr(K), _ptr(V), _ptr(mass), t,
           _ptr(lens), _ptr(out), _ptr(workspace), n)
     return out
+
+
+# ---- eviction ---------------------------------------------------------------------
+def evict_workspace_bytes(cfg: Config, t: int, heavy: int, recent: int) -> int:
+    """Scratch for every call with this config, at most this t and at most as
+    many kept rows."""
+    return int(lib().radar_evict_workspace_bytes(ctypes.byref(cfg.c_struct()), t, heavy,
+                                                 recent))
+
+
+def evict(cfg: Config, K, V, mass, t: int, heavy: int, recent: int, lens=None,
+          new_lens=None, kept=None, workspace=None) -> int:
+    """radar_evict: cut the cache of t rows (or lens[b]) to n = cfg.n_sink +
+    heavy + recent: the sinks, the last `recent` rows, and the `heavy` rows of
+    the others with the largest mass move to the front of K, V and mass, in
+    their order; the masses behind them become 0. new_lens (int64 [B], may be
+    lens) receives the new lengths, kept (int32 [B][Hkv][min(n, t)]) the rows
+    kept. The summaries hold for the old rows: build_index() follows. Returns
+    the bound of the new lengths, min(t, n)."""
+    _cache(cfg, K, V)
+    _mass(cfg, mass)
+    n = min(cfg.n_sink + heavy + recent, t)
+    lens = _lens_of(lens, cfg.batch)
+    if new_lens is not None:
+        _need(new_lens, torch.int64, "new_lens", cfg.batch)
+    if kept is not None:
+        _need(kept, torch.int32, "kept", cfg.batch * cfg.n_kv_heads * n)
+    _one_device(mass, K, V, lens, new_lens, kept, workspace)
+    c = ctypes.byref(cfg.c_struct())
+    need = (lib().radar_evict_workspace_bytes(c, t, heavy, recent)
+            if workspace is None else 0)
+    workspace, size = _workspace(workspace, need, mass.device)
+    _call("radar_evict", mass, c, _ptr(K), _ptr(V), _ptr(mass), t, _ptr(lens), heavy, recent,
+          _ptr(new_lens), _ptr(kept), _ptr(workspace), size)
+    return n
