@@ -3,13 +3,12 @@
 // type and head dim: -DRADAR_ATTEND_F32=0|1 -DRADAR_ATTEND_D=64|128).
 //
 // One pass over K and V with a running maximum m and sum l per query row, in 32
-// bits (m in units of log2). A workgroup of four waves takes 32 RW query rows:
-// RW waves with 32 rows each, and 4 / RW such groups that share the tokens of a
-// tile. Both products are 32x32 MFMAs that put the query rows on the lanes,
+// bits (m in units of log2). Both products are MFMAs that put the query rows on
+// the lanes,
 //   S[token][row] = K Q^T,    O^T[dim][row] += V^T P^T,
-// so m, l and every scale are one value per lane, and the logits that a lane
-// ends with (tokens 8 (i / 4) + 4 (lane / 32) + i % 4) are its k-slots of P^T if
-// the rows of V are taken in the same order: no value of P crosses lanes.
+// so m, l and every scale are one value per lane; and a lane's logits are of
+// four consecutive tokens at a time, which are its k-slots of P^T if the rows of
+// V are taken in the same order: no value of P crosses lanes.
 //
 // K and V come to LDS through registers, the next tile's loads in flight while
 // this one is computed. Rows are stored whole, their 16-byte chunks at places
@@ -29,20 +28,50 @@ namespace {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
+typedef short s16x8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8v_t __attribute__((ext_vector_type(8)));
 
-// token (of 32) of a lane's i-th logit
-__device__ __forceinline__ int token_of(int i, int half) {
-  return 8 * (i / 4) + 4 * half + (i % 4);
-}
+// The operands of one wave: kRows query rows (a lane's row is lane % kRows)
+// against steps of kTok tokens, of which a lane gets kVals logits: token
+// token_of(i) is its i-th. acc[block][i] is dim block * kDims + dim_of(i).
 
-// The operands of one wave: 32 query rows (a lane's row is lane % 32) against
-// tiles of rows of D elements in LDS.
-template <typename T, int D> struct Ops;
+// 32 rows: 32x32 products; a lane's half takes four of every eight tokens (dims)
+struct Wide {
+  static constexpr int kRows = 32, kTok = 32, kVals = 16, kDims = 32;
+  typedef f32x16_t Vec;
+  __device__ static __forceinline__ int token_of(int i, int lane) {
+    return 8 * (i / 4) + 4 * (lane >> 5) + (i % 4);
+  }
+  __device__ static __forceinline__ int dim_of(int i, int lane) { return token_of(i, lane); }
+  // over the lanes of a row
+  __device__ static __forceinline__ float row_maximum(float v) {
+    float lo, hi;
+    xor_pair<32>(v, lo, hi);
+    return fmaxf(lo, hi);
+  }
+  __device__ static __forceinline__ float row_total(float v) { return xor_sum<32>(v); }
+};
 
-template <int D> struct Ops<bf16_t, D> {
+// 16 rows: 16x16 products; a lane's quarter takes four of sixteen
+struct Narrow {
+  static constexpr int kRows = 16, kTok = 16, kVals = 4, kDims = 16;
+  typedef f32x4_t Vec;
+  __device__ static __forceinline__ int token_of(int i, int lane) { return 4 * (lane >> 4) + i; }
+  __device__ static __forceinline__ int dim_of(int i, int lane) { return token_of(i, lane); }
+  __device__ static __forceinline__ float row_maximum(float v) {
+    float lo, hi;
+    xor_pair<16>(v, lo, hi);
+    xor_pair<32>(fmaxf(lo, hi), lo, hi);
+    return fmaxf(lo, hi);
+  }
+  __device__ static __forceinline__ float row_total(float v) { return xor_sum<32>(xor_sum<16>(v)); }
+};
+
+template <typename T, int D, int RW> struct Ops;
+
+template <int D, int RW> struct Ops<bf16_t, D, RW> : Wide {
   static constexpr int CPR = D / 8;              // 16-byte chunks per row
-  static constexpr int NDB = D / 32;             // 32-dim blocks
+  static constexpr int NDB = D / kDims;
   bf16x8v_t q[D / 16];
 
   __device__ static __forceinline__ int k_place(int row, int c) {
@@ -58,76 +87,96 @@ template <int D> struct Ops<bf16_t, D> {
       q[ks] = *reinterpret_cast<const bf16x8v_t*>(row + ks * 16 + (lane >> 5) * 8);
   }
   // logits of tokens tok0 .. tok0 + 31 of the tile
-  __device__ __forceinline__ f32x16_t logits(const unsigned char* k, int tok0, int lane) const {
+  __device__ __forceinline__ Vec logits(const unsigned char* k, int tok0, int lane) const {
     const int row = tok0 + (lane & 31), h = lane >> 5;
-    f32x16_t s = {};
+    bf16x8v_t a[D / 16];
 #pragma unroll
-    for (int ks = 0; ks < D / 16; ++ks) {
-      const bf16x8v_t a =
-          *reinterpret_cast<const bf16x8v_t*>(k + row * (D * 2) + k_place(row, 2 * ks + h) * 16);
-      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, q[ks], s, 0, 0, 0);
-    }
+    for (int ks = 0; ks < D / 16; ++ks)
+      a[ks] = *reinterpret_cast<const bf16x8v_t*>(k + row * (D * 2) + k_place(row, 2 * ks + h) * 16);
+    Vec s = {};
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks)
+      s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks], q[ks], s, 0, 0, 0);
     return s;
   }
-  // acc += V^T P^T. The matrix cores take p in bf16. Where the 32 columns hold
-  // 16 rows twice (`low` set in the second copy), the first takes p's upper 8
-  // bits and the second the next 8, and their accumulators are added at the end:
-  // p to 16 bits at no cost. Otherwise p is rounded to bf16, half a step of 2^-8
-  // each, of the size of the output's own rounding; the second product that
-  // more bits would take is half of the kernel's matrix work again.
-  __device__ __forceinline__ void pv(const unsigned char* v, int tok0, const f32x16_t& p, bool twice,
-                                     bool low, f32x16_t (&acc)[NDB], int lane) const {
+  // The matrix cores take p in bf16. Where the 32 columns hold 16 rows twice
+  // (RW = 1; `low` set in the second copy), the first takes p's upper 8 bits and
+  // the second the next 8, and their accumulators are added at the end: p to 16
+  // bits at no cost. Otherwise p is rounded to bf16, half a step of 2^-8 each, of
+  // the size of the output's own rounding; the second product that more bits
+  // would take is half of the kernel's matrix work again.
+  __device__ static __forceinline__ bf16x8v_t p_operand(const Vec& p, int ks, bool twice, bool low) {
     constexpr float kTiny = 1.17549435e-38f;     // smallest normal number
-    const int h = lane >> 5, l16 = lane & 15, hf = (lane >> 4) & 1;
+    bf16x8v_t b;
+    if (RW == 1 && twice) {                // uniform
+      uint32_t w[4];
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      bf16x8v_t b;
-      if (twice) {                         // uniform
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          uint32_t x[2];
-#pragma unroll
-          for (int z = 0; z < 2; ++z) {
-            const float pz = p[8 * ks + 2 * i + z];
-            const float rest = pz - __uint_as_float(__float_as_uint(pz) & 0xffff0000u);
-            // (never 0 where p is not: an infinite V times 0 would be NaN)
-            x[z] = __float_as_uint(low ? __builtin_amdgcn_fmed3f(rest, pz, kTiny) : pz);
-          }
-          w[i] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);   // upper halves
-        }
-        b = __builtin_bit_cast(bf16x8v_t, make_uint4(w[0], w[1], w[2], w[3]));
-      } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) b[i] = (__bf16)p[8 * ks + i];
-      }
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) {
-        // lane (hf, l16) of a half ends with dim 32 db + 16 hf + l16 of the
-        // tokens 16 ks + 4 h .. + 3 and 16 ks + 8 + 4 h .. + 3: transposed reads
-        // of four rows by 16 dims, of which it supplies row l16 / 4, dims
-        // 4 (l16 % 4) .. + 3
-        s16x4_t part[2];
+      for (int i = 0; i < 4; ++i) {
+        uint32_t x[2];
 #pragma unroll
         for (int z = 0; z < 2; ++z) {
-          const int row = tok0 + 16 * ks + 8 * z + 4 * h + (l16 >> 2);
-          const int c = (32 * db + 16 * hf) / 8 + ((l16 & 3) >> 1);
-          const unsigned char* src = v + row * (D * 2) + v_place(row, c) * 16 + (l16 & 1) * 8;
-          part[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (__attribute__((address_space(3))) s16x4_t*)(src));
+          const float pz = p[8 * ks + 2 * i + z];
+          const float rest = pz - __uint_as_float(__float_as_uint(pz) & 0xffff0000u);
+          // (never 0 where p is not: an infinite V times 0 would be NaN)
+          x[z] = __float_as_uint(low ? __builtin_amdgcn_fmed3f(rest, pz, kTiny) : pz);
         }
-        typedef short s16x8_t __attribute__((ext_vector_type(8)));
-        const s16x8_t av = __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7);
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8v_t, av), b,
-                                                          acc[db], 0, 0, 0);
+        w[i] = __builtin_amdgcn_perm(x[1], x[0], 0x07060302u);   // upper halves
       }
+      b = __builtin_bit_cast(bf16x8v_t, make_uint4(w[0], w[1], w[2], w[3]));
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) b[i] = (__bf16)p[8 * ks + i];
     }
+    return b;
+  }
+  // Lane (hf, l16) of a half gets dim 32 db + 16 hf + l16 of the tokens
+  // t0 + 4 h .. + 3 and t0 + 8 + 4 h .. + 3: transposed reads of four rows by 16
+  // dims, of which it supplies row l16 / 4, dims 4 (l16 % 4) .. + 3.
+  __device__ static __forceinline__ void v_operands(const unsigned char* v, int t0, int lane,
+                                                    bf16x8v_t (&a)[NDB]) {
+    const int h = lane >> 5, l16 = lane & 15, hf = (lane >> 4) & 1;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      s16x4_t part[2];
+#pragma unroll
+      for (int z = 0; z < 2; ++z) {
+        const int row = t0 + 8 * z + 4 * h + (l16 >> 2);
+        const int c = (32 * db + 16 * hf) / 8 + ((l16 & 3) >> 1);
+        const unsigned char* src = v + row * (D * 2) + v_place(row, c) * 16 + (l16 & 1) * 8;
+        part[z] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+            (__attribute__((address_space(3))) s16x4_t*)(src));
+      }
+      a[db] = __builtin_bit_cast(bf16x8v_t,
+                                 __builtin_shufflevector(part[0], part[1], 0, 1, 2, 3, 4, 5, 6, 7));
+    }
+  }
+  // acc += V^T P^T over N steps of 32 tokens; with RW > 1, where the products
+  // bound the loop, the operands of the next 16 tokens are read before the
+  // products of these
+  template <int N>
+  __device__ static __forceinline__ void pv(const unsigned char* v, int tok0, const Vec (&p)[N],
+                                            bool twice, bool low, Vec (&acc)[NDB], int lane) {
+    constexpr int kPin = 0x6;              // vector and scalar ALU may pass
+    constexpr int kAhead = RW > 1 ? 1 : 0;
+    bf16x8v_t a[1 + kAhead][NDB];
+    if constexpr (kAhead) v_operands(v, tok0, lane, a[0]);
+    static_for<0, 2 * N>([&](auto kc) {
+      constexpr int ks = decltype(kc)::value, next = ks + kAhead;
+      if constexpr (kAhead) __builtin_amdgcn_sched_barrier(kPin);
+      if constexpr (next < 2 * N) v_operands(v, tok0 + 16 * next, lane, a[next & kAhead]);
+      const bf16x8v_t b = p_operand(p[ks / 2], ks % 2, twice, low);
+      if constexpr (kAhead) __builtin_amdgcn_sched_barrier(kPin);
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[ks & kAhead][db], b, acc[db], 0, 0, 0);
+    });
   }
 };
 
-template <int D> struct Ops<float, D> {
+// 32-bit operands for more than 16 rows
+template <int D, int RW> struct Ops<float, D, RW> : Wide {
   static constexpr int CPR = D / 4;
-  static constexpr int NDB = D / 32;
+  static constexpr int NDB = D / kDims;
   float q[D / 2];
 
   __device__ static __forceinline__ int k_place(int row, int c) { return c ^ (row & 15); }
@@ -141,9 +190,9 @@ template <int D> struct Ops<float, D> {
       q[4 * j] = x.x; q[4 * j + 1] = x.y; q[4 * j + 2] = x.z; q[4 * j + 3] = x.w;
     }
   }
-  __device__ __forceinline__ f32x16_t logits(const unsigned char* k, int tok0, int lane) const {
+  __device__ __forceinline__ Vec logits(const unsigned char* k, int tok0, int lane) const {
     const int row = tok0 + (lane & 31), h = lane >> 5;
-    f32x16_t s = {};
+    Vec s = {};
 #pragma unroll
     for (int j = 0; j < D / 8; ++j) {
       const float4 x =
@@ -155,155 +204,276 @@ template <int D> struct Ops<float, D> {
     }
     return s;
   }
-  __device__ __forceinline__ void pv(const unsigned char* v, int tok0, const f32x16_t& p, bool, bool,
-                                     f32x16_t (&acc)[NDB], int lane) const {
-    const int h = lane >> 5, dim = lane & 31;
+  template <int N>
+  __device__ static __forceinline__ void pv(const unsigned char* v, int tok0, const Vec (&p)[N],
+                                            bool, bool, Vec (&acc)[NDB], int lane) {
+    const int dim = lane & 31;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const int row = tok0 + token_of(i, h);
+    for (int i = 0; i < N * kVals; ++i) {
+      const int row = tok0 + i / kVals * kTok + token_of(i % kVals, lane);
 #pragma unroll
       for (int db = 0; db < NDB; ++db) {
         const float x = *reinterpret_cast<const float*>(
             v + row * (D * 4) + v_place(row, 8 * db + (dim >> 2)) * 16 + (dim & 3) * 4);
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[i], acc[db], 0, 0, 0);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, p[i / kVals][i % kVals], acc[db], 0, 0, 0);
       }
     }
   }
 };
 
+// 32-bit operands for up to 16 rows, at half the matrix work of 32
+template <int D> struct Ops<float, D, 1> : Narrow {
+  static constexpr int CPR = D / 4;
+  static constexpr int NDB = D / kDims;
+  float q[D / 4];
+
+  __device__ static __forceinline__ int k_place(int row, int c) { return c ^ (row & 15); }
+  // the four quarters of a wave read rows four apart, 64 bytes of each
+  __device__ static __forceinline__ int v_place(int row, int c) { return c ^ (((row >> 2) & 3) << 2); }
+  // (dims in the order that logits() takes them: 16 j + 4 quarter + e)
+  __device__ __forceinline__ void load_q(const float* row, int lane) {
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const float4 x = *reinterpret_cast<const float4*>(row + 16 * j + 4 * (lane >> 4));
+      q[4 * j] = x.x; q[4 * j + 1] = x.y; q[4 * j + 2] = x.z; q[4 * j + 3] = x.w;
+    }
+  }
+  __device__ __forceinline__ Vec logits(const unsigned char* k, int tok0, int lane) const {
+    const int row = tok0 + (lane & 15), g = lane >> 4;
+    Vec s = {};
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const float4 x =
+          *reinterpret_cast<const float4*>(k + row * (D * 4) + k_place(row, 4 * j + g) * 16);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(x.x, q[4 * j], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(x.y, q[4 * j + 1], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(x.z, q[4 * j + 2], s, 0, 0, 0);
+      s = __builtin_amdgcn_mfma_f32_16x16x4f32(x.w, q[4 * j + 3], s, 0, 0, 0);
+    }
+    return s;
+  }
+  template <int N>
+  __device__ static __forceinline__ void pv(const unsigned char* v, int tok0, const Vec (&p)[N],
+                                            bool, bool, Vec (&acc)[NDB], int lane) {
+    const int dim = lane & 15;
+#pragma unroll
+    for (int i = 0; i < N * kVals; ++i) {
+      const int row = tok0 + i / kVals * kTok + token_of(i % kVals, lane);
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        const float x = *reinterpret_cast<const float*>(
+            v + row * (D * 4) + v_place(row, 4 * db + (dim >> 2)) * 16 + (dim & 3) * 4);
+        acc[db] = __builtin_amdgcn_mfma_f32_16x16x4f32(x, p[i / kVals][i % kVals], acc[db], 0, 0, 0);
+      }
+    }
+  }
+};
+
+// Orders the scheduler's region: AHEAD operand reads from LDS, then one more for
+// each of the N matrix instructions. (Left alone the compiler puts every read
+// right before its use, and the matrix instructions wait for LDS one by one.)
+template <int N, int AHEAD>
+__device__ __forceinline__ void interleave() {
+  constexpr int kMfma = 0x8, kRead = 0x100;
+  __builtin_amdgcn_sched_group_barrier(kRead, AHEAD, 0);
+  static_for<0, N - AHEAD>([](auto) {
+    __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(kRead, 1, 0);
+  });
+  __builtin_amdgcn_sched_group_barrier(kMfma, AHEAD, 0);
+}
+
+// A workgroup of four waves. RW = 1: every wave takes the same query rows (up to
+// kRows) and tiles of its own, in its own part of the LDS, with no barrier in the
+// loop: what memory bounds. RW = 2 or 4: RW waves with 32 rows each, and 4 / RW
+// such groups that share the tokens of a tile.
 template <typename T, int D, int RW>
 struct Flash {
-  static constexpr int TW = 4 / RW;              // groups that share a tile's tokens
-  static constexpr int NT = flash_tile(sizeof(T), RW);
-  static constexpr int kSub = NT / TW / 32;      // 32-token steps of a wave in a tile
-  static constexpr int kBytes = NT * D * (int)sizeof(T);   // of K, and of V
-  static constexpr int NCH = kBytes / 16 / 256;  // chunks of each per thread
-  static constexpr int NDB = D / 32;
+  using O = Ops<T, D, RW>;
+  using Vec = typename O::Vec;
+  static constexpr int TW = 4 / RW;              // groups with tokens of their own
+  static constexpr int NTG = flash_tile(sizeof(T), RW);   // tokens of a workgroup's step
+  static constexpr int NT = RW == 1 ? NTG / 4 : NTG;      // of one tile in LDS
+  static constexpr int NTHR = RW == 1 ? 64 : 256;         // threads that load it
+  static constexpr int kSub = NTG / TW / O::kTok;         // steps of a wave in it
+  static constexpr int kBytes = NT * D * (int)sizeof(T);  // of K, and of V
+  static constexpr int NCH = kBytes / 16 / NTHR; // chunks of each per thread
+  static constexpr int NDB = O::NDB;
+  // two buffers save the barrier before a tile is written
+  static constexpr int kBuf = RW > 1 && 4 * kBytes <= (64 << 10) ? 2 : 1;
+  static constexpr int kTiles = (RW == 1 ? 4 : kBuf) * 2 * kBytes;
   // the groups' accumulators are added in LDS
-  static constexpr int kMerge = TW > 1 ? 4 * 32 * D * 4 : 0;
-  static constexpr int kLds = 2 * kBytes > kMerge ? 2 * kBytes : kMerge;
-  using O = Ops<T, D>;
+  static constexpr int kMerge = TW > 1 ? 4 * O::kRows * D * 4 : 0;
+  static constexpr int kLds = kTiles > kMerge ? kTiles : kMerge;
 
   // Rows [r0, r1) of K and V (r1 > r0) for the query rows of this workgroup:
   // row_q(i) points to row i < rows; the partials go to acc_out [rows][D] and
   // ml_out [rows][2]. With LOG the logits of row i go to log_out + i * log_stride,
-  // by token.
+  // by token; rows is a power of two then, at most 8.
   template <bool LOG, typename RowQ>
   __device__ static __forceinline__ void block(const T* __restrict__ K, const T* __restrict__ V,
                                                int64_t r0, int64_t r1, int rows, float qscale,
                                                RowQ&& row_q, float* acc_out, float* ml_out,
                                                float* log_out, int64_t log_stride,
-                                               unsigned char* lds, float (*wm)[32 * RW],
-                                               float (*wl)[32 * RW]) {
+                                               unsigned char* lds, float (*wm)[O::kRows * RW],
+                                               float (*wl)[O::kRows * RW]) {
+    // The running maximum may lag the true one by this much (in log2): p grows
+    // to 256 at most, which no sum minds, and the accumulators are rescaled once
+    // or twice a run instead of whenever one of a wave's rows meets a new
+    // maximum.
+    constexpr float kSlack = 8.f;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rw = wave % RW, tw = wave / RW;
-    const int h = lane >> 5, col = lane & 31;
+    const int col = lane % O::kRows;
     const bool twice = RW == 1 && sizeof(T) == 2 && rows <= 16;
     const bool low = twice && col >= 16;
-    const int row = rw * 32 + (twice ? col & 15 : col);    // this lane's query row
-    unsigned char* kl = lds;
-    unsigned char* vl = lds + kBytes;
+    // this lane's query row (rows < 16 with logits: over and over)
+    const int row = rw * O::kRows + (twice ? col & 15 : col);
+    const int row_in = LOG ? col & (rows - 1) : min(row, rows - 1);
+    const int ltid = RW == 1 ? lane : tid;
+    unsigned char* tile0 = lds + (RW == 1 ? wave * 2 * kBytes : 0);
 
     O ops;
-    ops.load_q(row_q(min(row, rows - 1)), lane);
-    f32x16_t acc[NDB];
+    ops.load_q(row_q(row_in), lane);
+    Vec acc[NDB];
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) acc[db] = f32x16_t{};
+    for (int db = 0; db < NDB; ++db) acc[db] = Vec{};
     float m = -INFINITY, l = 0.f;
 
     uint4 kr[NCH], vr[NCH];
+    constexpr int kRowBytes = D * (int)sizeof(T);
     // rows behind the last are read as the last, and zeroed on the way to LDS
     // (their weight is 0, which an infinity there would turn into NaN)
     auto load = [&](int64_t at) {
+      const unsigned char* kb = reinterpret_cast<const unsigned char*>(K + at * D);
+      const unsigned char* vb = reinterpret_cast<const unsigned char*>(V + at * D);
+      auto get = [](const unsigned char* p) {
+        return RW < 4 ? ld_stream(p) : *reinterpret_cast<const uint4*>(p);
+      };
+      if (at + NT <= r1) {                       // uniform
 #pragma unroll
-      for (int i = 0; i < NCH; ++i) {
-        const int x = i * 256 + tid;
-        const int64_t r = min(at + x / O::CPR, r1 - 1);
-        const int64_t off = r * D + (x % O::CPR) * (16 / (int)sizeof(T));
-        kr[i] = RW < 4 ? ld_stream(K + off) : *reinterpret_cast<const uint4*>(K + off);
-        vr[i] = RW < 4 ? ld_stream(V + off) : *reinterpret_cast<const uint4*>(V + off);
+        for (int i = 0; i < NCH; ++i) kr[i] = get(kb + (i * NTHR + ltid) * 16);
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) vr[i] = get(vb + (i * NTHR + ltid) * 16);
+      } else {
+        const int last = (int)(r1 - at) - 1;
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+          const int x = i * NTHR + ltid, r = x / O::CPR;
+          const int off = min(r, last) * kRowBytes + x % O::CPR * 16;
+          kr[i] = get(kb + off);
+          vr[i] = get(vb + off);
+          if (r > last) vr[i] = make_uint4(0, 0, 0, 0);
+        }
       }
     };
-    load(r0);
-    for (int64_t at = r0; at < r1; at += NT) {
-      const int len = (int)min<int64_t>(NT, r1 - at);
-      if (at > r0) __syncthreads();              // the last tile is read
+    auto sync = [] {
+      if constexpr (RW == 1) {                   // (the wave reads what it wrote)
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      } else {
+        __syncthreads();
+      }
+    };
+    int64_t at = r0 + (RW == 1 ? wave * NT : 0);
+    if (at < r1) load(at);
+    int buf = 0;
+#pragma unroll 1
+    for (; at < r1; at += NTG) {
+      unsigned char* kl = tile0 + buf * 2 * kBytes;
+      unsigned char* vl = kl + kBytes;
+      if (kBuf == 1) sync();                     // the last tile is read
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
-        const int x = i * 256 + tid, r = x / O::CPR, c = x % O::CPR;
-        if (len < NT && r >= len) vr[i] = make_uint4(0, 0, 0, 0);
+        const int x = i * NTHR + ltid, r = x / O::CPR, c = x % O::CPR;
         *reinterpret_cast<uint4*>(kl + (r * O::CPR + O::k_place(r, c)) * 16) = kr[i];
         *reinterpret_cast<uint4*>(vl + (r * O::CPR + O::v_place(r, c)) * 16) = vr[i];
       }
-      __syncthreads();
-      if (at + NT < r1) load(at + NT);
+      sync();
+      if (at + NTG < r1) load(at + NTG);
       __builtin_amdgcn_sched_barrier(0);
+      buf = kBuf == 2 ? buf ^ 1 : 0;
+      const int len = (int)min<int64_t>(NT, r1 - at);
+      const int tok0 = RW == 1 ? 0 : tw * kSub * O::kTok;
+      Vec s[kSub];
 #pragma unroll
-      for (int sub = 0; sub < kSub; ++sub) {
-        const int tok0 = (tw * kSub + sub) * 32;
-        if (tok0 >= len) break;                  // wave-uniform
-        f32x16_t s = ops.logits(kl, tok0, lane);
-        if constexpr (LOG) {
-          if (row < rows && !low) {
+      for (int sub = 0; sub < kSub; ++sub) s[sub] = ops.logits(kl, tok0 + sub * O::kTok, lane);
+      if constexpr (sizeof(T) == 2) interleave<kSub * D / 16, D / 32>();
+      if constexpr (LOG) {
+        // Row r's logits are in the columns r, r + rows, ...: copy u writes the
+        // u-th four of the lane's tokens, so that a step's logits of a row leave
+        // as whole lines by one store.
+        static_assert(kSub == 1, "one step per tile");
+        const int u = col / rows;
+        float4 v = make_float4(s[0][0], s[0][1], s[0][2], s[0][3]);
+        int tok = O::token_of(0, lane);
 #pragma unroll
-            for (int i = 0; i < 16; i += 4) {
-              const int tok = tok0 + token_of(i, h);
-              if (tok < len)                     // (rows come in fours, padded)
-                *reinterpret_cast<float4*>(log_out + row * log_stride + at + tok) =
-                    make_float4(s[i], s[i + 1], s[i + 2], s[i + 3]);
-            }
+        for (int i = 4; i < O::kVals; i += 4)
+          if (4 * u == i) {
+            v = make_float4(s[0][i], s[0][i + 1], s[0][i + 2], s[0][i + 3]);
+            tok = O::token_of(i, lane);
           }
-        }
-        if (tok0 + 32 > len) {                   // uniform
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = tok0 + token_of(i, h) < len ? s[i] : -INFINITY;
-        }
-        float mt = s[0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) mt = fmaxf(mt, s[i]);
-        float lo, hi;
-        xor_pair<32>(mt, lo, hi);
-        const float mn = fmaxf(m, fmaxf(lo, hi) * qscale);
-        const float mref = mn == -INFINITY ? 0.f : mn;
-        if (__ballot(mn != m)) {                 // some row's maximum grew
-          const float scale = fast_exp2(m - mref);   // 0 on the row's first tile
-          l *= scale;
-#pragma unroll
-          for (int db = 0; db < NDB; ++db)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[db][i] *= scale;
-          m = mn;
-        }
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          s[i] = fast_exp2(fmaf(s[i], qscale, -mref));
-          sum += s[i];
-        }
-        l += sum;
-        ops.pv(vl, tok0, s, twice, low, acc, lane);
+        if (4 * u < O::kVals && tok < len)       // (rows come in fours, padded)
+          *reinterpret_cast<float4*>(log_out + row_in * log_stride + at + tok) = v;
       }
+      if (len < NT) {                            // uniform
+#pragma unroll
+        for (int sub = 0; sub < kSub; ++sub)
+#pragma unroll
+          for (int i = 0; i < O::kVals; ++i)
+            s[sub][i] = tok0 + sub * O::kTok + O::token_of(i, lane) < len ? s[sub][i] : -INFINITY;
+      }
+      float mt = s[0][0];
+#pragma unroll
+      for (int sub = 0; sub < kSub; ++sub)
+#pragma unroll
+        for (int i = 0; i < O::kVals; ++i) mt = fmaxf(mt, s[sub][i]);
+      const float mn = O::row_maximum(mt) * qscale;
+      if (__ballot(mn > m + kSlack)) {
+        const float top = fmaxf(m, mn);
+        const float scale = top == -INFINITY ? 1.f : fast_exp2(m - top);   // 0 at first
+        l *= scale;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int i = 0; i < (int)(sizeof(Vec) / 4); ++i) acc[db][i] *= scale;
+        m = top;
+      }
+      const float mref = m == -INFINITY ? 0.f : m;
+      float sum = 0.f;
+#pragma unroll
+      for (int sub = 0; sub < kSub; ++sub)
+#pragma unroll
+        for (int i = 0; i < O::kVals; ++i) {
+          s[sub][i] = fast_exp2(fmaf(s[sub][i], qscale, -mref));
+          sum += s[sub][i];
+        }
+      l += sum;
+      O::pv(vl, tok0, s, twice, low, acc, lane);
     }
-    l = xor_sum<32>(l);
+    l = O::row_total(l);
+    constexpr int kAccVals = (int)(sizeof(Vec) / 4);
     if (twice) {                                 // the two parts of p
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[db][i] = xor_sum<16>(acc[db][i]);
+        for (int i = 0; i < kAccVals; ++i) acc[db][i] = xor_sum<16>(acc[db][i]);
     }
     const bool mine = row < rows && !low;
+    const bool first = lane < O::kRows;          // one lane of a row
     if constexpr (TW == 1) {
       if (!mine) return;
 #pragma unroll
       for (int db = 0; db < NDB; ++db)
 #pragma unroll
-        for (int i = 0; i < 16; i += 4)
-          *reinterpret_cast<float4*>(acc_out + (int64_t)row * D + 32 * db + token_of(i, h)) =
+        for (int i = 0; i < kAccVals; i += 4)
+          *reinterpret_cast<float4*>(acc_out + (int64_t)row * D + O::kDims * db + O::dim_of(i, lane)) =
               make_float4(acc[db][i], acc[db][i + 1], acc[db][i + 2], acc[db][i + 3]);
-      if (h == 0) *reinterpret_cast<float2*>(ml_out + 2 * row) = make_float2(m, l);
+      if (first) *reinterpret_cast<float2*>(ml_out + 2 * row) = make_float2(m, l);
     } else {
-      constexpr int RS = 32 * RW;
+      constexpr int RS = O::kRows * RW;
       float* wacc = reinterpret_cast<float*>(lds);
       // 16-byte pieces of a row at places XORed with the row
       auto place = [](int r, int piece) { return piece ^ (r & (D / 4 - 1)); };
@@ -312,11 +482,12 @@ struct Flash {
 #pragma unroll
         for (int db = 0; db < NDB; ++db)
 #pragma unroll
-          for (int i = 0; i < 16; i += 4)
-            *reinterpret_cast<float4*>(wacc + (tw * RS + row) * D +
-                                       4 * place(row, 8 * db + token_of(i, h) / 4)) =
+          for (int i = 0; i < kAccVals; i += 4)
+            *reinterpret_cast<float4*>(
+                wacc + (tw * RS + row) * D +
+                4 * place(row, (O::kDims * db + O::dim_of(i, lane)) / 4)) =
                 make_float4(acc[db][i], acc[db][i + 1], acc[db][i + 2], acc[db][i + 3]);
-        if (h == 0) { wm[tw][row] = m; wl[tw][row] = l; }
+        if (first) { wm[tw][row] = m; wl[tw][row] = l; }
       }
       __syncthreads();
       for (int x = tid; x < rows * (D / 4); x += 256) {
@@ -345,49 +516,55 @@ struct Flash {
 // i + 8 share an XCD and its L2: the row tiles of one (kv head, split) read the
 // same rows and lie 8 apart.
 template <typename T, int D, int RW, bool LOG>
-__global__ __launch_bounds__(256, flash_wgs(sizeof(T), D)) void k_flash(FlashArgs a) {
+__global__ __launch_bounds__(256, 2) void k_flash(FlashArgs a) {
   using F = Flash<T, D, RW>;
   using F1 = Flash<T, D, 1>;
   constexpr int kLds = F::kLds > F1::kLds ? F::kLds : F1::kLds;
   __shared__ __attribute__((aligned(16))) unsigned char lds[kLds];
-  __shared__ float wm[4][32], wl[4][32];         // [TW][32 RW]
+  __shared__ float wm[4 * 32], wl[4 * 32];       // [TW][rows]
   const int n_units = a.Hkv * a.splits;          // (kv head, split)
   const int n_prefix = (n_units + 7) / 8 * 8 * a.mtiles;
   int i = blockIdx.x;
   if constexpr (!LOG) {
     if (i < n_prefix) {
+      using RowArray = float (*)[F::O::kRows * RW];
       const int unit = i / (8 * a.mtiles) * 8 + i % 8, mt = i / 8 % a.mtiles;
       if (unit >= n_units) return;
       const int hk = unit / a.splits, sp = unit % a.splits;
-      const int64_t r0 = (int64_t)sp * a.tiles_p * F::NT;
-      const int64_t r1 = min(a.P, r0 + (int64_t)a.tiles_p * F::NT);
-      const int row0 = mt * 32 * RW;
+      const int64_t r0 = (int64_t)sp * a.tiles_p * F::NTG;
+      const int64_t r1 = min(a.P, r0 + (int64_t)a.tiles_p * F::NTG);
+      const int row0 = mt * F::O::kRows * RW;
       const int64_t at = (int64_t)unit * a.M + row0;
       F::template block<false>(
           static_cast<const T*>(a.Kp) + hk * a.Pcap * D, static_cast<const T*>(a.Vp) + hk * a.Pcap * D,
-          r0, r1, min(a.M - row0, 32 * RW), a.qscale,
+          r0, r1, min(a.M - row0, F::O::kRows * RW), a.qscale,
           [&](int r) {
             const int x = row0 + r;              // b G + g
             return static_cast<const T*>(a.q) + ((int64_t)(x / a.G) * a.Hq + hk * a.G + x % a.G) * D;
           },
-          a.pacc + at * D, a.pml + at * 2, nullptr, 0, lds,
-          reinterpret_cast<float (*)[32 * RW]>(wm), reinterpret_cast<float (*)[32 * RW]>(wl));
+          a.pacc + at * D, a.pml + at * 2, nullptr, 0, lds, reinterpret_cast<RowArray>(wm),
+          reinterpret_cast<RowArray>(wl));
       return;
     }
     i -= n_prefix;
   }
-  const int64_t bh = i / a.parts, part = i % a.parts;
+  using RowArray = float (*)[F1::O::kRows];
+  // (the parts of a pair on different XCDs, and an XCD's parts of different pairs:
+  // pairs of a ragged batch have different numbers of them)
+  const int pairs = a.B * a.Hkv, part = i / pairs;
+  const int64_t bh = (i + part) % pairs;
   const int64_t b = bh / a.Hkv, hk = bh % a.Hkv;
   const int64_t len = own_len(a, b, LOG ? 1 : 0);
-  const int64_t r0 = part * a.tiles_o * F1::NT;
+  const int64_t r0 = (int64_t)part * a.tiles_o * F1::NTG;
   if (r0 >= len) return;
-  const int64_t r1 = min(len, r0 + (int64_t)a.tiles_o * F1::NT);
+  const int64_t r1 = min(len, r0 + (int64_t)a.tiles_o * F1::NTG);
   const int64_t at = (bh * a.parts + part) * a.G;
   F1::template block<LOG>(
       static_cast<const T*>(a.K) + bh * a.cap * D, static_cast<const T*>(a.V) + bh * a.cap * D, r0, r1,
       a.G, a.qscale,
       [&](int r) { return static_cast<const T*>(a.q) + (b * a.Hq + hk * a.G + r) * D; },
-      a.oacc + at * D, a.oml + at * 2, a.logits + bh * a.G * a.tpad, a.tpad, lds, wm, wl);
+      a.oacc + at * D, a.oml + at * 2, a.logits + bh * a.G * a.tpad, a.tpad, lds,
+      reinterpret_cast<RowArray>(wm), reinterpret_cast<RowArray>(wl));
 }
 
 template <typename T, int D>

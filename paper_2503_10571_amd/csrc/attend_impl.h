@@ -9,8 +9,8 @@ namespace radar_impl {
 
 // A call's attention is cut into blocks, one workgroup each, that leave a
 // partial (max, sum, acc[d]) for each of their query rows:
-//  - of the shared prefix: (kv head, row tile, split), 32 RW query rows b G + g
-//    against tiles_p tiles of prefix rows;
+//  - of the shared prefix: (kv head, row tile, split), flash_rows query rows b G +
+//    g against tiles_p tiles of prefix rows;
 //  - of the sequences' own rows: (b, kv head, part), the G query rows of the
 //    pair against tiles_o tiles.
 struct FlashArgs {
@@ -32,13 +32,12 @@ struct FlashArgs {
   int64_t tpad;
 };
 
-// rows a tile holds, by element size and row waves
+// cache rows of a workgroup's step, by element size and row waves
 constexpr int flash_tile(int esz, int rw) {
-  return rw == 1 ? 128 : esz == 2 || rw == 2 ? 64 : 32;
+  return rw == 1 ? (esz == 2 ? 128 : 64) : esz == 2 || rw == 2 ? 64 : 32;
 }
-// workgroups of a CU that run at once: the LDS holds two tiles of 64 KB, or one
-// of 128 KB
-constexpr int flash_wgs(int esz, int d) { return esz == 4 && d == 128 ? 1 : 2; }
+// query rows of a workgroup
+constexpr int flash_rows(int esz, int rw) { return rw == 1 && esz == 4 ? 16 : 32 * rw; }
 // a sequence's own rows: its length, or -1 where lens holds none in [lo, t]
 __device__ __forceinline__ int64_t own_len(const FlashArgs& a, int64_t b, int lo) {
   const int64_t n = a.lens ? a.lens[b] : a.t;
