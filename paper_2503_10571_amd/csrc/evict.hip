@@ -11,14 +11,23 @@ struct EvictArgs {
   const int64_t* lens;
   int64_t* new_lens;
   int32_t* kept;
-  int* src;                // [B Hkv][n]: the rows that stay, ascending
   int* cut;                // [B Hkv]: the length where it is cut, else -1
+  int* turn;               // [B Hkv][2]: chunks of K and V taken so far
+  int* arrived;            // [B Hkv][2][chunks]: the chunk is in registers
+  int* src;                // [B Hkv][n]: the rows that stay, ascending
   int B, Hkv;
   int64_t t, cap;
   int sink, heavy, recent;
   int64_t n;               // sink + heavy + recent
   int n_kept;              // min(n, t): row length of kept
-  int row_bytes;
+  int row_bytes, chunks;
+  // caches of more than kStep rows: slices of slice_rows
+  int slices, slice_rows;
+  int* hist;               // [B Hkv][slices][kBins]
+  int4* found;             // [B Hkv]: leading bits, how many of them to take, all
+  int2* counts;            // [B Hkv][slices]: rows above the bin, rows in it
+  uint32_t* list;          // [B Hkv][slices][slice_rows]: the keys in the bin
+  float* moved;            // [B Hkv][n]: the masses of the rows that stay
 };
 
 // order-preserving key of a mass: larger is better; -0 as 0, a NaN above all
@@ -28,182 +37,515 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
   return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// One workgroup per (b, kv head): the heavy-th largest key of the rows between
-// the sinks and the recent ones by a radix search over 11, 11 and 10 bits, then
-// one ascending pass that lists the rows and moves the masses.
-constexpr int kSelThreads = 1024;
-constexpr int kBins = 2048;
+// ---------------------------------------------------------------------------
+// which rows stay
+// ---------------------------------------------------------------------------
+// The heavy-th largest key of the rows between the sinks and the recent ones, by
+// a radix search: a histogram of the keys' upper 11 bits gives its bin; the
+// bin's keys are listed and ranked (up to kRank), or searched by two more
+// histograms (11 and 10 bits). Then one ascending pass lists the rows.
+//
+// A cache of up to kStep rows takes one workgroup and one kernel that holds its
+// masses in registers. Longer ones are cut into slices, a workgroup each, and the
+// three stages are kernels: one workgroup alone spends 2.2 us on a stage's 8192
+// rows (86 us for 65600 rows of 48 pairs, 42 in slices).
+constexpr int kSelThreads = 1024, kPer = 8;
+constexpr int kStep = kSelThreads * kPer;
+constexpr int kSlices = 32;                // at most
+constexpr int64_t kMostRows = INT32_MAX - 2 * kStep;   // row numbers of a step fit 32 bits
+constexpr int kBins = 2048, kRank = 256;   // (1024 keys: 25 us to rank, 6 by two histograms)
+constexpr int kSelWaves = kSelThreads / kWave;
 
-__global__ __launch_bounds__(kSelThreads) void k_evict_select(EvictArgs a) {
-  __shared__ int hist[kBins];
-  __shared__ int wsum[kSelThreads / kWave];
-  __shared__ int pick[2];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t bh = blockIdx.x, b = bh / a.Hkv;
+// Histograms in LDS are kept four times, by lane, side by side: a wave's keys
+// share few bins (rows that were never met share one), and additions to one
+// place follow one another.
+constexpr int kCopies = 4;
+
+// what the workgroup of a pair works on
+struct Rows {
+  int64_t bh;
+  int len, lo, hi;         // rows [lo, hi) are candidates
+  int begin, end;          // this workgroup's
+  float* mass;
+};
+
+// Fills the rows of slice `slice` of pair bh; false where there are none. The
+// first slice's workgroup also sets what the move needs, and what an uncut
+// sequence gets.
+__device__ __forceinline__ bool rows_of(const EvictArgs& a, int64_t bh, int slice, int slice_rows,
+                                        bool first_kernel, Rows* r) {
+  const int tid = threadIdx.x;
+  const int64_t b = bh / a.Hkv;
   const int64_t len64 = a.lens ? a.lens[b] : a.t;
-  const int64_t cut = len64 > a.n && len64 <= a.t ? len64 : -1;
-  if (tid == 0) a.cut[bh] = (int)cut;
-  int32_t* kept = a.kept ? a.kept + bh * a.n_kept : nullptr;
-  if (cut < 0) {
-    if (kept)
+  const bool cut = len64 > a.n && len64 <= a.t;
+  if (first_kernel && slice == 0) {
+    if (tid == 0) a.cut[bh] = cut ? (int)len64 : -1;
+    if (cut) {
+      for (int i = tid; i < 2 * a.chunks; i += kSelThreads) a.arrived[bh * 2 * a.chunks + i] = 0;
+      if (tid < 2) a.turn[bh * 2 + tid] = 0;
+    } else if (a.kept) {
       for (int i = tid; i < a.n_kept; i += kSelThreads)
-        kept[i] = len64 <= a.t && i < len64 ? i : -1;
-    return;
+        a.kept[bh * a.n_kept + i] = len64 <= a.t && i < len64 ? i : -1;
+    }
   }
-  const int len = (int)cut, lo = a.sink, hi = len - a.recent;
-  float* mass = a.mass + bh * a.cap;
-  // (prefix, mask): the leading bits of the heavy-th largest key found so far,
-  // of which `need` are still to be taken among the keys that match
-  uint32_t prefix = 0, mask = 0;
-  int need = a.heavy;
-#pragma unroll 1
-  for (int pass = 0; pass < 3 && need > 0; ++pass) {
-    const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-    const int bits = pass == 2 ? 10 : 11;
-    for (int i = tid; i < kBins; i += kSelThreads) hist[i] = 0;
-    __syncthreads();
-    for (int i0 = lo; i0 < hi; i0 += kSelThreads) {
-      const int i = i0 + tid;
-      const uint32_t u = i < hi ? mass_key(mass[i]) : 0;
-      const bool in = i < hi && (u & mask) == prefix;
-      const int bin = (int)(u >> shift) & ((1 << bits) - 1);
-      // (rows that were never met share a bin: one addition for the wave)
-      const u64 some = __ballot(in);
-      if (some == 0) continue;
-      const int first = __builtin_amdgcn_readlane(bin, (int)__builtin_ctzll(some));
-      if (__ballot(in && bin != first) == 0) {
-        if (lane == 0) atomicAdd(&hist[first], (int)__popcll(some));
-      } else if (in) {
-        atomicAdd(&hist[bin], 1);
-      }
-    }
-    __syncthreads();
-    // the bin, from the top, in which the need-th key lies: thread x takes bins
-    // 2 x and 2 x + 1 from the top
-    const int nb = 1 << bits;
-    const int b0 = nb - 1 - 2 * tid, b1 = b0 - 1;
-    const int c0 = b0 >= 0 ? hist[b0] : 0, c1 = b1 >= 0 ? hist[b1] : 0;
-    const int incl = wave_incl_scan(c0 + c1, lane);
-    if (lane == kWave - 1) wsum[wave] = incl;
-    __syncthreads();
-    int before = incl - (c0 + c1);
-    for (int w = 0; w < wave; ++w) before += wsum[w];
-    if (before < need && need <= before + c0) { pick[0] = b0; pick[1] = before; }
-    else if (before + c0 < need && need <= before + c0 + c1) { pick[0] = b1; pick[1] = before + c0; }
-    __syncthreads();
-    prefix |= (uint32_t)pick[0] << shift;
-    mask |= ((uint32_t)(nb - 1)) << shift;
-    need -= pick[1];
-    __syncthreads();
-  }
-  // keys above `prefix` stay, and the first `need` of those equal to it
-  int* src = a.src + bh * a.n;
-  int n_out = 0, n_eq = 0;                 // listed so far, equal keys so far
-#pragma unroll 1
-  for (int i0 = 0; i0 < len; i0 += kSelThreads) {
-    const int i = i0 + tid;
-    float x = 0.f;
-    bool take = false, eq = false;
-    if (i < len) {
-      x = mass[i];
-      if (i < lo || i >= hi) {
-        take = true;
-      } else if (a.heavy > 0) {
-        const uint32_t u = mass_key(x);
-        take = u > prefix;
-        eq = u == prefix;
-      }
-    }
-    // ranks among the equal keys, then among the rows taken
-    const u64 be = __ballot(eq);
-    const u64 below = lane == 0 ? 0ull : ~0ull >> (64 - lane);
-    if (lane == 0) wsum[wave] = (int)__popcll(be);
-    __syncthreads();
-    int eq_before = n_eq, eq_all = 0;
-    for (int w = 0; w < kSelThreads / kWave; ++w) {
-      eq_before += w < wave ? wsum[w] : 0;
-      eq_all += wsum[w];
-    }
-    if (eq && eq_before + (int)__popcll(be & below) < need) take = true;
-    n_eq += eq_all;
-    __syncthreads();
-    const u64 bt = __ballot(take);
-    if (lane == 0) wsum[wave] = (int)__popcll(bt);
-    __syncthreads();
-    int at = n_out, all = 0;
-    for (int w = 0; w < kSelThreads / kWave; ++w) {
-      at += w < wave ? wsum[w] : 0;
-      all += wsum[w];
-    }
-    // (every mass of this step is read: the place is at most the row itself)
-    if (take) {
-      at += (int)__popcll(bt & below);
-      src[at] = i;
-      mass[at] = x;
-      if (kept) kept[at] = i;
-    }
-    n_out += all;
-    __syncthreads();
-  }
-  for (int i = (int)a.n + tid; i < len; i += kSelThreads) mass[i] = 0.f;
+  if (!cut) return false;
+  r->bh = bh;
+  r->len = (int)len64;
+  r->lo = a.sink;
+  r->hi = r->len - a.recent;
+  r->begin = slice * slice_rows;
+  r->end = min(r->len, r->begin + slice_rows);
+  r->mass = a.mass + bh * a.cap;
+  return r->begin < r->len;
 }
 
-// The rows' move: row i takes row src[i] >= i. A workgroup takes one 128-byte
-// column of a (b, kv head)'s K or V and goes through the rows in ascending
-// blocks: a block's rows are all in registers before any is written, and the
-// rows of later blocks lie behind everything written so far, so the next block
-// is loaded while this one is written. The new lengths, which may replace the old
-// ones, are written here, when nobody reads those any more.
-constexpr int kMoveThreads = 512, kMoveRows = 8;   // 16-byte chunks per thread
+// a step's rows: i0 + 512 wave + 64 j + lane
+__device__ __forceinline__ int step_row(int i0, int j) {
+  return i0 + (int)(threadIdx.x & ~63u) * kPer + j * kWave + (int)(threadIdx.x & 63u);
+}
+__device__ __forceinline__ void load_step(const Rows& r, int i0, float (&x)[kPer]) {
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) x[j] = r.mass[min(step_row(i0, j), r.len - 1)];
+}
+// f(first row of the step, its masses) over the workgroup's rows; a step's loads
+// are in flight together, and the next step's beside this one's work
+template <typename F>
+__device__ __forceinline__ void each_step(const Rows& r, F&& f) {
+  float x[kPer], y[kPer];
+  load_step(r, r.begin, x);
+#pragma unroll 1
+  for (int i0 = r.begin; i0 < r.end; i0 += kStep) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) y[j] = x[j];
+    if (i0 + kStep < r.end) load_step(r, i0 + kStep, x);
+    f(i0, y);
+  }
+}
 
+__device__ __forceinline__ void clear_bins(int* hist) {
+  for (int i = threadIdx.x; i < kBins * kCopies; i += kSelThreads) hist[i] = 0;
+  __syncthreads();
+}
+__device__ __forceinline__ void add_bin(int* hist, int bin) {
+  atomicAdd(&hist[bin * kCopies + (threadIdx.x & (kCopies - 1))], 1);
+}
+__device__ __forceinline__ int bin_count(const int* hist, int bin) {
+  const int4 v = *reinterpret_cast<const int4*>(hist + bin * kCopies);
+  return (v.x + v.y) + (v.z + v.w);
+}
+
+// The bin, from the top, that holds the need-th key: x its number, y the keys
+// above it, z its own; count(bin): its keys. Thread x takes bins 2 x and 2 x + 1
+// from the top. A call of the whole workgroup.
+template <typename Count>
+__device__ __forceinline__ int3 pick_bin(int nb, int need, int* wsum, int* pick, Count&& count) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int b0 = nb - 1 - 2 * tid, b1 = b0 - 1;
+  const int c0 = b0 >= 0 ? count(b0) : 0, c1 = b1 >= 0 ? count(b1) : 0;
+  const int incl = wave_incl_scan(c0 + c1, lane);
+  if (lane == kWave - 1) wsum[wave] = incl;
+  __syncthreads();
+  int before = incl - (c0 + c1);
+  for (int w = 0; w < wave; ++w) before += wsum[w];
+  if (before < need && need <= before + c0) {
+    pick[0] = b0; pick[1] = before; pick[2] = c0;
+  } else if (before + c0 < need && need <= before + c0 + c1) {
+    pick[0] = b1; pick[1] = before + c0; pick[2] = c1;
+  }
+  __syncthreads();
+  const int3 got = make_int3(pick[0], pick[1], pick[2]);
+  __syncthreads();
+  return got;
+}
+
+// The need-th largest of n keys that share the bits of `prefix` under `mask`
+// (the upper 11): the key, and how many equal to it are to be taken. key(i): the
+// i-th. A call of the whole workgroup; ranks: kRank words of LDS.
+struct Threshold {
+  uint32_t key;
+  int need;
+};
+template <typename Key>
+__device__ __forceinline__ Threshold find_key(uint32_t prefix, int need, int n, Key&& key, int* hist,
+                                              uint32_t* ranks, int* wsum, int* pick) {
+  const int tid = threadIdx.x;
+  if (n <= kRank) {
+    if (tid < n) ranks[tid] = key(tid);
+    __syncthreads();
+    if (tid < n) {
+      const uint32_t u = ranks[tid];
+      int above = 0, equal = 0;
+#pragma unroll 8
+      for (int i = 0; i < n; ++i) {
+        above += ranks[i] > u ? 1 : 0;
+        equal += ranks[i] == u ? 1 : 0;
+      }
+      // (equal keys agree)
+      if (above < need && need <= above + equal) { pick[0] = (int)u; pick[1] = above; }
+    }
+    __syncthreads();
+    const Threshold got{(uint32_t)pick[0], need - pick[1]};
+    __syncthreads();
+    return got;
+  }
+  uint32_t mask = 0xffe00000u;
+#pragma unroll 1
+  for (int shift = 10; shift >= 0; shift -= 10) {
+    const int nb = shift ? 2048 : 1024;
+    clear_bins(hist);
+    for (int i = tid; i < n; i += kSelThreads) {
+      const uint32_t u = key(i);
+      if ((u & mask) == prefix) add_bin(hist, (int)(u >> shift) & (nb - 1));
+    }
+    __syncthreads();
+    const int3 b = pick_bin(nb, need, wsum, pick, [&](int x) { return bin_count(hist, x); });
+    prefix |= (uint32_t)b.x << shift;
+    mask |= (uint32_t)(nb - 1) << shift;
+    need -= b.y;
+  }
+  return {prefix, need};
+}
+
+// A step's part of the last pass: keys above the threshold stay, and the first
+// th.need of those equal to it. n_gt, n_eq: rows taken outright, and ties, before
+// the step, moved on behind it. put(place, row, mass) of every row that stays.
+// Every mass of the step is read before any is put: one barrier.
+template <typename Put>
+__device__ __forceinline__ void list_step(const EvictArgs& a, const Rows& r, const Threshold& th, int i0,
+                                          const float (&y)[kPer], int& n_gt, int& n_eq,
+                                          uint32_t* wcount, Put&& put) {
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  uint32_t gt_bits = 0, eq_bits = 0;       // of this lane's rows
+  uint32_t gt_all = 0, eq_all = 0;         // of the wave's
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int i = step_row(i0, j);
+    const uint32_t u = mass_key(y[j]);
+    const bool fixed = i < r.lo || i >= r.hi;
+    const bool gt = i < r.len && (fixed || (a.heavy > 0 && u > th.key));
+    const bool eq = i < r.len && !fixed && a.heavy > 0 && u == th.key;
+    gt_bits |= (gt ? 1u : 0u) << j;
+    eq_bits |= (eq ? 1u : 0u) << j;
+    gt_all += (uint32_t)__popcll(__ballot(gt));
+    eq_all += (uint32_t)__popcll(__ballot(eq));
+  }
+  if (lane == 0) wcount[wave] = gt_all | (eq_all << 16);   // (at most kStep each)
+  __syncthreads();
+  // the waves before this one, and all of them
+  const uint32_t c = lane < kSelWaves ? wcount[lane] : 0u;
+  const uint32_t incl = (uint32_t)wave_incl_scan((int)c, lane);
+  const uint32_t all = (uint32_t)__builtin_amdgcn_readlane((int)incl, kSelWaves - 1);
+  const uint32_t mine = (uint32_t)__builtin_amdgcn_readlane((int)(incl - c), wave);
+  int gt = n_gt + (int)(mine & 0xffffu), eq = n_eq + (int)(mine >> 16);
+  const u64 below = (1ull << lane) - 1;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const u64 bg = __ballot((gt_bits >> j) & 1u), be = __ballot((eq_bits >> j) & 1u);
+    const int eq_rank = eq + (int)__popcll(be & below);
+    if (((gt_bits >> j) & 1u) || (((eq_bits >> j) & 1u) && eq_rank < th.need))
+      put(gt + (int)__popcll(bg & below) + min(eq_rank, th.need), step_row(i0, j), y[j]);
+    gt += (int)__popcll(bg);
+    eq += (int)__popcll(be);
+  }
+  n_gt += (int)(all & 0xffffu);
+  n_eq += (int)(all >> 16);
+}
+
+// Appends the step's keys in the bin to `list`, of which n_list counts the
+// entries; returns this lane's rows above the bin (fixed rows too).
+__device__ __forceinline__ int collect_step(const Rows& r, uint32_t prefix, int i0,
+                                            const float (&y)[kPer], uint32_t* list, int* n_list) {
+  constexpr uint32_t kTop = 0xffe00000u;
+  const int lane = threadIdx.x & 63;
+  uint32_t u[kPer];
+  u64 in[kPer];
+  int n = 0, above = 0;
+#pragma unroll
+  for (int j = 0; j < kPer; ++j) {
+    const int i = step_row(i0, j);
+    u[j] = mass_key(y[j]);
+    const bool cand = i >= r.lo && i < r.hi;
+    in[j] = __ballot(cand && (u[j] & kTop) == prefix);
+    above += i < r.len && (!cand || (u[j] & kTop) > prefix) ? 1 : 0;
+    n += (int)__popcll(in[j]);
+  }
+  if (n > 0) {                             // wave-uniform
+    int at = 0;
+    if (lane == 0) at = atomicAdd(n_list, n);
+    at = __builtin_amdgcn_readfirstlane(at);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      if ((in[j] >> lane) & 1ull) list[at + (int)__popcll(in[j] & ((1ull << lane) - 1))] = u[j];
+      at += (int)__popcll(in[j]);
+    }
+  }
+  return above;
+}
+
+// caches of up to kStep rows; the masses move in place (a place is at most the
+// row itself)
+__global__ __launch_bounds__(kSelThreads) void k_evict_select(EvictArgs a) {
+  __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];
+  __shared__ uint32_t list[kStep];
+  __shared__ uint32_t ranks[kRank];
+  __shared__ int wsum[kSelWaves], pick[3], n_list;
+  __shared__ uint32_t wcount[kSelWaves];
+  const int tid = threadIdx.x;
+  Rows r;
+  if (!rows_of(a, blockIdx.x, 0, kStep, true, &r)) return;
+  float x[kPer];
+  load_step(r, 0, x);
+  Threshold th{0u, 0};
+  if (a.heavy > 0) {
+    if (tid == 0) n_list = 0;
+    clear_bins(hist);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (step_row(0, j) >= r.lo && step_row(0, j) < r.hi) add_bin(hist, (int)(mass_key(x[j]) >> 21));
+    __syncthreads();
+    const int3 b = pick_bin(kBins, a.heavy, wsum, pick, [&](int i) { return bin_count(hist, i); });
+    const uint32_t prefix = (uint32_t)b.x << 21;
+    collect_step(r, prefix, 0, x, list, &n_list);
+    __syncthreads();
+    th = find_key(prefix, a.heavy - b.y, b.z, [&](int i) { return list[i]; }, hist, ranks, wsum, pick);
+  }
+  int* src = a.src + r.bh * a.n;
+  int32_t* kept = a.kept ? a.kept + r.bh * a.n_kept : nullptr;
+  int n_gt = 0, n_eq = 0;
+  list_step(a, r, th, 0, x, n_gt, n_eq, wcount, [&](int at, int i, float m) {
+    src[at] = i;
+    r.mass[at] = m;
+    if (kept) kept[at] = i;
+  });
+  __syncthreads();
+  for (int i = (int)a.n + tid; i < r.len; i += kSelThreads) r.mass[i] = 0.f;
+}
+
+// the stages over slices: the histogram of each,
+__global__ __launch_bounds__(kSelThreads) void k_evict_hist(EvictArgs a) {
+  __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];
+  Rows r;
+  if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, true, &r)) return;
+  clear_bins(hist);
+  each_step(r, [&](int i0, const float (&y)[kPer]) {
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int i = step_row(i0, j);
+      if (i >= r.lo && i < min(r.hi, r.end)) add_bin(hist, (int)(mass_key(y[j]) >> 21));
+    }
+  });
+  __syncthreads();
+  int* out = a.hist + (r.bh * a.slices + blockIdx.x) * kBins;
+  for (int i = threadIdx.x; i < kBins; i += kSelThreads) out[i] = bin_count(hist, i);
+}
+
+// the bin of the whole, and each slice's keys in it and rows above it,
+__global__ __launch_bounds__(kSelThreads) void k_evict_bin(EvictArgs a) {
+  __shared__ int wsum[kSelWaves], pick[3], n_list, n_above;
+  Rows r;
+  if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, false, &r)) return;
+  const int slices = (r.len + a.slice_rows - 1) / a.slice_rows;
+  const int* hist = a.hist + r.bh * a.slices * kBins;
+  if (threadIdx.x == 0) { n_list = 0; n_above = 0; }
+  // (with nothing to choose, a bin above all keys)
+  int3 b = make_int3(kBins, 0, 0);
+  if (a.heavy > 0)
+    b = pick_bin(kBins, a.heavy, wsum, pick, [&](int i) {
+      int c = 0;
+#pragma unroll 8
+      for (int s = 0; s < slices; ++s) c += hist[s * kBins + i];
+      return c;
+    });
+  else
+    __syncthreads();
+  const uint32_t prefix = (uint32_t)b.x << 21;
+  const int64_t at = r.bh * a.slices + blockIdx.x;
+  int above = 0;
+  each_step(r, [&](int i0, const float (&y)[kPer]) {
+    if (a.heavy > 0) {
+      above += collect_step(r, prefix, i0, y, a.list + at * a.slice_rows, &n_list);
+    } else {
+#pragma unroll
+      for (int j = 0; j < kPer; ++j) {
+        const int i = step_row(i0, j);
+        above += i < r.len && (i < r.lo || i >= r.hi) ? 1 : 0;
+      }
+    }
+  });
+  above = wave_sum_i32(above);
+  if ((threadIdx.x & 63) == 0) atomicAdd(&n_above, above);
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    a.counts[at] = make_int2(n_above, n_list);
+    if (blockIdx.x == 0) a.found[r.bh] = make_int4((int)prefix, a.heavy - b.y, b.z, 0);
+  }
+}
+
+// and the rows that stay: every workgroup finds the threshold among all slices'
+// keys in the bin, and its place behind the slices before it
+__global__ __launch_bounds__(kSelThreads) void k_evict_list(EvictArgs a) {
+  __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];
+  __shared__ uint32_t ranks[kRank];
+  __shared__ uint32_t held[kStep];
+  __shared__ int wsum[kSelWaves], pick[3], ends[kSlices + 1], before[2];
+  __shared__ uint32_t wcount[2][kSelWaves];
+  const int tid = threadIdx.x, lane = tid & 63;
+  Rows r;
+  if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, false, &r)) return;
+  const int slices = (r.len + a.slice_rows - 1) / a.slice_rows;
+  const int mine = blockIdx.x;
+  const int2* counts = a.counts + r.bh * a.slices;
+  const uint32_t* list = a.list + r.bh * a.slices * (int64_t)a.slice_rows;
+  if (tid < kWave) {                       // slices <= 32: where each one's keys begin
+    const int2 c = lane < slices ? counts[lane] : make_int2(0, 0);
+    const int incl = wave_incl_scan(c.y, lane);
+    if (lane <= slices) ends[lane] = incl - c.y;
+    const int above = wave_sum_i32(lane < mine ? c.x : 0);
+    if (lane == 0) { before[0] = above; before[1] = 0; }
+  }
+  __syncthreads();
+  const int4 f = a.found[r.bh];
+  const bool fits = f.z <= kStep;          // all slices' keys, in LDS
+  if (fits) {
+    for (int s = 0; s < slices; ++s)
+      for (int i = tid; i < ends[s + 1] - ends[s]; i += kSelThreads)
+        held[ends[s] + i] = list[(int64_t)s * a.slice_rows + i];
+    __syncthreads();
+  }
+  auto key = [&](int i) {                  // of all slices' keys, in order
+    if (fits) return held[i];
+    int s = 0;
+    while (i >= ends[s + 1]) ++s;
+    return list[(int64_t)s * a.slice_rows + i - ends[s]];
+  };
+  Threshold th{0u, 0};
+  if (a.heavy > 0) {
+    th = find_key((uint32_t)f.x, f.y, f.z, key, hist, ranks, wsum, pick);
+    // the keys of the slices before this one that are above it or equal
+    int gt = 0, eq = 0;
+    for (int i = tid; i < ends[mine]; i += kSelThreads) {
+      const uint32_t u = key(i);
+      gt += u > th.key ? 1 : 0;
+      eq += u == th.key ? 1 : 0;
+    }
+    gt = wave_sum_i32(gt);
+    eq = wave_sum_i32(eq);
+    if (lane == 0 && gt) atomicAdd(&before[0], gt);
+    if (lane == 0 && eq) atomicAdd(&before[1], eq);
+    __syncthreads();
+  }
+  int n_gt = before[0], n_eq = before[1], parity = 0;
+  int* src = a.src + r.bh * a.n;
+  float* moved = a.moved + r.bh * a.n;
+  int32_t* kept = a.kept ? a.kept + r.bh * a.n_kept : nullptr;
+  each_step(r, [&](int i0, const float (&y)[kPer]) {
+    list_step(a, r, th, i0, y, n_gt, n_eq, wcount[parity], [&](int at, int i, float m) {
+      src[at] = i;
+      moved[at] = m;
+      if (kept) kept[at] = i;
+    });
+    parity ^= 1;
+  });
+}
+
+// ---------------------------------------------------------------------------
+// k_evict_move: row i of K and V takes row src[i] >= i, in place
+// ---------------------------------------------------------------------------
+// A workgroup moves a chunk of 128 KB of K or V (with 64 KB: 192 us below): it loads the chunk's rows into
+// registers, says so, and writes them once every chunk before it that reads rows
+// at or behind its own first place has said so too (the chunks behind it read
+// rows behind everything it writes). Chunks are handed out in ascending order,
+// so the ones waited for have started, and none of them waits before it has
+// loaded: every wait ends. What is waited for is that reads are over, no data
+// goes from one workgroup to another, so nothing has to be flushed. Moving whole
+// columns of a pair in order needs no waits but leaves few workgroups (315 us
+// for 48 pairs of 16K rows of 256 bytes, 182 this way: 4.4 TB/s).
+// The new lengths, which may replace the old ones, are written here, when nobody
+// reads those any more.
+constexpr int kMoveThreads = 512, kMoveVecs = 16;
+constexpr int kMoveBytes = kMoveThreads * kMoveVecs * 16;
+
+template <int CPR>                         // 16-byte chunks of a row
 __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a) {
+  constexpr int R = kMoveThreads * kMoveVecs / CPR;        // rows per chunk
+  __shared__ int turn;
+  __shared__ int from[R];
+  const int tid = threadIdx.x;
   const int64_t bh = blockIdx.y;
   const bool cut = a.cut[bh] >= 0;                 // workgroup-uniform
-  if (a.new_lens && bh % a.Hkv == 0 && blockIdx.x == 0 && blockIdx.z == 0 && threadIdx.x == 0) {
+  if (a.new_lens && bh % a.Hkv == 0 && blockIdx.x == 0 && blockIdx.z == 0 && tid == 0) {
     const int64_t b = bh / a.Hkv;
     a.new_lens[b] = cut ? a.n : a.lens ? a.lens[b] : a.t;
   }
-  if (!cut || a.n == 0) return;
-  constexpr int RPP = kMoveThreads / 8;            // rows per load instruction
-  constexpr int R = RPP * kMoveRows;               // rows per block
-  unsigned char* base = (blockIdx.z ? a.V : a.K) + bh * a.cap * a.row_bytes +
-                        (int64_t)blockIdx.x * 128 + (threadIdx.x & 7) * 16;
-  const int* src = a.src + bh * a.n;
-  const int r = threadIdx.x >> 3;
+  if (!cut) return;
   const int n = (int)a.n;
-  uint4 x[kMoveRows], y[kMoveRows];
-  auto load = [&](uint4 (&v)[kMoveRows], int i0) {
-#pragma unroll
-    for (int j = 0; j < kMoveRows; ++j) {
-      const int i = min(i0 + j * RPP + r, n - 1);
-      v[j] = *reinterpret_cast<const uint4*>(base + (int64_t)src[i] * a.row_bytes);
-    }
-  };
-  auto store = [&](const uint4 (&v)[kMoveRows], int i0) {
-#pragma unroll
-    for (int j = 0; j < kMoveRows; ++j) {
-      const int i = i0 + j * RPP + r;
-      if (i < n) *reinterpret_cast<uint4*>(base + (int64_t)i * a.row_bytes) = v[j];
-    }
-  };
-  // all loads of the block have arrived, for every thread of the workgroup
-  auto arrived = [&] {
-    __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0);
-    __syncthreads();
-    __builtin_amdgcn_sched_barrier(0);
-  };
-  load(x, 0);
-#pragma unroll 1
-  for (int i0 = 0; i0 < n; i0 += 2 * R) {
-    arrived();
-    if (i0 + R < n) load(y, i0 + R);
-    store(x, i0);
-    if (i0 + R >= n) break;
-    arrived();
-    if (i0 + 2 * R < n) load(x, i0 + 2 * R);
-    store(y, i0 + R);
+  if (blockIdx.z == 2) {                           // the masses, where slices listed them
+    float* mass = a.mass + bh * a.cap;
+    for (int i = blockIdx.x * kMoveThreads + tid; i < a.cut[bh]; i += gridDim.x * kMoveThreads)
+      mass[i] = i < n ? a.moved[bh * a.n + i] : 0.f;
+    return;
   }
+  if (n == 0) return;
+  const int64_t half = bh * 2 + blockIdx.z;
+  if (tid == 0) turn = atomicAdd(&a.turn[half], 1);
+  __syncthreads();
+  const int c = turn, i0 = c * R;
+  const int* src = a.src + bh * a.n;
+  int* arrived = a.arrived + half * a.chunks;
+  for (int i = tid; i < R; i += kMoveThreads) from[i] = src[min(i0 + i, n - 1)];
+  __syncthreads();
+  unsigned char* base = (blockIdx.z ? a.V : a.K) + bh * a.cap * a.row_bytes + (tid % CPR) * 16;
+  uint4 x[kMoveVecs];
+#pragma unroll
+  for (int j = 0; j < kMoveVecs; ++j)
+    x[j] = ld_stream(base + (int64_t)from[(j * kMoveThreads + tid) / CPR] * a.row_bytes);
+  // every load of this thread has arrived, then of every thread
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt(0);
+  __syncthreads();
+  if (tid == 0) __hip_atomic_store(&arrived[c], 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  for (int o = tid; o < c; o += kMoveThreads)
+    if (src[(o + 1) * R - 1] >= i0)
+      while (__hip_atomic_load(&arrived[o], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == 0)
+        __builtin_amdgcn_s_sleep(2);
+  __syncthreads();
+  __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+  for (int j = 0; j < kMoveVecs; ++j) {
+    const int i = i0 + (j * kMoveThreads + tid) / CPR;
+    if (i < n) *reinterpret_cast<uint4*>(base + (int64_t)i * a.row_bytes) = x[j];
+  }
+}
+
+// rows of a slice: whole steps, and at most kSlices slices
+int64_t slice_rows(int64_t t) { return ceil_div(ceil_div(t, kSlices), kStep) * kStep; }
+
+struct EvictWs {
+  size_t turn, arrived, src, hist, found, counts, list, moved, total;
+  int64_t chunks;
+};
+EvictWs evict_ws(const Shape& s, int64_t t, int64_t n) {
+  const size_t pairs = (size_t)s.B * s.Hkv;
+  const int row_bytes = s.d * (s.dt == RADAR_BF16 ? 2 : 4);
+  EvictWs w;
+  w.chunks = ceil_div(n * row_bytes, kMoveBytes);
+  w.turn = align256(pairs * 4);
+  w.arrived = w.turn + align256(pairs * 8);
+  w.src = w.arrived + align256(pairs * 2 * w.chunks * 4);
+  w.total = w.src + align256(pairs * n * 4);
+  w.hist = w.found = w.counts = w.list = w.moved = w.total;
+  if (t > kStep) {
+    // (bounds for every smaller t too, whose slices may be more)
+    const size_t steps = (size_t)ceil_div(t, kStep);
+    const size_t slices = std::min<size_t>(kSlices, steps);
+    w.found = w.hist + align256(pairs * slices * kBins * 4);
+    w.counts = w.found + align256(pairs * sizeof(int4));
+    w.list = w.counts + align256(pairs * slices * sizeof(int2));
+    w.moved = w.list + align256(pairs * (steps + steps / kSlices + 2) * kStep * 4);
+    w.total = w.moved + align256(pairs * n * 4);
+  }
+  return w;
 }
 
 }  // namespace
@@ -217,10 +559,10 @@ size_t radar_evict_workspace_bytes(const radar_config* cfg, int64_t t, int64_t h
                                    int64_t recent) {
   Shape s;
   if (check_cache(cfg, &s) != RADAR_OK || t < 0 || t > s.cap || heavy < 0 || recent < 0 ||
-      heavy > INT32_MAX || recent > INT32_MAX || s.n_sink + heavy + recent > INT32_MAX)
+      t > kMostRows || heavy > INT32_MAX || recent > INT32_MAX ||
+      s.n_sink + heavy + recent > INT32_MAX)
     return 0;
-  const int64_t n = std::min<int64_t>(s.n_sink + heavy + recent, t);
-  return align256((size_t)s.B * s.Hkv * n * 4) + align256((size_t)s.B * s.Hkv * 4);
+  return evict_ws(s, t, std::min<int64_t>(s.n_sink + heavy + recent, t)).total;
 }
 
 radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass, int64_t t,
@@ -236,28 +578,53 @@ radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass,
     return RADAR_EINVAL;
   if (t < 0 || t > s.cap) return RADAR_ECAPACITY;
   const size_t need = radar_evict_workspace_bytes(cfg, t, heavy, recent);
-  if (need == 0) return RADAR_EUNSUPPORTED;
+  if (need == 0) return RADAR_EUNSUPPORTED;            // (the sizes are checked there)
   if (!workspace || !aligned16(workspace) || workspace_bytes < need) return RADAR_EWORKSPACE;
   EvictArgs a{};
   a.K = static_cast<unsigned char*>(K);
   a.V = static_cast<unsigned char*>(V);
   a.mass = mass;
   a.lens = lens; a.new_lens = new_lens; a.kept = kept;
-  a.cut = static_cast<int*>(workspace);
-  a.src = a.cut + align256((size_t)s.B * s.Hkv * 4) / 4;
+  const EvictWs w = evict_ws(s, t, std::min<int64_t>(s.n_sink + heavy + recent, t));
+  unsigned char* ws = static_cast<unsigned char*>(workspace);
+  a.cut = reinterpret_cast<int*>(ws);
+  a.turn = reinterpret_cast<int*>(ws + w.turn);
+  a.arrived = reinterpret_cast<int*>(ws + w.arrived);
+  a.src = reinterpret_cast<int*>(ws + w.src);
+  a.chunks = (int)w.chunks;
+  a.hist = reinterpret_cast<int*>(ws + w.hist);
+  a.found = reinterpret_cast<int4*>(ws + w.found);
+  a.counts = reinterpret_cast<int2*>(ws + w.counts);
+  a.list = reinterpret_cast<uint32_t*>(ws + w.list);
+  a.moved = reinterpret_cast<float*>(ws + w.moved);
+  a.slice_rows = (int)slice_rows(t);
+  a.slices = t > 0 ? (int)ceil_div(t, a.slice_rows) : 1;
   a.B = s.B; a.Hkv = s.Hkv; a.t = t; a.cap = s.cap;
   a.sink = s.n_sink; a.heavy = (int)heavy; a.recent = (int)recent;
   a.n = s.n_sink + heavy + recent;
   a.n_kept = (int)std::min<int64_t>(a.n, t);
   a.row_bytes = s.d * (s.dt == RADAR_BF16 ? 2 : 4);
   const unsigned pairs = (unsigned)(s.B * s.Hkv);
-  launch(RADAR_K_TOPK, k_evict_select, dim3(pairs), dim3(kSelThreads), 0, stream, a);
+  const bool sliced = t > kStep && a.n < t;
+  if (sliced) {
+    const dim3 grid((unsigned)a.slices, pairs), block(kSelThreads);
+    launch(RADAR_K_TOPK, k_evict_hist, grid, block, 0, stream, a);
+    launch(RADAR_K_TOPK, k_evict_bin, grid, block, 0, stream, a);
+    launch(RADAR_K_TOPK, k_evict_list, grid, block, 0, stream, a);
+  } else {
+    launch(RADAR_K_TOPK, k_evict_select, dim3(pairs), dim3(kSelThreads), 0, stream, a);
+  }
   r = launch_status();
-  const bool moves = a.n > 0 && a.n < t;                   // else no row does
-  if (r != RADAR_OK || !(moves || new_lens)) return r;
-  launch(RADAR_K_APPEND, k_evict_move,
-         moves ? dim3((unsigned)(a.row_bytes / 128), pairs, 2) : dim3(1, pairs, 1),
-         dim3(kMoveThreads), 0, stream, a);
+  // (n = 0: the masses alone; n >= t: no sequence is longer)
+  const bool moves = a.n > 0 && a.n < t;
+  if (r != RADAR_OK || !(moves || sliced || new_lens)) return r;
+  const dim3 grid(std::max(1u, moves ? (unsigned)w.chunks : 1u), pairs, sliced ? 3 : moves ? 2 : 1);
+  auto go = [&](auto cpr) {
+    launch(RADAR_K_APPEND, k_evict_move<decltype(cpr)::value>, grid, dim3(kMoveThreads), 0, stream, a);
+  };
+  if (a.row_bytes == 128) go(std::integral_constant<int, 8>{});
+  else if (a.row_bytes == 256) go(std::integral_constant<int, 16>{});
+  else go(std::integral_constant<int, 32>{});
   return launch_status();
 }
 

@@ -131,7 +131,34 @@ def test_ties_and_special_masses(kind):
         _run(2, 2, 64, 2100, 4, heavy, 50, [2100, 2003], "f32", masses=masses)
 
 
+@pytest.mark.parametrize("t", [8191, 8192, 8193, 16385])
+def test_around_a_slice(t):
+    _run(2, 2, 64, t, 4, t // 3, 100, [t, t - 1], "bf16")
+
+
+def test_slices_of_ragged_sequences():
+    """Sequences that end in the first slice, at a slice's end, behind it."""
+    for heavy, recent in ((3000, 900), (0, 40), (5, 0), (0, 0)):
+        _run(5, 1, 64, 20000, 4, heavy, recent, [20000, 4500, 8192, 16384, 8193], "bf16")
+    _run(2, 1, 64, 9000, 0, 0, 0, [9000, 8000], "f32")
+
+
+@pytest.mark.parametrize("kind", ["zero", "few", "near"])
+def test_ties_across_slices(kind):
+    def masses(B, Hkv, cap, g):
+        if kind == "zero":
+            return torch.zeros(B, Hkv, cap)
+        if kind == "few":
+            return torch.randint(0, 3, (B, Hkv, cap), generator=g).float()
+        x = torch.randint(0, 3000, (B, Hkv, cap), generator=g, dtype=torch.int32) + 0x3f800000
+        return x.view(torch.float32)
+
+    for heavy in (1, 5000, 17000):
+        _run(1, 2, 64, 18001, 4, heavy, 50, None, "bf16", masses=masses)
+
+
 def test_long_cache():
+    _run(1, 1, 64, 270001, 4, 100000, 5000, None, "bf16")          # slices of two steps
     _run(1, 1, 64, 131077, 4, 60000, 5000, None, "bf16")
 
 
