@@ -529,13 +529,19 @@ class RadarLayer:
     schedule="fixed" keeps cfg.seg_len and cfg.window. schedule="sqrt"
     follows Algorithm 1's restructuring: at every perfect-square context
     length the summaries are rebuilt with c = sqrt(t), and each decode
-    attends the c restructured segments' top-k plus the buffer [c^2, t)."""
+    attends the c restructured segments' top-k plus the buffer [c^2, t).
+
+    rope: rotary positions (Rope); queries and keys are then given unrotated.
+    `pos` is the position of the next token: `t` until rows are evicted, the
+    number of tokens seen from then on. accumulate() and evict() make room in
+    a full cache by the weights that its rows get."""
 
     def __init__(self, cfg: Config, omega, K=None, V=None, t: int = 0,
-                 top_k: int = 16, device="cuda", schedule: str = "fixed"):
+                 top_k: int = 16, device="cuda", schedule: str = "fixed",
+                 rope: Rope | None = None):
         if schedule not in ("fixed", "sqrt"):
             raise ValueError(schedule)
-        self.cfg, self.k, self.schedule = cfg, top_k, schedule
+        self.cfg, self.k, self.schedule, self.rope = cfg, top_k, schedule, rope
         # summaries and workspace live on the GPU; K and V may be given in
         # pinned, device-mapped host memory
         if K is None:
@@ -548,7 +554,8 @@ class RadarLayer:
         self.K = K if K is not None else torch.zeros(shape, dtype=cfg.dtype, device=device)
         self.V = V if V is not None else torch.zeros(shape, dtype=cfg.dtype, device=device)
         self.omega = omega
-        self.t = t
+        self.t = self.pos = t
+        self.mass = None                           # rows' weights, from accumulate() on
         if schedule == "sqrt":
             c0 = schedule_sqrt(max(t, 1))[0]
             rows = cfg.capacity // c0              # the smallest c comes first
@@ -567,10 +574,43 @@ class RadarLayer:
         c, w = schedule_sqrt(t)
         return dataclasses.replace(self.cfg, seg_len=c, window=w)
 
+    def _reindex(self):
+        """The summaries of the cache as it is now."""
+        if self.schedule == "sqrt":
+            self.cfg = self._cfg_at(max(self.t, 1))
+            if self.cfg.summary_rows > self.summaries.shape[2]:    # t has shrunk
+                self.summaries = new_summaries(self.cfg, self.device)
+        if self.t > 0:
+            build_index(self.cfg, self.K, self.omega, self.t, self.summaries)
+
+    def prefill(self, k, v, q=None, q_out=None):
+        """A chunk of tokens behind the cache's rows: k, v [B][T][Hkv][d],
+        rotated with rope, and the index of all rows. With q [B][T][Hq][d] and
+        rope returns its rotation too (q itself without rope)."""
+        T = k.shape[1]
+        if self.rope is not None:
+            q = rotary_fill(self.cfg, self.rope, self.K, self.V, k, v, self.t, pos=self.pos,
+                            q=q, q_out=q_out)
+        else:
+            if self.t + T > self.cfg.capacity:
+                raise RadarError("prefill", 2)
+            self.K[:, :, self.t:self.t + T].copy_(k.transpose(1, 2))
+            self.V[:, :, self.t:self.t + T].copy_(v.transpose(1, 2))
+        self.t += T
+        self.pos += T
+        self._reindex()
+        return q
+
     def append(self, k_new, v_new):
+        if self.rope is not None:
+            k_new = rotary(self.rope, k_new, self.pos)
+        self._append(k_new, v_new)
+
+    def _append(self, k_new, v_new):
         append(self.cfg, self.K, self.V, k_new, v_new, self.omega, self.t,
                self.summaries)
         self.t += 1
+        self.pos += 1
         if self.schedule == "sqrt":
             c_old = self.cfg.seg_len
             self.cfg = self._cfg_at(self.t)
@@ -580,6 +620,11 @@ class RadarLayer:
                 self.restructures += 1
 
     def decode(self, q, out=None, selected=None, scores=None):
+        if self.rope is not None:                  # the last token's query
+            q = rotary(self.rope, q, self.pos - 1)
+        return self._decode(q, out, selected, scores)
+
+    def _decode(self, q, out, selected, scores):
         self._fit_workspace()
         return decode(self.cfg, q, self.K, self.V, self.omega, self.summaries,
                       self.t, self.k, out=out, selected=selected, scores=scores,
@@ -588,17 +633,37 @@ class RadarLayer:
     def step(self, q, k_new, v_new, out=None, selected=None, scores=None):
         """append(k_new, v_new) then decode(q), as one radar_append_decode
         call unless the sqrt schedule restructures at this token."""
+        if self.rope is not None:
+            q, k_new = rotary_qk(self.rope, q, k_new, self.pos)
         if self.schedule == "sqrt" and self._cfg_at(self.t + 1).seg_len != self.cfg.seg_len:
-            self.append(k_new, v_new)
-            return self.decode(q, out=out, selected=selected, scores=scores)
+            self._append(k_new, v_new)
+            return self._decode(q, out, selected, scores)
         if self.schedule == "sqrt":
             self.cfg = self._cfg_at(self.t + 1)
         self._fit_workspace()
         self.t += 1
+        self.pos += 1
         return append_decode(self.cfg, q, self.K, self.V, k_new, v_new,
                              self.omega, self.summaries, self.t, self.k,
                              out=out, selected=selected, scores=scores,
                              workspace=self.workspace)
+
+    def accumulate(self, q, out=None):
+        """Exact attention of the last token's query over the whole cache,
+        adding the weight of every row to `mass`."""
+        if self.mass is None:
+            self.mass = new_mass(self.cfg, self.device)
+        if self.rope is not None:
+            q = rotary(self.rope, q, self.pos - 1)
+        return attend_accumulate(self.cfg, q, self.K, self.V, self.mass, self.t, out=out)
+
+    def evict(self, heavy: int, recent: int, kept=None):
+        """Cuts the cache to its sinks, its last `recent` rows and the `heavy`
+        others with the most accumulated weight, and rebuilds the index."""
+        if self.mass is None:
+            raise RuntimeError("evict() needs the weights that accumulate() gathers")
+        self.t = evict(self.cfg, self.K, self.V, self.mass, self.t, heavy, recent, kept=kept)
+        self._reindex()
 
     def _fit_workspace(self):
         # the scratch size follows the window, which grows between
