@@ -12,7 +12,7 @@ import math
 import torch
 
 from . import (RADAR_BF16, RADAR_F32, Config, RadarError, _cache, _check, _Config,
-               _need, _ptr, _query, lib)
+               _need, _query, lib)
 
 _P = ctypes.c_void_p
 _DTYPES = {torch.float32: RADAR_F32, torch.bfloat16: RADAR_BF16}
@@ -52,6 +52,10 @@ def declare(L) -> None:
         getattr(L, fn).restype = ctypes.c_int
 
 
+def _ptr(x):
+    return None if x is None else x.data_ptr()
+
+
 def _one_device(x, *others):
     """Every device tensor of a call lies on x's GPU."""
     d = x.get_device()
@@ -62,11 +66,11 @@ def _one_device(x, *others):
 
 def _call(fn, x, *args):
     """lib().fn(*args, stream) with x's device current (a stream takes launches
-    from its own device only). The stream is asked for as torch's own generated
-    code asks: its handle alone, 2 us less than a stream object."""
+    from its own device only). Device and stream are asked for as torch's own
+    generated code asks: the stream's handle alone, 2 us less than an object."""
     f = getattr(lib(), fn)
     i = x.get_device()
-    if i == torch.cuda.current_device():
+    if i == torch._C._cuda_getDevice():
         st = f(*args, torch._C._cuda_getCurrentRawStream(i))
     else:
         with torch.cuda.device(i):
@@ -166,6 +170,10 @@ def _out_rows(x, out, name):
     """(out, struct) for the input x: a new dense tensor, or the given one."""
     if out is None:
         out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        H, d = x.shape[-2:]
+        if d * out.element_size() % 16 == 0:
+            T = x.shape[1] if x.dim() == 4 else 1
+            return out, _Rows(out.data_ptr(), T * H * d, H * d, d)
     else:
         if out.shape != x.shape or out.dtype != x.dtype or out.device != x.device:
             raise ValueError(f"{name} must have the input's shape, type and device")
