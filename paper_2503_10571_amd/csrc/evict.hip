@@ -48,7 +48,7 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 // A cache of up to kStep rows takes one workgroup and one kernel that holds its
 // masses in registers. Longer ones are cut into slices, a workgroup each, and the
 // three stages are kernels: one workgroup alone spends 2.2 us on a stage's 8192
-// rows (86 us for 65600 rows of 48 pairs, 42 in slices).
+// rows (86 us for 65600 rows of 64 pairs, 39 in slices; 200000 rows of 8: 26).
 constexpr int kSelThreads = 1024, kPer = 8;
 constexpr int kStep = kSelThreads * kPer;
 constexpr int kSlices = 32;                // at most
@@ -107,12 +107,12 @@ __device__ __forceinline__ void load_step(const Rows& r, int i0, float (&x)[kPer
 #pragma unroll
   for (int j = 0; j < kPer; ++j) x[j] = r.mass[min(step_row(i0, j), r.len - 1)];
 }
-// f(first row of the step, its masses) over the workgroup's rows; a step's loads
-// are in flight together, and the next step's beside this one's work
+// f(first row of the step, its masses) over the workgroup's rows; x: the first
+// step's, loaded ahead of whatever comes before; a step's loads are in flight
+// together, and the next step's beside this one's work
 template <typename F>
-__device__ __forceinline__ void each_step(const Rows& r, F&& f) {
-  float x[kPer], y[kPer];
-  load_step(r, r.begin, x);
+__device__ __forceinline__ void each_step(const Rows& r, float (&x)[kPer], F&& f) {
+  float y[kPer];
 #pragma unroll 1
   for (int i0 = r.begin; i0 < r.end; i0 += kStep) {
 #pragma unroll
@@ -133,15 +133,19 @@ __device__ __forceinline__ int bin_count(const int* hist, int bin) {
   const int4 v = *reinterpret_cast<const int4*>(hist + bin * kCopies);
   return (v.x + v.y) + (v.z + v.w);
 }
+__device__ __forceinline__ int2 two_bins(const int* hist, int bin) {
+  return make_int2(bin_count(hist, bin), bin_count(hist, bin + 1));
+}
 
 // The bin, from the top, that holds the need-th key: x its number, y the keys
-// above it, z its own; count(bin): its keys. Thread x takes bins 2 x and 2 x + 1
-// from the top. A call of the whole workgroup.
+// above it, z its own; count(bin): the keys of the (even) bin and of the next.
+// Thread x takes bins 2 x and 2 x + 1 from the top. A call of the whole workgroup.
 template <typename Count>
 __device__ __forceinline__ int3 pick_bin(int nb, int need, int* wsum, int* pick, Count&& count) {
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int b0 = nb - 1 - 2 * tid, b1 = b0 - 1;
-  const int c0 = b0 >= 0 ? count(b0) : 0, c1 = b1 >= 0 ? count(b1) : 0;
+  const int2 both = b1 >= 0 ? count(b1) : make_int2(0, 0);
+  const int c0 = both.y, c1 = both.x;
   const int incl = wave_incl_scan(c0 + c1, lane);
   if (lane == kWave - 1) wsum[wave] = incl;
   __syncthreads();
@@ -198,7 +202,7 @@ __device__ __forceinline__ Threshold find_key(uint32_t prefix, int need, int n, 
       if ((u & mask) == prefix) add_bin(hist, (int)(u >> shift) & (nb - 1));
     }
     __syncthreads();
-    const int3 b = pick_bin(nb, need, wsum, pick, [&](int x) { return bin_count(hist, x); });
+    const int3 b = pick_bin(nb, need, wsum, pick, [&](int x) { return two_bins(hist, x); });
     prefix |= (uint32_t)b.x << shift;
     mask |= (uint32_t)(nb - 1) << shift;
     need -= b.y;
@@ -304,7 +308,7 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_select(EvictArgs a) {
     for (int j = 0; j < kPer; ++j)
       if (step_row(0, j) >= r.lo && step_row(0, j) < r.hi) add_bin(hist, (int)(mass_key(x[j]) >> 21));
     __syncthreads();
-    const int3 b = pick_bin(kBins, a.heavy, wsum, pick, [&](int i) { return bin_count(hist, i); });
+    const int3 b = pick_bin(kBins, a.heavy, wsum, pick, [&](int i) { return two_bins(hist, i); });
     const uint32_t prefix = (uint32_t)b.x << 21;
     collect_step(r, prefix, 0, x, list, &n_list);
     __syncthreads();
@@ -327,8 +331,10 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_hist(EvictArgs a) {
   __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];
   Rows r;
   if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, true, &r)) return;
+  float x[kPer];
+  load_step(r, r.begin, x);
   clear_bins(hist);
-  each_step(r, [&](int i0, const float (&y)[kPer]) {
+  each_step(r, x, [&](int i0, const float (&y)[kPer]) {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const int i = step_row(i0, j);
@@ -347,14 +353,20 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_bin(EvictArgs a) {
   if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, false, &r)) return;
   const int slices = (r.len + a.slice_rows - 1) / a.slice_rows;
   const int* hist = a.hist + r.bh * a.slices * kBins;
+  float x[kPer];
+  load_step(r, r.begin, x);
   if (threadIdx.x == 0) { n_list = 0; n_above = 0; }
   // (with nothing to choose, a bin above all keys)
   int3 b = make_int3(kBins, 0, 0);
   if (a.heavy > 0)
     b = pick_bin(kBins, a.heavy, wsum, pick, [&](int i) {
-      int c = 0;
+      int2 c = make_int2(0, 0);
 #pragma unroll 8
-      for (int s = 0; s < slices; ++s) c += hist[s * kBins + i];
+      for (int s = 0; s < slices; ++s) {
+        const int2 v = *reinterpret_cast<const int2*>(hist + s * kBins + i);
+        c.x += v.x;
+        c.y += v.y;
+      }
       return c;
     });
   else
@@ -362,7 +374,7 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_bin(EvictArgs a) {
   const uint32_t prefix = (uint32_t)b.x << 21;
   const int64_t at = r.bh * a.slices + blockIdx.x;
   int above = 0;
-  each_step(r, [&](int i0, const float (&y)[kPer]) {
+  each_step(r, x, [&](int i0, const float (&y)[kPer]) {
     if (a.heavy > 0) {
       above += collect_step(r, prefix, i0, y, a.list + at * a.slice_rows, &n_list);
     } else {
@@ -395,6 +407,8 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_list(EvictArgs a) {
   if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, false, &r)) return;
   const int slices = (r.len + a.slice_rows - 1) / a.slice_rows;
   const int mine = blockIdx.x;
+  float x[kPer];
+  load_step(r, r.begin, x);
   const int2* counts = a.counts + r.bh * a.slices;
   const uint32_t* list = a.list + r.bh * a.slices * (int64_t)a.slice_rows;
   if (tid < kWave) {                       // slices <= 32: where each one's keys begin
@@ -407,18 +421,24 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_list(EvictArgs a) {
   __syncthreads();
   const int4 f = a.found[r.bh];
   const bool fits = f.z <= kStep;          // all slices' keys, in LDS
-  if (fits) {
-    for (int s = 0; s < slices; ++s)
-      for (int i = tid; i < ends[s + 1] - ends[s]; i += kSelThreads)
-        held[ends[s] + i] = list[(int64_t)s * a.slice_rows + i];
-    __syncthreads();
-  }
-  auto key = [&](int i) {                  // of all slices' keys, in order
-    if (fits) return held[i];
+  auto listed = [&](int i) {               // the i-th of all slices' keys, in order
     int s = 0;
-    while (i >= ends[s + 1]) ++s;
+#pragma unroll
+    for (int step = kSlices / 2; step > 0; step /= 2)
+      if (s + step < slices && ends[s + step] <= i) s += step;
     return list[(int64_t)s * a.slice_rows + i - ends[s]];
   };
+  if (fits) {
+    uint32_t u[kPer];                      // (loads in flight together)
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (j * kSelThreads + tid < f.z) u[j] = listed(j * kSelThreads + tid);
+#pragma unroll
+    for (int j = 0; j < kPer; ++j)
+      if (j * kSelThreads + tid < f.z) held[j * kSelThreads + tid] = u[j];
+    __syncthreads();
+  }
+  auto key = [&](int i) { return fits ? held[i] : listed(i); };
   Threshold th{0u, 0};
   if (a.heavy > 0) {
     th = find_key((uint32_t)f.x, f.y, f.z, key, hist, ranks, wsum, pick);
@@ -439,7 +459,7 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_list(EvictArgs a) {
   int* src = a.src + r.bh * a.n;
   float* moved = a.moved + r.bh * a.n;
   int32_t* kept = a.kept ? a.kept + r.bh * a.n_kept : nullptr;
-  each_step(r, [&](int i0, const float (&y)[kPer]) {
+  each_step(r, x, [&](int i0, const float (&y)[kPer]) {
     list_step(a, r, th, i0, y, n_gt, n_eq, wcount[parity], [&](int at, int i, float m) {
       src[at] = i;
       moved[at] = m;

@@ -16,7 +16,7 @@ constexpr int kMaxPartials = kSlots + 2 + kFiner * kSlots + 2;
 //   out = sum_i acc_i 2^(m_i - m) / sum_i l_i 2^(m_i - m),  m = max_i m_i
 template <typename T, int D>
 __device__ __forceinline__ void merge_head(const FlashArgs& a, T* __restrict__ out, int64_t bhq,
-                                           int lo, int n_tile_o) {
+                                           int lo, int64_t n_tile_o) {
   constexpr int TPP = D / 4, NG = 256 / TPP;
   __shared__ float f_lds[kMaxPartials];
   __shared__ float red[8];
@@ -79,7 +79,7 @@ __device__ __forceinline__ void merge_head(const FlashArgs& a, T* __restrict__ o
 }
 
 template <typename T, int D>
-__global__ __launch_bounds__(256) void k_merge(FlashArgs a, T* out, int n_tile_o) {
+__global__ __launch_bounds__(256) void k_merge(FlashArgs a, T* out, int64_t n_tile_o) {
   merge_head<T, D>(a, out, blockIdx.x, 0, n_tile_o);
 }
 
@@ -93,7 +93,7 @@ constexpr int kMassRows = 2048;
 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_settle(FlashArgs a, T* out, float* __restrict__ mass,
-                                                int n_tile_o, int chunks) {
+                                                int64_t n_tile_o, int chunks) {
   const int n_head = a.B * a.Hq;
   if ((int)blockIdx.x < n_head) {
     merge_head<T, D>(a, out, blockIdx.x, 1, n_tile_o);
@@ -283,7 +283,7 @@ radar_status radar_attend_prefix(const radar_config* cfg, const void* q, const v
     r = launch_status();
     if (r != RADAR_OK) return r;
   }
-  const int n_tile_o = p.tiles_o * flash_tile(esize(s), 1);
+  const int64_t n_tile_o = (int64_t)p.tiles_o * flash_tile(esize(s), 1);
   by_type(s, [&](auto tag, auto d) {
     typedef decltype(tag) T;
     launch(RADAR_K_COMBINE, k_merge<T, decltype(d)::value>, dim3((unsigned)(s.B * s.Hq)),
@@ -319,7 +319,7 @@ radar_status radar_attend_accumulate(const radar_config* cfg, const void* q, con
   launch_flash_any(s, a, 1, stream);
   r = launch_status();
   if (r != RADAR_OK) return r;
-  const int n_tile_o = p.tiles_o * flash_tile(esize(s), 1);
+  const int64_t n_tile_o = (int64_t)p.tiles_o * flash_tile(esize(s), 1);
   const int chunks = (int)ceil_div(t, kMassRows);
   const unsigned grid = (unsigned)(s.B * s.Hq) + (unsigned)(s.B * s.Hkv) * chunks;
   by_type(s, [&](auto tag, auto d) {
