@@ -26,6 +26,7 @@
 namespace radar_impl {
 namespace {
 
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef short s16x4_t __attribute__((ext_vector_type(4)));
 typedef short s16x8_t __attribute__((ext_vector_type(8)));
@@ -283,6 +284,13 @@ __device__ __forceinline__ void interleave() {
   __builtin_amdgcn_sched_group_barrier(kMfma, AHEAD, 0);
 }
 
+// x, of which the compiler computes nothing ahead of this place: what only a last,
+// partial tile needs would take registers through the whole loop
+__device__ __forceinline__ int here(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+
 // A workgroup of four waves. RW = 1: every wave takes the same query rows (up to
 // kRows) and tiles of its own, in its own part of the LDS, with no barrier in the
 // loop: what memory bounds. RW = 2 or 4: RW waves with 32 rows each, and 4 / RW
@@ -309,7 +317,7 @@ struct Flash {
   // Rows [r0, r1) of K and V (r1 > r0) for the query rows of this workgroup:
   // row_q(i) points to row i < rows; the partials go to acc_out [rows][D] and
   // ml_out [rows][2]. With LOG the logits of row i go to log_out + i * log_stride,
-  // by token; rows is a power of two then, at most 8.
+  // by token, a whole step's; rows is a power of two then, at most 8.
   template <bool LOG, typename RowQ>
   __device__ static __forceinline__ void block(const T* __restrict__ K, const T* __restrict__ V,
                                                int64_t r0, int64_t r1, int rows, float qscale,
@@ -341,31 +349,23 @@ struct Flash {
     for (int db = 0; db < NDB; ++db) acc[db] = Vec{};
     float m = -INFINITY, l = 0.f;
 
-    uint4 kr[NCH], vr[NCH];
+    u32x4_t kr[NCH], vr[NCH];
     constexpr int kRowBytes = D * (int)sizeof(T);
-    // rows behind the last are read as the last, and zeroed on the way to LDS
-    // (their weight is 0, which an infinity there would turn into NaN)
+    // rows behind the last are read as the last
     auto load = [&](int64_t at) {
       const unsigned char* kb = reinterpret_cast<const unsigned char*>(K + at * D);
       const unsigned char* vb = reinterpret_cast<const unsigned char*>(V + at * D);
       auto get = [](const unsigned char* p) {
-        return RW < 4 ? ld_stream(p) : *reinterpret_cast<const uint4*>(p);
+        const u32x4_t* v = reinterpret_cast<const u32x4_t*>(p);
+        return RW < 4 ? __builtin_nontemporal_load(v) : *v;
       };
-      if (at + NT <= r1) {                       // uniform
+      const int last = (int)min<int64_t>(NT, r1 - at) - 1, lt = here(ltid);
 #pragma unroll
-        for (int i = 0; i < NCH; ++i) kr[i] = get(kb + (i * NTHR + ltid) * 16);
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) vr[i] = get(vb + (i * NTHR + ltid) * 16);
-      } else {
-        const int last = (int)(r1 - at) - 1;
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-          const int x = i * NTHR + ltid, r = x / O::CPR;
-          const int off = min(r, last) * kRowBytes + x % O::CPR * 16;
-          kr[i] = get(kb + off);
-          vr[i] = get(vb + off);
-          if (r > last) vr[i] = make_uint4(0, 0, 0, 0);
-        }
+      for (int i = 0; i < NCH; ++i) {
+        const int x = i * NTHR + lt, r = x / O::CPR;
+        const uint32_t off = min(r, last) * kRowBytes + x % O::CPR * 16;
+        kr[i] = get(kb + off);
+        vr[i] = get(vb + off);
       }
     };
     auto sync = [] {
@@ -384,18 +384,32 @@ struct Flash {
     for (; at < r1; at += NTG) {
       unsigned char* kl = tile0 + buf * 2 * kBytes;
       unsigned char* vl = kl + kBytes;
+      const int len = (int)min<int64_t>(NT, r1 - at);
       if (kBuf == 1) sync();                     // the last tile is read
+      // V's rows behind the last become zeros here (their weight is 0, which an
+      // infinity would turn into NaN); done where they are loaded, it would wait
+      // for one load after the other
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
         const int x = i * NTHR + ltid, r = x / O::CPR, c = x % O::CPR;
-        *reinterpret_cast<uint4*>(kl + (r * O::CPR + O::k_place(r, c)) * 16) = kr[i];
-        *reinterpret_cast<uint4*>(vl + (r * O::CPR + O::v_place(r, c)) * 16) = vr[i];
+        *reinterpret_cast<u32x4_t*>(kl + (r * O::CPR + O::k_place(r, c)) * 16) = kr[i];
+        *reinterpret_cast<u32x4_t*>(vl + (r * O::CPR + O::v_place(r, c)) * 16) = vr[i];
+      }
+      if (len < NT) {                            // uniform
+        const int lt = here(ltid);
+#pragma unroll
+        for (int i = 0; i < NCH; ++i) {
+          const int x = i * NTHR + lt, r = x / O::CPR, c = x % O::CPR;
+          if (r >= len)
+            *reinterpret_cast<u32x4_t*>(vl + (r * O::CPR + O::v_place(r, c)) * 16) = u32x4_t{0, 0, 0, 0};
+        }
       }
       sync();
-      if (at + NTG < r1) load(at + NTG);
-      __builtin_amdgcn_sched_barrier(0);
+      if constexpr (!LOG) {
+        if (at + NTG < r1) load(at + NTG);
+        __builtin_amdgcn_sched_barrier(0);
+      }
       buf = kBuf == 2 ? buf ^ 1 : 0;
-      const int len = (int)min<int64_t>(NT, r1 - at);
       const int tok0 = RW == 1 ? 0 : tw * kSub * O::kTok;
       Vec s[kSub];
 #pragma unroll
@@ -404,19 +418,25 @@ struct Flash {
       if constexpr (LOG) {
         // Row r's logits are in the columns r, r + rows, ...: copy u writes the
         // u-th four of the lane's tokens, so that a step's logits of a row leave
-        // as whole lines by one store.
+        // as whole lines by one store. (Ahead of the next tile's loads: behind
+        // them, the wait for those would be one for the store too; 123 -> 118 us
+        // for eight ragged sequences of 32K rows, 102 with no store at all.)
         static_assert(kSub == 1, "one step per tile");
         const int u = col / rows;
-        float4 v = make_float4(s[0][0], s[0][1], s[0][2], s[0][3]);
+        float x[4] = {s[0][0], s[0][1], s[0][2], s[0][3]};
         int tok = O::token_of(0, lane);
 #pragma unroll
-        for (int i = 4; i < O::kVals; i += 4)
-          if (4 * u == i) {
-            v = make_float4(s[0][i], s[0][i + 1], s[0][i + 2], s[0][i + 3]);
-            tok = O::token_of(i, lane);
-          }
-        if (4 * u < O::kVals && tok < len)       // (rows come in fours, padded)
-          *reinterpret_cast<float4*>(log_out + row_in * log_stride + at + tok) = v;
+        for (int i = 4; i < O::kVals; i += 4) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) x[e] = 4 * u == i ? s[0][i + e] : x[e];
+          tok = 4 * u == i ? O::token_of(i, lane) : tok;
+        }
+        if (4 * u < O::kVals)
+          *reinterpret_cast<float4*>(log_out + row_in * log_stride + at + tok) =
+              make_float4(x[0], x[1], x[2], x[3]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (at + NTG < r1) load(at + NTG);
+        __builtin_amdgcn_sched_barrier(0);
       }
       if (len < NT) {                            // uniform
 #pragma unroll

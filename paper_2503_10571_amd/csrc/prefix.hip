@@ -200,7 +200,11 @@ FlashWs flash_ws(const Shape& s, int64_t splits, int64_t parts, int64_t logits) 
   return w;
 }
 
-int64_t padded(int64_t t) { return (t + 3) / 4 * 4; }
+// a row's logits are written by whole steps
+int64_t padded(const Shape& s, int64_t t) {
+  const int n = flash_tile(esize(s), 1);
+  return ceil_div(t, n) * n;
+}
 
 FlashArgs flash_args(const Shape& s, const Plan& p, const FlashWs& w, unsigned char* ws,
                      const void* q, const void* K, const void* V, int64_t t,
@@ -295,7 +299,7 @@ radar_status radar_attend_prefix(const radar_config* cfg, const void* q, const v
 size_t radar_attend_accumulate_workspace_bytes(const radar_config* cfg, int64_t t) {
   Shape s;
   if (check_cache(cfg, &s) != RADAR_OK || t < 1 || t > s.cap) return 0;
-  return flash_ws(s, 0, most_parts(s, t), padded(t)).total;
+  return flash_ws(s, 0, most_parts(s, t), padded(s, t)).total;
 }
 
 radar_status radar_attend_accumulate(const radar_config* cfg, const void* q, const void* K,
@@ -310,12 +314,12 @@ radar_status radar_attend_accumulate(const radar_config* cfg, const void* q, con
     return RADAR_EINVAL;
   if (t < 1 || t > s.cap) return RADAR_ECAPACITY;
   const Plan p = plan_flash(s, 0, t, lens != nullptr);
-  const FlashWs w = flash_ws(s, 0, most_parts(s, t), padded(t));
+  const FlashWs w = flash_ws(s, 0, most_parts(s, t), padded(s, t));
   if (bad16(workspace) || workspace_bytes < w.total) return RADAR_EWORKSPACE;
   unsigned char* ws = static_cast<unsigned char*>(workspace);
   FlashArgs a = flash_args(s, p, w, ws, q, K, V, t, lens);
   a.logits = reinterpret_cast<float*>(ws + w.logits);
-  a.tpad = padded(t);
+  a.tpad = padded(s, t);
   launch_flash_any(s, a, 1, stream);
   r = launch_status();
   if (r != RADAR_OK) return r;
