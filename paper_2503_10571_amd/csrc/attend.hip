@@ -10,6 +10,13 @@
 // four consecutive tokens at a time, which are its k-slots of P^T if the rows of
 // V are taken in the same order: no value of P crosses lanes.
 //
+// Up to 32 query rows per kv head (16 in fp32) memory bounds it: 6.4 TB/s of the
+// 7.2 that reads reach (32000 own rows of 8 x 8 pairs, head dim 128: 162 us). Above,
+// the matrix cores, the exponentials and the LDS reads of their operands share
+// the time: 0.76 PFLOP/s of the 1.28 that a large library product reaches (512
+// rows per kv head over a prefix of 100000: 275 us). In fp32 the matrix cores' 32-bit
+// rate.
+//
 // K and V come to LDS through registers, the next tile's loads in flight while
 // this one is computed. Rows are stored whole, their 16-byte chunks at places
 // XORed with the row, so that neither the operand reads nor the writes meet on
@@ -310,6 +317,10 @@ struct Flash {
   // two buffers save the barrier before a tile is written
   static constexpr int kBuf = RW > 1 && 4 * kBytes <= (64 << 10) ? 2 : 1;
   static constexpr int kTiles = (RW == 1 ? 4 : kBuf) * 2 * kBytes;
+  // rows that one workgroup reads pass the caches by: kept there, they make the next
+  // call over the same 200 MB up to 10% faster, but one over another layer's 14%
+  // slower (eight sequences of 6000 rows: 36.1 us against 36.7, and 43.3 against 37.9)
+  static constexpr bool kOnce = RW == 1 || (RW == 2 && sizeof(T) == 2);
   // the groups' accumulators are added in LDS
   static constexpr int kMerge = TW > 1 ? 4 * O::kRows * D * 4 : 0;
   static constexpr int kLds = kTiles > kMerge ? kTiles : kMerge;
@@ -357,7 +368,7 @@ struct Flash {
       const unsigned char* vb = reinterpret_cast<const unsigned char*>(V + at * D);
       auto get = [](const unsigned char* p) {
         const u32x4_t* v = reinterpret_cast<const u32x4_t*>(p);
-        return RW < 4 ? __builtin_nontemporal_load(v) : *v;
+        return kOnce ? __builtin_nontemporal_load(v) : *v;
       };
       const int last = (int)min<int64_t>(NT, r1 - at) - 1, lt = here(ltid);
 #pragma unroll

@@ -472,10 +472,10 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_list(EvictArgs a) {
 // ---------------------------------------------------------------------------
 // k_evict_move: row i of K and V takes row src[i] >= i, in place
 // ---------------------------------------------------------------------------
-// A workgroup moves a chunk of 128 KB of K or V (with 64 KB: 192 us below): it loads the chunk's rows into
-// registers, says so, and writes them once every chunk before it that reads rows
-// at or behind its own first place has said so too (the chunks behind it read
-// rows behind everything it writes). Chunks are handed out in ascending order,
+// A workgroup moves a chunk of 128 KB of K or V (with 64 KB: 192 us below): it
+// loads the chunk's rows into registers, says so, and writes them once every chunk
+// before it that reads rows at or behind its own first place has said so too (the
+// chunks behind it read rows behind everything it writes). Chunks are handed out in ascending order,
 // so the ones waited for have started, and none of them waits before it has
 // loaded: every wait ends. What is waited for is that reads are over, no data
 // goes from one workgroup to another, so nothing has to be flushed. Moving whole

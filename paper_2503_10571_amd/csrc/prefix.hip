@@ -12,7 +12,8 @@ constexpr int kSlots = 512, kFiner = 3;
 constexpr int kMaxPartials = kSlots + 2 + kFiner * kSlots + 2;
 
 // One head's output from its partials: 256 threads, D / 4 of them on four dims
-// each of one partial, 1024 / D partials at once.
+// each of one partial, 1024 / D partials at once. Few partials take a launch's 4 us,
+// the 34 MB of 128 sequences of 32 heads 10 us.
 //   out = sum_i acc_i 2^(m_i - m) / sum_i l_i 2^(m_i - m),  m = max_i m_i
 template <typename T, int D>
 __device__ __forceinline__ void merge_head(const FlashArgs& a, T* __restrict__ out, int64_t bhq,
@@ -87,7 +88,8 @@ __global__ __launch_bounds__(256) void k_merge(FlashArgs a, T* out, int64_t n_ti
 // the others add the weights of kMassRows rows of a (b, kv head):
 //   mass[i] += sum_g 2^(s_gi - m_g) / l_g.
 // The logits were written by the attention pass, G words a row beside the 2 d
-// elements that it read (6% at four heads of 128 in bf16); reading K again
+// elements that it read (at four heads of 128 in bf16 3% of the bytes, which cost
+// the pass 15% and this one, with the masses, 10 us for 22 MB); reading K again
 // instead would be half of the pass.
 constexpr int kMassRows = 2048;
 
@@ -141,18 +143,27 @@ __global__ __launch_bounds__(256) void k_settle(FlashArgs a, T* out, float* __re
 
 // How a call is cut: about as many workgroups as the chip holds at once (two per
 // CU), each with the same number of rows. Twice or three times as many only cost
-// starts and partials (64K rows for 32 sequences of four heads: 54 us, 68, 73).
-// Sequences of different lengths have their own rows cut three times finer, as
-// many of those workgroups find nothing (eight of 4K to 32K rows: 130 us, 123).
+// starts and partials (64K rows for 32 sequences of four heads, with the merge:
+// 68 us, 84, 97). Sequences of different lengths have their own rows cut three
+// times finer, as many of those workgroups find nothing (eight of up to 32K rows,
+// weights accumulated: 129 us, 117 this way). Counting the own rows for less than
+// the prefix's, as several of a ragged batch's are not there, gains nothing.
 struct Plan {
   int rw, mtiles, splits, tiles_p, parts, tiles_o;
 };
 
 int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
 int slots() { return std::min(kSlots, 2 * num_cu()); }
+// Row waves: the fewest that hold a kv head's query rows, at most four. In fp32,
+// where the matrix cores bound even few rows, two where that leaves fewer rows of
+// the last tile empty (132 rows over a prefix of 32768: 84 us against 104); in bf16
+// reading the prefix three times instead of two takes that back (134 us to 187 at
+// 100000, 31.7 to 29.1 at 8192).
 int row_waves(const Shape& s) {
   const int M = s.B * s.G;
-  return M <= flash_rows(esize(s), 1) ? 1 : M <= 64 ? 2 : 4;
+  if (M <= flash_rows(esize(s), 1)) return 1;
+  if (esize(s) == 4) return ceil_div(M, 64) * 64 < ceil_div(M, 128) * 128 ? 2 : 4;
+  return M <= 64 ? 2 : 4;
 }
 int row_tiles(const Shape& s) {
   return (int)ceil_div(s.B * s.G, flash_rows(esize(s), row_waves(s)));

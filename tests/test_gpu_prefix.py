@@ -98,6 +98,16 @@ def test_prefix(B, Hq, Hkv, d, P, t, lens, dtype):
 
 
 @DTYPES
+@pytest.mark.parametrize("B,G", [(16, 2), (33, 1), (17, 4), (64, 2), (33, 4), (193, 1), (40, 8)])
+def test_prefix_row_tiles(B, G, dtype):
+    """Query rows of a kv head around what one workgroup holds."""
+    q, Kp, Vp, K, V = _inputs(B, G, 1, 64, 1000, 20, None, dtype, seed=B)
+    cfg = _cfg(B, G, 1, 64, K.shape[2], dtype)
+    out = radar.attend_prefix(cfg, q, Kp, Vp, 1000, K, V, 20)
+    _check_prefix(out, q, Kp, Vp, 1000, K, V, 20, None, dtype, B, G, 1)
+
+
+@DTYPES
 @pytest.mark.parametrize("B", [1, 20])
 def test_prefix_sharp_and_flat(B, dtype):
     """Logits of some hundreds (one row takes all) and all equal."""
