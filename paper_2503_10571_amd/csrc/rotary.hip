@@ -58,6 +58,13 @@ __device__ __forceinline__ bool token_at(const RotArgs& a, int64_t i, TokenAt* o
   return true;
 }
 
+// the first of a workgroup's four tokens: a launch has fewer than 2^32 threads along
+// x, so more than kRotWgs workgroups go on along z
+constexpr int64_t kRotWgs = 1 << 23;
+__device__ __forceinline__ int64_t first_token() {
+  return ((int64_t)blockIdx.z * kRotWgs + blockIdx.x) * 4;
+}
+
 // (cos, sin) of a pair, times mscale; the sign of the direction in sin
 __device__ __forceinline__ float2 turn_of(const RotArgs& a, int pair, int64_t pos) {
   constexpr double kInv2Pi = 0.15915494309189533577;
@@ -135,7 +142,7 @@ __global__ __launch_bounds__(256) void k_rotary(RotArgs a, int lpr_log2) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   TokenAt at;
-  if (!token_at(a, (int64_t)blockIdx.x * 4 + wave, &at)) return;   // wave-uniform
+  if (!token_at(a, first_token() + wave, &at)) return;   // wave-uniform
   float2* turn = turn_lds[wave];
   for (int i = lane; i < a.pairs; i += kWave) turn[i] = turn_of(a, i, at.pos);
   // (the wave reads what it wrote)
@@ -219,7 +226,7 @@ __global__ __launch_bounds__(256) void k_rotary_any(RotArgs a, int inter) {
   const int lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   TokenAt at;
-  if (!token_at(a, (int64_t)blockIdx.x * 4 + wave, &at)) return;
+  if (!token_at(a, first_token() + wave, &at)) return;
   for (int i = lane; i < a.d / 2; i += kWave) {
     const bool turned = i < a.pairs;
     float2 t = make_float2(1.f, 0.f);
@@ -271,18 +278,19 @@ radar_status check_rope(const radar_rope* rope, int head_dim, radar_dtype dt) {
 template <typename T>
 void launch_rotary(const RotArgs& a, const radar_rope& rope, hipStream_t st) {
   constexpr int EPL = Elem<T>::kPer16;
-  const unsigned gx = (unsigned)ceil_div(a.n_tok, 4);
+  const int64_t wgs = ceil_div(a.n_tok, 4);
+  const unsigned gx = (unsigned)std::min(wgs, kRotWgs), gz = (unsigned)ceil_div(wgs, kRotWgs);
   // vectors where the pairs of a 16-byte chunk are whole chunks (or lie in it)
   const bool whole = rope.interleaved ? rope.rot_dim % EPL == 0 : a.pairs % EPL == 0;
   if (!whole) {
-    launch(RADAR_K_APPEND, k_rotary_any<T>, dim3(gx, (unsigned)ceil_div(a.heads, 8)), dim3(256), 0,
-           st, a, (int)rope.interleaved);
+    launch(RADAR_K_APPEND, k_rotary_any<T>, dim3(gx, (unsigned)ceil_div(a.heads, 8), gz),
+           dim3(256), 0, st, a, (int)rope.interleaved);
     return;
   }
   int lpr_log2 = 0;
   while ((1 << lpr_log2) < a.d / EPL / 2) ++lpr_log2;
   const int per_wave = (kWave >> lpr_log2) * kRotPasses;
-  const dim3 grid(gx, (unsigned)ceil_div(a.heads, per_wave));
+  const dim3 grid(gx, (unsigned)ceil_div(a.heads, per_wave), gz);
   if (rope.interleaved)
     launch(RADAR_K_APPEND, k_rotary<T, true>, grid, dim3(256), 0, st, a, lpr_log2);
   else

@@ -135,6 +135,21 @@ def test_lens_leave_the_rest():
         assert bool((out[b, n:] == 3.0).all())
 
 
+@pytest.mark.parametrize("rot", [16, 6])
+def test_more_tokens_than_a_launch_has_threads(rot):
+    """2^26 tokens of a wave each are 2^32 threads."""
+    T = (1 << 26) + 5
+    rope = _rope(rot)
+    x = torch.zeros(1, T, 1, 16, dtype=torch.bfloat16, device="cuda")
+    at = torch.tensor([0, 3, (1 << 25) - 1, 1 << 25, (1 << 25) + 4, T - 6, T - 5, T - 1])
+    x[:, at.cuda()] = torch.randn(1, len(at), 1, 16, device="cuda").bfloat16()
+    was = x[:, at.cuda()].clone()
+    radar.rotary(rope, x, 0, out=x)
+    _close(x[:, at.cuda()], *_ref(was, rope, at[None]))
+    x[:, at.cuda()] = 0
+    assert not bool(x.any())
+
+
 @pytest.mark.parametrize("inter", [False, True])
 def test_gradient(inter):
     """inverse is the transposed map: <R x, y> = <x, R' y>, and what differences
