@@ -23,10 +23,9 @@ struct EvictArgs {
   int row_bytes, chunks;
   // caches of more than kStep rows: slices of slice_rows
   int slices, slice_rows;
-  int* hist;               // [B Hkv][slices][kBins]
-  int4* found;             // [B Hkv]: leading bits, how many of them to take, all
-  int2* counts;            // [B Hkv][slices]: rows above the bin, rows in it
-  uint32_t* list;          // [B Hkv][slices][slice_rows]: the keys in the bin
+  int* hist;               // [B Hkv][3][slices][kBins]
+  int2* found;             // [B Hkv][2]: leading bits of the key, how many to take of them
+  int* above;              // [B Hkv][2][slices]: of the slices before, keys above the bin
   float* moved;            // [B Hkv][n]: the masses of the rows that stay
 };
 
@@ -41,18 +40,24 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 // which rows stay
 // ---------------------------------------------------------------------------
 // The heavy-th largest key of the rows between the sinks and the recent ones, by
-// a radix search: a histogram of the keys' upper 11 bits gives its bin; the
-// bin's keys are listed and ranked (up to kRank), or searched by two more
-// histograms (11 and 10 bits). Then one ascending pass lists the rows.
+// a radix search: a histogram of the keys' upper 11 bits gives its bin, two more of
+// the bin's keys (11 and 10 bits) give the key. Then one ascending pass lists the
+// rows.
 //
 // A cache of up to kStep rows takes one workgroup and one kernel that holds its
-// masses in registers. Longer ones are cut into slices, a workgroup each, and the
-// three stages are kernels: one workgroup alone spends 2.2 us on a stage's 8192
-// rows (86 us for 65600 rows of 64 pairs, 39 in slices; 200000 rows of 8: 26).
+// masses in registers, lists the first bin's keys and ranks them if they are few.
+// Longer ones are cut into slices, a workgroup each, with a kernel for each
+// histogram, which adds up the one before over the slices, and one for the rows:
+// one workgroup alone spends 2.2 us on a stage's 8192 rows (65600 rows of 64 pairs 86
+// us, in slices 41; 200000 rows of 8 pairs 31; 16.8 MB of masses are read four times).
+// Listing the first bin's keys instead of two more histograms is 2 us faster where
+// they are few, and where most masses share a bin 1.5 ms slower (a million rows).
 constexpr int kSelThreads = 1024, kPer = 8;
 constexpr int kStep = kSelThreads * kPer;
 constexpr int kSlices = 32;                // at most
 constexpr int64_t kMostRows = INT32_MAX - 2 * kStep;   // row numbers of a step fit 32 bits
+// bits of the key below each histogram's
+__host__ __device__ constexpr int key_shift(int level) { return level == 0 ? 21 : level == 1 ? 10 : 0; }
 constexpr int kBins = 2048, kRank = 256;   // (1024 keys: 25 us to rank, 6 by two histograms)
 constexpr int kSelWaves = kSelThreads / kWave;
 
@@ -326,136 +331,104 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_select(EvictArgs a) {
   for (int i = (int)a.n + tid; i < r.len; i += kSelThreads) r.mass[i] = 0.f;
 }
 
-// the stages over slices: the histogram of each,
+// What the histograms of one level, added up over the slices, say about the need-th
+// key: its bin, the keys above that, and of the slices before `mine` the keys above
+// the bin and in it. A call of the whole workgroup.
+struct Level {
+  int bin, above, gt, eq;
+};
+__device__ __forceinline__ Level read_level(const EvictArgs& a, const Rows& r, int level, int need, int mine,
+                                            int* wsum, int* pick, int* before) {
+  const int slices = (r.len + a.slice_rows - 1) / a.slice_rows;
+  const int* hist = a.hist + (r.bh * 3 + level) * a.slices * kBins;
+  const int nb = level < 2 ? kBins : kBins / 2;
+  int2 first = make_int2(0, 0);                // of the slices before
+  if (threadIdx.x < 2) before[threadIdx.x] = 0;
+  const int3 b = pick_bin(nb, need, wsum, pick, [&](int bin) {
+    int2 all = make_int2(0, 0);
+#pragma unroll 8
+    for (int s = 0; s < slices; ++s) {
+      const int2 v = *reinterpret_cast<const int2*>(hist + s * kBins + bin);
+      all.x += v.x;
+      all.y += v.y;
+      first.x += s < mine ? v.x : 0;
+      first.y += s < mine ? v.y : 0;
+    }
+    return all;
+  });
+  const int b0 = nb - 1 - 2 * (int)threadIdx.x, b1 = b0 - 1;   // as pick_bin has them
+  const int gt = wave_sum_i32((b0 > b.x ? first.y : 0) + (b1 > b.x ? first.x : 0));
+  if ((threadIdx.x & 63) == 0 && gt) atomicAdd(&before[0], gt);
+  if (b0 == b.x) before[1] = first.y;
+  if (b1 == b.x) before[1] = first.x;
+  __syncthreads();
+  return {b.x, b.y, before[0], before[1]};
+}
+
+// the histogram of each slice: of all its candidates, or of those in the bin that
+// the last one gives
+template <int LEVEL>
 __global__ __launch_bounds__(kSelThreads) void k_evict_hist(EvictArgs a) {
   __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];
+  __shared__ int wsum[kSelWaves], pick[3], before[2];
+  const int mine = blockIdx.x;
   Rows r;
-  if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, true, &r)) return;
+  if (!rows_of(a, blockIdx.y, mine, a.slice_rows, LEVEL == 0, &r) || a.heavy == 0) return;
   float x[kPer];
   load_step(r, r.begin, x);
   clear_bins(hist);
+  uint32_t prefix = 0;
+  if constexpr (LEVEL > 0) {
+    constexpr int kLast = LEVEL > 0 ? LEVEL - 1 : 0;
+    int need = a.heavy;
+    if constexpr (LEVEL == 2) {
+      const int2 f = a.found[r.bh * 2];
+      prefix = (uint32_t)f.x;
+      need = f.y;
+    }
+    const Level v = read_level(a, r, kLast, need, mine, wsum, pick, before);
+    prefix |= (uint32_t)v.bin << key_shift(kLast);
+    if (threadIdx.x == 0) {
+      a.above[(r.bh * 2 + kLast) * a.slices + mine] = v.gt;
+      if (mine == 0) a.found[r.bh * 2 + kLast] = make_int2((int)prefix, need - v.above);
+    }
+  }
+  constexpr int kShift = key_shift(LEVEL), kAbove = LEVEL > 0 ? key_shift(LEVEL - 1) : 31;
+  constexpr int nb = LEVEL < 2 ? kBins : kBins / 2;
   each_step(r, x, [&](int i0, const float (&y)[kPer]) {
 #pragma unroll
     for (int j = 0; j < kPer; ++j) {
       const int i = step_row(i0, j);
-      if (i >= r.lo && i < min(r.hi, r.end)) add_bin(hist, (int)(mass_key(y[j]) >> 21));
+      const uint32_t u = mass_key(y[j]);
+      if (i >= r.lo && i < min(r.hi, r.end) && (LEVEL == 0 || u >> kAbove == prefix >> kAbove))
+        add_bin(hist, (int)(u >> kShift) & (nb - 1));
     }
   });
   __syncthreads();
-  int* out = a.hist + (r.bh * a.slices + blockIdx.x) * kBins;
-  for (int i = threadIdx.x; i < kBins; i += kSelThreads) out[i] = bin_count(hist, i);
+  int* out = a.hist + ((r.bh * 3 + LEVEL) * a.slices + mine) * kBins;
+  for (int i = threadIdx.x; i < nb; i += kSelThreads) out[i] = bin_count(hist, i);
 }
 
-// the bin of the whole, and each slice's keys in it and rows above it,
-__global__ __launch_bounds__(kSelThreads) void k_evict_bin(EvictArgs a) {
-  __shared__ int wsum[kSelWaves], pick[3], n_list, n_above;
-  Rows r;
-  if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, false, &r)) return;
-  const int slices = (r.len + a.slice_rows - 1) / a.slice_rows;
-  const int* hist = a.hist + r.bh * a.slices * kBins;
-  float x[kPer];
-  load_step(r, r.begin, x);
-  if (threadIdx.x == 0) { n_list = 0; n_above = 0; }
-  // (with nothing to choose, a bin above all keys)
-  int3 b = make_int3(kBins, 0, 0);
-  if (a.heavy > 0)
-    b = pick_bin(kBins, a.heavy, wsum, pick, [&](int i) {
-      int2 c = make_int2(0, 0);
-#pragma unroll 8
-      for (int s = 0; s < slices; ++s) {
-        const int2 v = *reinterpret_cast<const int2*>(hist + s * kBins + i);
-        c.x += v.x;
-        c.y += v.y;
-      }
-      return c;
-    });
-  else
-    __syncthreads();
-  const uint32_t prefix = (uint32_t)b.x << 21;
-  const int64_t at = r.bh * a.slices + blockIdx.x;
-  int above = 0;
-  each_step(r, x, [&](int i0, const float (&y)[kPer]) {
-    if (a.heavy > 0) {
-      above += collect_step(r, prefix, i0, y, a.list + at * a.slice_rows, &n_list);
-    } else {
-#pragma unroll
-      for (int j = 0; j < kPer; ++j) {
-        const int i = step_row(i0, j);
-        above += i < r.len && (i < r.lo || i >= r.hi) ? 1 : 0;
-      }
-    }
-  });
-  above = wave_sum_i32(above);
-  if ((threadIdx.x & 63) == 0) atomicAdd(&n_above, above);
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    a.counts[at] = make_int2(n_above, n_list);
-    if (blockIdx.x == 0) a.found[r.bh] = make_int4((int)prefix, a.heavy - b.y, b.z, 0);
-  }
-}
-
-// and the rows that stay: every workgroup finds the threshold among all slices'
-// keys in the bin, and its place behind the slices before it
+// and the rows that stay, each slice's behind those of the slices before it
 __global__ __launch_bounds__(kSelThreads) void k_evict_list(EvictArgs a) {
-  __shared__ __attribute__((aligned(16))) int hist[kBins * kCopies];
-  __shared__ uint32_t ranks[kRank];
-  __shared__ uint32_t held[kStep];
-  __shared__ int wsum[kSelWaves], pick[3], ends[kSlices + 1], before[2];
+  __shared__ int wsum[kSelWaves], pick[3], before[2];
   __shared__ uint32_t wcount[2][kSelWaves];
-  const int tid = threadIdx.x, lane = tid & 63;
-  Rows r;
-  if (!rows_of(a, blockIdx.y, blockIdx.x, a.slice_rows, false, &r)) return;
-  const int slices = (r.len + a.slice_rows - 1) / a.slice_rows;
   const int mine = blockIdx.x;
+  Rows r;
+  if (!rows_of(a, blockIdx.y, mine, a.slice_rows, false, &r)) return;
   float x[kPer];
   load_step(r, r.begin, x);
-  const int2* counts = a.counts + r.bh * a.slices;
-  const uint32_t* list = a.list + r.bh * a.slices * (int64_t)a.slice_rows;
-  if (tid < kWave) {                       // slices <= 32: where each one's keys begin
-    const int2 c = lane < slices ? counts[lane] : make_int2(0, 0);
-    const int incl = wave_incl_scan(c.y, lane);
-    if (lane <= slices) ends[lane] = incl - c.y;
-    const int above = wave_sum_i32(lane < mine ? c.x : 0);
-    if (lane == 0) { before[0] = above; before[1] = 0; }
-  }
-  __syncthreads();
-  const int4 f = a.found[r.bh];
-  const bool fits = f.z <= kStep;          // all slices' keys, in LDS
-  auto listed = [&](int i) {               // the i-th of all slices' keys, in order
-    int s = 0;
-#pragma unroll
-    for (int step = kSlices / 2; step > 0; step /= 2)
-      if (s + step < slices && ends[s + step] <= i) s += step;
-    return list[(int64_t)s * a.slice_rows + i - ends[s]];
-  };
-  if (fits) {
-    uint32_t u[kPer];                      // (loads in flight together)
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (j * kSelThreads + tid < f.z) u[j] = listed(j * kSelThreads + tid);
-#pragma unroll
-    for (int j = 0; j < kPer; ++j)
-      if (j * kSelThreads + tid < f.z) held[j * kSelThreads + tid] = u[j];
-    __syncthreads();
-  }
-  auto key = [&](int i) { return fits ? held[i] : listed(i); };
   Threshold th{0u, 0};
+  int n_gt = min(r.begin, r.lo) + max(r.begin - r.hi, 0), n_eq = 0, parity = 0;   // fixed rows
   if (a.heavy > 0) {
-    th = find_key((uint32_t)f.x, f.y, f.z, key, hist, ranks, wsum, pick);
-    // the keys of the slices before this one that are above it or equal
-    int gt = 0, eq = 0;
-    for (int i = tid; i < ends[mine]; i += kSelThreads) {
-      const uint32_t u = key(i);
-      gt += u > th.key ? 1 : 0;
-      eq += u == th.key ? 1 : 0;
-    }
-    gt = wave_sum_i32(gt);
-    eq = wave_sum_i32(eq);
-    if (lane == 0 && gt) atomicAdd(&before[0], gt);
-    if (lane == 0 && eq) atomicAdd(&before[1], eq);
-    __syncthreads();
+    const int2 f = a.found[r.bh * 2 + 1];
+    const int* above = a.above + r.bh * 2 * a.slices + mine;
+    n_gt += above[0] + above[a.slices];
+    const Level v = read_level(a, r, 2, f.y, mine, wsum, pick, before);
+    th = {(uint32_t)f.x | (uint32_t)v.bin, f.y - v.above};
+    n_gt += v.gt;
+    n_eq = v.eq;
   }
-  int n_gt = before[0], n_eq = before[1], parity = 0;
   int* src = a.src + r.bh * a.n;
   float* moved = a.moved + r.bh * a.n;
   int32_t* kept = a.kept ? a.kept + r.bh * a.n_kept : nullptr;
@@ -542,7 +515,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a) {
 int64_t slice_rows(int64_t t) { return ceil_div(ceil_div(t, kSlices), kStep) * kStep; }
 
 struct EvictWs {
-  size_t turn, arrived, src, hist, found, counts, list, moved, total;
+  size_t turn, arrived, src, hist, found, above, moved, total;
   int64_t chunks;
 };
 EvictWs evict_ws(const Shape& s, int64_t t, int64_t n) {
@@ -554,15 +527,13 @@ EvictWs evict_ws(const Shape& s, int64_t t, int64_t n) {
   w.arrived = w.turn + align256(pairs * 8);
   w.src = w.arrived + align256(pairs * 2 * w.chunks * 4);
   w.total = w.src + align256(pairs * n * 4);
-  w.hist = w.found = w.counts = w.list = w.moved = w.total;
+  w.hist = w.found = w.above = w.moved = w.total;
   if (t > kStep) {
     // (bounds for every smaller t too, whose slices may be more)
-    const size_t steps = (size_t)ceil_div(t, kStep);
-    const size_t slices = std::min<size_t>(kSlices, steps);
-    w.found = w.hist + align256(pairs * slices * kBins * 4);
-    w.counts = w.found + align256(pairs * sizeof(int4));
-    w.list = w.counts + align256(pairs * slices * sizeof(int2));
-    w.moved = w.list + align256(pairs * (steps + steps / kSlices + 2) * kStep * 4);
+    const size_t slices = (size_t)std::min<int64_t>(kSlices, ceil_div(t, kStep));
+    w.found = w.hist + align256(pairs * 3 * slices * kBins * 4);
+    w.above = w.found + align256(pairs * 2 * sizeof(int2));
+    w.moved = w.above + align256(pairs * 2 * slices * 4);
     w.total = w.moved + align256(pairs * n * 4);
   }
   return w;
@@ -613,9 +584,8 @@ radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass,
   a.src = reinterpret_cast<int*>(ws + w.src);
   a.chunks = (int)w.chunks;
   a.hist = reinterpret_cast<int*>(ws + w.hist);
-  a.found = reinterpret_cast<int4*>(ws + w.found);
-  a.counts = reinterpret_cast<int2*>(ws + w.counts);
-  a.list = reinterpret_cast<uint32_t*>(ws + w.list);
+  a.found = reinterpret_cast<int2*>(ws + w.found);
+  a.above = reinterpret_cast<int*>(ws + w.above);
   a.moved = reinterpret_cast<float*>(ws + w.moved);
   a.slice_rows = (int)slice_rows(t);
   a.slices = t > 0 ? (int)ceil_div(t, a.slice_rows) : 1;
@@ -628,8 +598,11 @@ radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass,
   const bool sliced = t > kStep && a.n < t;
   if (sliced) {
     const dim3 grid((unsigned)a.slices, pairs), block(kSelThreads);
-    launch(RADAR_K_TOPK, k_evict_hist, grid, block, 0, stream, a);
-    launch(RADAR_K_TOPK, k_evict_bin, grid, block, 0, stream, a);
+    launch(RADAR_K_TOPK, k_evict_hist<0>, grid, block, 0, stream, a);
+    if (a.heavy > 0) {
+      launch(RADAR_K_TOPK, k_evict_hist<1>, grid, block, 0, stream, a);
+      launch(RADAR_K_TOPK, k_evict_hist<2>, grid, block, 0, stream, a);
+    }
     launch(RADAR_K_TOPK, k_evict_list, grid, block, 0, stream, a);
   } else {
     launch(RADAR_K_TOPK, k_evict_select, dim3(pairs), dim3(kSelThreads), 0, stream, a);
