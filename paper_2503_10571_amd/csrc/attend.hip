@@ -328,14 +328,18 @@ struct Flash {
   // Rows [r0, r1) of K and V (r1 > r0) for the query rows of this workgroup:
   // row_q(i) points to row i < rows; the partials go to acc_out [rows][D] and
   // ml_out [rows][2]. With LOG the logits of row i go to log_out + i * log_stride,
-  // by token, a whole step's; rows is a power of two then, at most 8.
-  template <bool LOG, typename RowQ>
+  // by token, a whole step's; rows is a power of two then, at most 8. With BOTH (RW =
+  // 1) the rows [0, own_r1) of own_K and own_V follow, and the outputs, not the
+  // partials, go to out [rows][D].
+  template <bool LOG, bool BOTH, typename RowQ>
   __device__ static __forceinline__ void block(const T* __restrict__ K, const T* __restrict__ V,
                                                int64_t r0, int64_t r1, int rows, float qscale,
                                                RowQ&& row_q, float* acc_out, float* ml_out,
                                                float* log_out, int64_t log_stride,
                                                unsigned char* lds, float (*wm)[O::kRows * RW],
-                                               float (*wl)[O::kRows * RW]) {
+                                               float (*wl)[O::kRows * RW], const T* __restrict__ own_K = nullptr,
+                                               const T* __restrict__ own_V = nullptr, int64_t own_r1 = 0,
+                                               T* out = nullptr) {
     // The running maximum may lag the true one by this much (in log2): p grows
     // to 256 at most, which no sum minds, and the accumulators are rescaled once
     // or twice a run instead of whenever one of a wave's rows meets a new
@@ -363,14 +367,20 @@ struct Flash {
     u32x4_t kr[NCH], vr[NCH];
     constexpr int kRowBytes = D * (int)sizeof(T);
     // rows behind the last are read as the last
+    // (BOTH: the own rows begin behind the prefix's last step)
+    const int64_t own_at = BOTH ? (r1 + NTG - 1) / NTG * NTG : 0;
+    const int64_t end = BOTH ? own_at + own_r1 : r1;
+    auto rows_left = [&](int64_t at) { return (BOTH && at < own_at ? r1 : end) - at; };
     auto load = [&](int64_t at) {
-      const unsigned char* kb = reinterpret_cast<const unsigned char*>(K + at * D);
-      const unsigned char* vb = reinterpret_cast<const unsigned char*>(V + at * D);
+      const bool own = BOTH && at >= own_at;
+      const int64_t row = own ? at - own_at : at;
+      const unsigned char* kb = reinterpret_cast<const unsigned char*>((own ? own_K : K) + row * D);
+      const unsigned char* vb = reinterpret_cast<const unsigned char*>((own ? own_V : V) + row * D);
       auto get = [](const unsigned char* p) {
         const u32x4_t* v = reinterpret_cast<const u32x4_t*>(p);
         return kOnce ? __builtin_nontemporal_load(v) : *v;
       };
-      const int last = (int)min<int64_t>(NT, r1 - at) - 1, lt = here(ltid);
+      const int last = (int)min<int64_t>(NT, rows_left(at)) - 1, lt = here(ltid);
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
         const int x = i * NTHR + lt, r = x / O::CPR;
@@ -388,14 +398,21 @@ struct Flash {
         __syncthreads();
       }
     };
+    // this wave's next tile: of the prefix one may lie behind its rows
+    auto there_is = [&](int64_t& at) {
+      if (BOTH && at < own_at && at >= r1) at += NTG;
+      return at < end;
+    };
     int64_t at = r0 + (RW == 1 ? wave * NT : 0);
-    if (at < r1) load(at);
+    if (there_is(at)) load(at);
     int buf = 0;
 #pragma unroll 1
-    for (; at < r1; at += NTG) {
+    for (int64_t next; at < end; at = next) {
+      next = at + NTG;
+      const bool more = there_is(next);
       unsigned char* kl = tile0 + buf * 2 * kBytes;
       unsigned char* vl = kl + kBytes;
-      const int len = (int)min<int64_t>(NT, r1 - at);
+      const int len = (int)min<int64_t>(NT, rows_left(at));
       if (kBuf == 1) sync();                     // the last tile is read
       // V's rows behind the last become zeros here (their weight is 0, which an
       // infinity would turn into NaN); done where they are loaded, it would wait
@@ -417,7 +434,7 @@ struct Flash {
       }
       sync();
       if constexpr (!LOG) {
-        if (at + NTG < r1) load(at + NTG);
+        if (more) load(next);
         __builtin_amdgcn_sched_barrier(0);
       }
       buf = kBuf == 2 ? buf ^ 1 : 0;
@@ -446,7 +463,7 @@ struct Flash {
           *reinterpret_cast<float4*>(log_out + row_in * log_stride + at + tok) =
               make_float4(x[0], x[1], x[2], x[3]);
         __builtin_amdgcn_sched_barrier(0);
-        if (at + NTG < r1) load(at + NTG);
+        if (more) load(next);
         __builtin_amdgcn_sched_barrier(0);
       }
       if (len < NT) {                            // uniform
@@ -536,8 +553,15 @@ struct Flash {
           a.z = fmaf(v.z, f, a.z); a.w = fmaf(v.w, f, a.w);
           L = fmaf(wl[w][r], f, L);
         }
-        *reinterpret_cast<float4*>(acc_out + (int64_t)r * D + 4 * c) = a;
-        if (c == 0) *reinterpret_cast<float2*>(ml_out + 2 * r) = make_float2(M, L);
+        if constexpr (BOTH) {
+          T* o = out + (int64_t)r * D + 4 * c;
+          const float x[4] = {a.x, a.y, a.z, a.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[e] = from_f32<T>(end > 0 ? x[e] / L : 0.f);
+        } else {
+          *reinterpret_cast<float4*>(acc_out + (int64_t)r * D + 4 * c) = a;
+          if (c == 0) *reinterpret_cast<float2*>(ml_out + 2 * r) = make_float2(M, L);
+        }
       }
     }
   }
@@ -566,7 +590,7 @@ __global__ __launch_bounds__(256, 2) void k_flash(FlashArgs a) {
       const int64_t r1 = min(a.P, r0 + (int64_t)a.tiles_p * F::NTG);
       const int row0 = mt * F::O::kRows * RW;
       const int64_t at = (int64_t)unit * a.M + row0;
-      F::template block<false>(
+      F::template block<false, false>(
           static_cast<const T*>(a.Kp) + hk * a.Pcap * D, static_cast<const T*>(a.Vp) + hk * a.Pcap * D,
           r0, r1, min(a.M - row0, F::O::kRows * RW), a.qscale,
           [&](int r) {
@@ -590,7 +614,7 @@ __global__ __launch_bounds__(256, 2) void k_flash(FlashArgs a) {
   if (r0 >= len) return;
   const int64_t r1 = min(len, r0 + (int64_t)a.tiles_o * F1::NTG);
   const int64_t at = (bh * a.parts + part) * a.G;
-  F1::template block<LOG>(
+  F1::template block<LOG, false>(
       static_cast<const T*>(a.K) + bh * a.cap * D, static_cast<const T*>(a.V) + bh * a.cap * D, r0, r1,
       a.G, a.qscale,
       [&](int r) { return static_cast<const T*>(a.q) + (b * a.Hq + hk * a.G + r) * D; },
@@ -598,10 +622,34 @@ __global__ __launch_bounds__(256, 2) void k_flash(FlashArgs a) {
       reinterpret_cast<RowArray>(wm), reinterpret_cast<RowArray>(wl));
 }
 
+// A short prefix and few own rows: a workgroup of each (b, kv head) attends both
+// and leaves the outputs.
+template <typename T, int D>
+__global__ __launch_bounds__(256, 2) void k_short(FlashArgs a) {
+  using F = Flash<T, D, 1>;
+  using RowArray = float (*)[F::O::kRows];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[F::kLds];
+  __shared__ float wm[4 * 32], wl[4 * 32];
+  const int64_t bh = blockIdx.x, b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int64_t len = own_len(a, b, 0), row0 = b * a.Hq + hk * a.G;
+  T* out = static_cast<T*>(a.out) + row0 * D;
+  if (len < 0) {
+    for (int x = threadIdx.x; x < a.G * D; x += 256) out[x] = from_f32<T>(__uint_as_float(0x7fc00000u));
+    return;
+  }
+  F::template block<false, true>(
+      static_cast<const T*>(a.Kp) + hk * a.Pcap * D, static_cast<const T*>(a.Vp) + hk * a.Pcap * D, 0, a.P,
+      a.G, a.qscale, [&](int r) { return static_cast<const T*>(a.q) + (row0 + r) * D; }, nullptr, nullptr,
+      nullptr, 0, lds, reinterpret_cast<RowArray>(wm), reinterpret_cast<RowArray>(wl),
+      static_cast<const T*>(a.K) + bh * a.cap * D, static_cast<const T*>(a.V) + bh * a.cap * D, len, out);
+}
+
 template <typename T, int D>
 void launch_flash(const FlashArgs& a, int rw, hipStream_t st) {
   const unsigned n = (unsigned)(ceil_div(a.Hkv * a.splits, 8) * 8 * a.mtiles + a.B * a.Hkv * a.parts);
-  if (a.logits)
+  if (rw == 0)
+    launch(RADAR_K_ATTEND, k_short<T, D>, dim3((unsigned)(a.B * a.Hkv)), dim3(256), 0, st, a);
+  else if (a.logits)
     launch(RADAR_K_ATTEND, k_flash<T, D, 1, true>, dim3(n), dim3(256), 0, st, a);
   else if (rw == 1)
     launch(RADAR_K_ATTEND, k_flash<T, D, 1, false>, dim3(n), dim3(256), 0, st, a);

@@ -15,6 +15,7 @@ namespace radar_impl {
 //    pair against tiles_o tiles.
 struct FlashArgs {
   const void* q;             // [B][Hq][d]
+  void* out;                 // the same (k_short)
   int B, Hq, Hkv, G;
   float qscale;              // log2(e) / sqrt(d)
   // prefix
@@ -44,7 +45,7 @@ __device__ __forceinline__ int64_t own_len(const FlashArgs& a, int64_t b, int lo
   return n >= lo && n <= a.t ? n : -1;
 }
 
-// attend.hip: rw in {1, 2, 4}; the prefix's blocks, then the own rows'
+// attend.hip: rw in {1, 2, 4}: the prefix's blocks, then the own rows'; 0: k_short
 void launch_flash_bf16_64(const FlashArgs& a, int rw, hipStream_t st);
 void launch_flash_bf16_128(const FlashArgs& a, int rw, hipStream_t st);
 void launch_flash_f32_64(const FlashArgs& a, int rw, hipStream_t st);

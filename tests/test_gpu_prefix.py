@@ -98,6 +98,30 @@ def test_prefix(B, Hq, Hkv, d, P, t, lens, dtype):
 
 
 @DTYPES
+@pytest.mark.parametrize("P,t", [(1, 0), (0, 1), (64, 64), (65, 128), (512, 128), (512, 129),
+                                 (640, 0), (0, 640), (0, 641), (33, 500), (192, 1), (129, 63)])
+def test_prefix_few_rows(P, t, dtype):
+    """Sizes on both sides of where one workgroup attends all of a pair's rows, with
+    lengths down to none and two that are none."""
+    lens = [t, t // 2, 0, 1 if t else 0, t + 1, -1]
+    q, Kp, Vp, K, V = _inputs(6, 4, 2, 128, P, t, [min(max(n, 0), t) for n in lens], dtype, seed=P)
+    cfg = _cfg(6, 4, 2, 128, K.shape[2], dtype)
+    out = Guarded(q.shape, q.dtype)
+    radar.attend_prefix(cfg, q, Kp, Vp, P, K, V, t, out=out.t, lens=torch.tensor(lens, device="cuda"))
+    torch.cuda.synchronize()
+    assert out.intact() and bool(out.t[4:].isnan().all())
+    _check_prefix(out.t[:4], q[:4], Kp, Vp, P, K[:4], V[:4], t, lens[:4], dtype, 4, 4, 2)
+
+
+@DTYPES
+def test_prefix_more_pairs_than_slots(dtype):
+    q, Kp, Vp, K, V = _inputs(520, 2, 1, 64, 40, 9, None, dtype)
+    cfg = _cfg(520, 2, 1, 64, K.shape[2], dtype)
+    out = radar.attend_prefix(cfg, q, Kp, Vp, 40, K, V, 9)
+    _check_prefix(out, q, Kp, Vp, 40, K, V, 9, None, dtype, 520, 2, 1)
+
+
+@DTYPES
 @pytest.mark.parametrize("B,G", [(16, 2), (33, 1), (17, 4), (64, 2), (33, 4), (193, 1), (40, 8)])
 def test_prefix_row_tiles(B, G, dtype):
     """Query rows of a kv head around what one workgroup holds."""
