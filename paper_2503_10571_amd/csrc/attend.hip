@@ -317,10 +317,6 @@ struct Flash {
   // two buffers save the barrier before a tile is written
   static constexpr int kBuf = RW > 1 && 4 * kBytes <= (64 << 10) ? 2 : 1;
   static constexpr int kTiles = (RW == 1 ? 4 : kBuf) * 2 * kBytes;
-  // rows that one workgroup reads pass the caches by: kept there, they make the next
-  // call over the same 200 MB up to 10% faster, but one over another layer's 14%
-  // slower (eight sequences of 6000 rows: 36.1 us against 36.7, and 43.3 against 37.9)
-  static constexpr bool kOnce = RW == 1 || (RW == 2 && sizeof(T) == 2);
   // the groups' accumulators are added in LDS
   static constexpr int kMerge = TW > 1 ? 4 * O::kRows * D * 4 : 0;
   static constexpr int kLds = kTiles > kMerge ? kTiles : kMerge;
@@ -330,8 +326,11 @@ struct Flash {
   // ml_out [rows][2]. With LOG the logits of row i go to log_out + i * log_stride,
   // by token, a whole step's; rows is a power of two then, at most 8. With BOTH (RW =
   // 1) the rows [0, own_r1) of own_K and own_V follow, and the outputs, not the
-  // partials, go to out [rows][D].
-  template <bool LOG, bool BOTH, typename RowQ>
+  // partials, go to out [rows][D]. ONCE: no other workgroup reads these rows, and they
+  // pass the caches by: kept there, they make the next call over the same 200 MB up to
+  // 10% faster, but one over another layer's 14% slower (eight sequences of 6000 rows:
+  // 36.1 us against 36.7, and 43.3 against 37.9).
+  template <bool LOG, bool BOTH, bool ONCE, typename RowQ>
   __device__ static __forceinline__ void block(const T* __restrict__ K, const T* __restrict__ V,
                                                int64_t r0, int64_t r1, int rows, float qscale,
                                                RowQ&& row_q, float* acc_out, float* ml_out,
@@ -378,7 +377,7 @@ struct Flash {
       const unsigned char* vb = reinterpret_cast<const unsigned char*>((own ? own_V : V) + row * D);
       auto get = [](const unsigned char* p) {
         const u32x4_t* v = reinterpret_cast<const u32x4_t*>(p);
-        return kOnce ? __builtin_nontemporal_load(v) : *v;
+        return ONCE ? __builtin_nontemporal_load(v) : *v;
       };
       const int last = (int)min<int64_t>(NT, rows_left(at)) - 1, lt = here(ltid);
 #pragma unroll
@@ -417,9 +416,11 @@ struct Flash {
       // V's rows behind the last become zeros here (their weight is 0, which an
       // infinity would turn into NaN); done where they are loaded, it would wait
       // for one load after the other
+      // (its registers are all in use: kept through the loop, the places spill; 5%)
+      const int pt = RW == 2 && sizeof(T) == 4 ? here(ltid) : ltid;
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
-        const int x = i * NTHR + ltid, r = x / O::CPR, c = x % O::CPR;
+        const int x = i * NTHR + pt, r = x / O::CPR, c = x % O::CPR;
         *reinterpret_cast<u32x4_t*>(kl + (r * O::CPR + O::k_place(r, c)) * 16) = kr[i];
         *reinterpret_cast<u32x4_t*>(vl + (r * O::CPR + O::v_place(r, c)) * 16) = vr[i];
       }
@@ -590,15 +591,26 @@ __global__ __launch_bounds__(256, 2) void k_flash(FlashArgs a) {
       const int64_t r1 = min(a.P, r0 + (int64_t)a.tiles_p * F::NTG);
       const int row0 = mt * F::O::kRows * RW;
       const int64_t at = (int64_t)unit * a.M + row0;
-      F::template block<false, false>(
-          static_cast<const T*>(a.Kp) + hk * a.Pcap * D, static_cast<const T*>(a.Vp) + hk * a.Pcap * D,
-          r0, r1, min(a.M - row0, F::O::kRows * RW), a.qscale,
-          [&](int r) {
-            const int x = row0 + r;              // b G + g
-            return static_cast<const T*>(a.q) + ((int64_t)(x / a.G) * a.Hq + hk * a.G + x % a.G) * D;
-          },
-          a.pacc + at * D, a.pml + at * 2, nullptr, 0, lds, reinterpret_cast<RowArray>(wm),
-          reinterpret_cast<RowArray>(wl));
+      auto block = [&](auto once) {
+        F::template block<false, false, decltype(once)::value>(
+            static_cast<const T*>(a.Kp) + hk * a.Pcap * D, static_cast<const T*>(a.Vp) + hk * a.Pcap * D,
+            r0, r1, min(a.M - row0, F::O::kRows * RW), a.qscale,
+            [&](int r) {
+              const int x = row0 + r;              // b G + g
+              return static_cast<const T*>(a.q) + ((int64_t)(x / a.G) * a.Hq + hk * a.G + x % a.G) * D;
+            },
+            a.pacc + at * D, a.pml + at * 2, nullptr, 0, lds, reinterpret_cast<RowArray>(wm),
+            reinterpret_cast<RowArray>(wl));
+      };
+      // (once: where there is one row tile)
+      if constexpr (sizeof(T) == 2) {
+        block(std::bool_constant<(RW < 4)>{});
+      } else if constexpr (RW == 1) {
+        if (a.mtiles == 1) block(std::true_type{});
+        else block(std::false_type{});
+      } else {
+        block(std::false_type{});
+      }
       return;
     }
     i -= n_prefix;
@@ -614,7 +626,7 @@ __global__ __launch_bounds__(256, 2) void k_flash(FlashArgs a) {
   if (r0 >= len) return;
   const int64_t r1 = min(len, r0 + (int64_t)a.tiles_o * F1::NTG);
   const int64_t at = (bh * a.parts + part) * a.G;
-  F1::template block<LOG, false>(
+  F1::template block<LOG, false, true>(
       static_cast<const T*>(a.K) + bh * a.cap * D, static_cast<const T*>(a.V) + bh * a.cap * D, r0, r1,
       a.G, a.qscale,
       [&](int r) { return static_cast<const T*>(a.q) + (b * a.Hq + hk * a.G + r) * D; },
@@ -637,7 +649,7 @@ __global__ __launch_bounds__(256, 2) void k_short(FlashArgs a) {
     for (int x = threadIdx.x; x < a.G * D; x += 256) out[x] = from_f32<T>(__uint_as_float(0x7fc00000u));
     return;
   }
-  F::template block<false, true>(
+  F::template block<false, true, true>(
       static_cast<const T*>(a.Kp) + hk * a.Pcap * D, static_cast<const T*>(a.Vp) + hk * a.Pcap * D, 0, a.P,
       a.G, a.qscale, [&](int r) { return static_cast<const T*>(a.q) + (row0 + r) * D; }, nullptr, nullptr,
       nullptr, 0, lds, reinterpret_cast<RowArray>(wm), reinterpret_cast<RowArray>(wl),

@@ -154,14 +154,15 @@ struct Plan {
 
 int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
 int slots() { return std::min(kSlots, 2 * num_cu()); }
-// Row waves: the fewest that hold a kv head's query rows, at most four. In fp32,
-// where the matrix cores bound even few rows, two where that leaves fewer rows of
-// the last tile empty (132 rows over a prefix of 32768: 84 us against 104); in bf16
-// reading the prefix three times instead of two takes that back (134 us to 187 at
-// 100000, 31.7 to 29.1 at 8192).
+// Row waves: the fewest that hold a kv head's query rows, at most four. In fp32, where
+// the matrix cores bound even few rows, those that leave fewer rows of the last tile
+// empty: tiles of 16 up to 48 rows (32 rows over a prefix of 30000: 64.7 us against
+// 90.7; 48: 90.2, 95.6; 80: 164, 162), then of 64 or 128 (132 over 32768: 82, 104). In
+// bf16 reading the prefix three times instead of two takes that back (132 rows: 134 us
+// to 187 at 100000, 31.7 to 29.1 at 8192).
 int row_waves(const Shape& s) {
   const int M = s.B * s.G;
-  if (M <= flash_rows(esize(s), 1)) return 1;
+  if (M <= (esize(s) == 4 ? 48 : flash_rows(esize(s), 1))) return 1;
   if (esize(s) == 4) return ceil_div(M, 64) * 64 < ceil_div(M, 128) * 128 ? 2 : 4;
   return M <= 64 ? 2 : 4;
 }

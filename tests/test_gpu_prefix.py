@@ -122,7 +122,7 @@ def test_prefix_more_pairs_than_slots(dtype):
 
 
 @DTYPES
-@pytest.mark.parametrize("B,G", [(16, 2), (33, 1), (17, 4), (64, 2), (33, 4), (193, 1), (40, 8)])
+@pytest.mark.parametrize("B,G", [(16, 2), (33, 1), (60, 1), (17, 4), (64, 2), (33, 4), (193, 1), (40, 8)])
 def test_prefix_row_tiles(B, G, dtype):
     """Query rows of a kv head around what one workgroup holds."""
     q, Kp, Vp, K, V = _inputs(B, G, 1, 64, 1000, 20, None, dtype, seed=B)
