@@ -13,8 +13,8 @@
 // Up to 32 query rows per kv head (16 in fp32) memory bounds it: 6.4 TB/s of the
 // 7.2 that reads reach (32000 own rows of 8 x 8 pairs, head dim 128: 162 us). Above,
 // the matrix cores, the exponentials and the LDS reads of their operands share
-// the time: 0.76 PFLOP/s of the 1.28 that a large library product reaches (512
-// rows per kv head over a prefix of 100000: 275 us). In fp32 the matrix cores' 32-bit
+// the time: 0.8 PFLOP/s of the 1.28 that a large library product reaches (512
+// rows per kv head over a prefix of 100000: 265 us, at a clock of 1.8 GHz). In fp32 the matrix cores' 32-bit
 // rate.
 //
 // K and V come to LDS through registers, the next tile's loads in flight while
@@ -467,6 +467,9 @@ struct Flash {
         if (more) load(next);
         __builtin_amdgcn_sched_barrier(0);
       }
+      // Of a SIMD's two waves the one with products to issue goes first: the other's
+      // vector instructions fit between them (512 rows over 32768: 105.6 us, 100.5).
+      if constexpr (RW == 4) __builtin_amdgcn_s_setprio(0);
       if (len < NT) {                            // uniform
 #pragma unroll
         for (int sub = 0; sub < kSub; ++sub)
@@ -500,6 +503,7 @@ struct Flash {
           sum += s[sub][i];
         }
       l += sum;
+      if constexpr (RW == 4) __builtin_amdgcn_s_setprio(2);
       O::pv(vl, tok0, s, twice, low, acc, lane);
     }
     l = O::row_total(l);
