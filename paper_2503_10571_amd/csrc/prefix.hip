@@ -148,6 +148,11 @@ __global__ __launch_bounds__(256) void k_settle(FlashArgs a, T* out, float* __re
 // times finer, as many of those workgroups find nothing (eight of up to 32K rows,
 // weights accumulated: 129 us, 117 this way). Counting the own rows for less than
 // the prefix's, as several of a ragged batch's are not there, gains nothing.
+// Blocks of the prefix of up to kShortBlock rows are twice as long: 32 sequences of four
+// heads over 8192 rows, 128 a block: 24.0 us, 19.9 this way; 16411, 257: 29.5, 26.4;
+// 32768, 512: 38.4, 37.1; but 65536, 1024: 60.7, 62.5.
+constexpr int kShortBlock = 512;
+
 struct Plan {
   int rw, mtiles, splits, tiles_p, parts, tiles_o;
 };
@@ -177,7 +182,9 @@ Plan plan_flash(const Shape& s, int64_t P, int64_t t, bool ragged) {
   p.mtiles = row_tiles(s);
   const int ntp = flash_tile(esize(s), p.rw), nto = flash_tile(esize(s), 1);
   const int64_t rows = ceil_div((int64_t)s.Hkv * p.mtiles * P + pairs * t, slots());
-  p.tiles_p = (int)std::max<int64_t>(1, ceil_div(rows, ntp));
+  // a block of a short prefix spends as long on its partials (64 KB at 128 query rows)
+  // as on its rows: one a CU then, twice as long
+  p.tiles_p = (int)std::max<int64_t>(1, ceil_div(rows <= kShortBlock ? 2 * rows : rows, ntp));
   p.tiles_o = (int)std::max<int64_t>(1, ceil_div(rows, (ragged ? kFiner : 1) * nto));
   // as many of each, of the same length (40 sequences of 2000 rows over 4096: 75 us, 70)
   const int64_t tp = ceil_div(P, ntp), to = ceil_div(t, nto);
