@@ -84,8 +84,8 @@ radar_status radar_rotary_fill(const radar_config* cfg, const radar_rope* rope,
  * Kp, Vp [n_kv_heads][prefix_capacity][head_dim], which all sequences share,
  * and rows [0, t) (with lens, nullable device int64 [batch], [0, lens[b]),
  * t their bound) of the sequence's own K and V: exact softmax attention with
- * the scale 1/sqrt(head_dim). The prefix's rows are read once for the whole
- * batch. 0 <= prefix_len <= prefix_capacity < 2^31, 0 <= t <= capacity; Kp and
+ * the scale 1/sqrt(head_dim). A read of a prefix row serves up to 128 query
+ * rows of its kv head (batch * n_q_heads / n_kv_heads). 0 <= prefix_len <= prefix_capacity < 2^31, 0 <= t <= capacity; Kp and
  * Vp may be NULL with prefix_len = 0, K and V with t = 0. A query that attends
  * no row gets a zero output; lens[b] outside [0, t] makes that sequence's
  * outputs NaN. */

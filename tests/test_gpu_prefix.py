@@ -295,6 +295,27 @@ def test_graph_replays(op):
         assert torch.equal(out, want) and torch.equal(mass, wmass), rep
 
 
+def test_graph_of_a_short_call():
+    """One launch, its output and workspace the graph's own."""
+    q, Kp, Vp, K, V = _inputs(3, 8, 2, 128, 200, 80, None, "bf16")
+    cfg = _cfg(3, 8, 2, 128, K.shape[2], "bf16")
+    lens = torch.tensor([80, 0, 33], device="cuda")
+    radar.attend_prefix(cfg, q, Kp, Vp, 200, K, V, 80, lens=lens)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = radar.attend_prefix(cfg, q, Kp, Vp, 200, K, V, 80, lens=lens)
+    for rep in range(3):
+        q.mul_(0.9)
+        lens.copy_(torch.tensor([79 - rep, 1, 0], device="cuda"))
+        want = radar.attend_prefix(cfg, q, Kp, Vp, 200, K, V, 80, lens=lens)
+        out.zero_()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.randn(1 << 20, device="cuda").sum().item()
+        assert torch.equal(out, want), rep
+
+
 def test_two_streams():
     """Two calls at once on streams of their own, each with its workspace."""
     ins = [_inputs(4, 8, 2, 128, 3000, 300, None, "bf16", seed=i) for i in range(2)]
