@@ -27,4 +27,13 @@ inline radar_status check_cache(const radar_config* cfg, Shape* s) {
   return RADAR_OK;
 }
 
+// 16 bytes to dst, past the caches or not
+template <bool PAST>
+__device__ __forceinline__ void put16(unsigned char* dst, const uint4& v) {
+  if constexpr (PAST)
+    __builtin_nontemporal_store(u32x4_t{v.x, v.y, v.z, v.w}, reinterpret_cast<u32x4_t*>(dst));
+  else
+    *reinterpret_cast<uint4*>(dst) = v;
+}
+
 }  // namespace radar_impl

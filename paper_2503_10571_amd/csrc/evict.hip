@@ -445,21 +445,21 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_list(EvictArgs a) {
 // ---------------------------------------------------------------------------
 // k_evict_move: row i of K and V takes row src[i] >= i, in place
 // ---------------------------------------------------------------------------
-// A workgroup moves a chunk of 128 KB of K or V (with 64 KB: 192 us below): it
+// A workgroup moves a chunk of 128 KB of K or V (with 64 KB 5% slower): it
 // loads the chunk's rows into registers, says so, and writes them once every chunk
 // before it that reads rows at or behind its own first place has said so too (the
-// chunks behind it read rows behind everything it writes). Chunks are handed out in ascending order,
-// so the ones waited for have started, and none of them waits before it has
-// loaded: every wait ends. What is waited for is that reads are over, no data
+// chunks behind it read rows behind everything it writes). Chunks are handed out in
+// ascending order, so the ones waited for have started, and none of them waits before
+// it has loaded: every wait ends. What is waited for is that reads are over, no data
 // goes from one workgroup to another, so nothing has to be flushed. Moving whole
 // columns of a pair in order needs no waits but leaves few workgroups (315 us
-// for 48 pairs of 16K rows of 256 bytes, 182 this way: 4.4 TB/s).
+// for 48 pairs of 16K rows of 256 bytes, 173 this way: 4.7 TB/s).
 // The new lengths, which may replace the old ones, are written here, when nobody
 // reads those any more.
-constexpr int kMoveThreads = 512, kMoveVecs = 16;
+constexpr int kMoveThreads = 1024, kMoveVecs = 8;
 constexpr int kMoveBytes = kMoveThreads * kMoveVecs * 16;
 
-template <int CPR>                         // 16-byte chunks of a row
+template <int CPR, bool PAST>              // 16-byte chunks of a row; stores past the caches
 __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a) {
   constexpr int R = kMoveThreads * kMoveVecs / CPR;        // rows per chunk
   __shared__ int turn;
@@ -507,7 +507,7 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a) {
 #pragma unroll
   for (int j = 0; j < kMoveVecs; ++j) {
     const int i = i0 + (j * kMoveThreads + tid) / CPR;
-    if (i < n) *reinterpret_cast<uint4*>(base + (int64_t)i * a.row_bytes) = x[j];
+    if (i < n) put16<PAST>(base + (int64_t)i * a.row_bytes, x[j]);
   }
 }
 
@@ -612,8 +612,14 @@ radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass,
   const bool moves = a.n > 0 && a.n < t;
   if (r != RADAR_OK || !(moves || sliced || new_lens)) return r;
   const dim3 grid(std::max(1u, moves ? (unsigned)w.chunks : 1u), pairs, sliced ? 3 : moves ? 2 : 1);
+  // The stores pass the caches by where the rows that stay are three times what those
+  // hold: 64 pairs of 21004 rows of 256 bytes 265 us, 238 this way; 16384, a third of
+  // them uncut: 183, 173; but 9004: 105, 110.
+  const bool past = 4 * a.n * pairs * a.row_bytes > ((int64_t)768 << 20);
   auto go = [&](auto cpr) {
-    launch(RADAR_K_APPEND, k_evict_move<decltype(cpr)::value>, grid, dim3(kMoveThreads), 0, stream, a);
+    constexpr int kCpr = decltype(cpr)::value;
+    if (past) launch(RADAR_K_APPEND, k_evict_move<kCpr, true>, grid, dim3(kMoveThreads), 0, stream, a);
+    else launch(RADAR_K_APPEND, k_evict_move<kCpr, false>, grid, dim3(kMoveThreads), 0, stream, a);
   };
   if (a.row_bytes == 128) go(std::integral_constant<int, 8>{});
   else if (a.row_bytes == 256) go(std::integral_constant<int, 16>{});

@@ -162,6 +162,25 @@ def test_long_cache():
     _run(1, 1, 64, 131077, 4, 60000, 5000, None, "bf16")
 
 
+@pytest.mark.parametrize("d,dtype,t", [(64, "bf16", 27000), (128, "bf16", 13500), (128, "f32", 6900)])
+def test_large_move(d, dtype, t):
+    """More than 768 MB moved, whose stores pass the caches by."""
+    cfg = radar.Config(8, 8, 8, d, 64, 16, 16, t, DT[dtype], 4)
+    K, V = (torch.randn(8, 8, t, d, device="cuda").to(DT[dtype]) for _ in range(2))
+    mass = torch.rand(8, 8, t, device="cuda")
+    K0, V0, mass0 = K.clone(), V.clone(), mass.clone()
+    heavy = t - 600
+    kept = torch.empty(8, 8, heavy + 104, dtype=torch.int32, device="cuda")
+    n = radar.evict(cfg, K, V, mass, t, heavy, 100, kept=kept)
+    assert n == heavy + 104 and 4 * n * 64 * d * K.element_size() > 768 << 20
+    at = kept.long()
+    assert bool((at[..., 1:] > at[..., :-1]).all())
+    rows = at[..., None].expand(-1, -1, -1, d)
+    assert torch.equal(K[:, :, :n], K0.gather(2, rows)) and torch.equal(V[:, :, :n], V0.gather(2, rows))
+    assert torch.equal(K[:, :, n:], K0[:, :, n:]) and torch.equal(V[:, :, n:], V0[:, :, n:])
+    assert torch.equal(mass[..., :n], mass0.gather(2, at)) and not bool(mass[..., n:].any())
+
+
 def test_new_lengths_in_place_of_the_old():
     _run(5, 4, 64, 400, 2, 100, 30, [400, 133, 132, 7, 401], "bf16", alias=True)
 
