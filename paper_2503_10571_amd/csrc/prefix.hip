@@ -157,13 +157,17 @@ __global__ __launch_bounds__(256) void k_settle(FlashArgs a, T* out, float* __re
 // How a call is cut: about as many workgroups as the chip holds at once (two per
 // CU), each with the same number of rows. Twice or three times as many only cost
 // starts and partials (64K rows for 32 sequences of four heads, with the merge:
-// 68 us, 84, 97). Sequences of different lengths have their own rows cut three
-// times finer, as many of those workgroups find nothing (eight of up to 32K rows,
-// weights accumulated: 129 us, 117 this way). Counting the own rows for less than
-// the prefix's, as several of a ragged batch's are not there, gains nothing.
-// Blocks of the prefix of up to kShortBlock rows are twice as long: 32 sequences of four
-// heads over 8192 rows, 128 a block: 24.0 us, 19.9 this way; 16411, 257: 29.5, 26.4;
-// 32768, 512: 38.4, 37.1; but 65536, 1024: 60.7, 62.5.
+// 68 us, 84, 97). Blocks of the prefix of up to kShortBlock rows are twice as long: 32
+// sequences over 8192 rows, 128 a block: 24.0 us, 19.9 this way; 16411, 257: 29.5,
+// 26.4; 32768, 512: 38.4, 37.1; but 65536, 1024: 60.7, 62.5.
+//
+// A sequence's own rows take as many blocks as come nearest to that length (32
+// sequences of 700 rows over 16411, blocks of 607: one each 36, two 38 us). Of sequences
+// of different lengths many blocks find nothing: they are cut three times finer (eight
+// of up to 32K rows, weights accumulated: 129 us, 117 this way), but not to single tiles
+// (eight of up to 2000: 20.1 us, 17.6 with two); beside a short prefix, whose blocks take
+// longer, as long as those (eight of up to 3000 over 8192: 25.9 us, 23.2). Counting the
+// own rows for less than the prefix's, as several are not there, gains nothing.
 constexpr int kShortBlock = 512;
 
 struct Plan {
@@ -197,10 +201,17 @@ Plan plan_flash(const Shape& s, int64_t P, int64_t t, bool ragged) {
   const int64_t rows = ceil_div((int64_t)s.Hkv * p.mtiles * P + pairs * t, slots());
   // a block of a short prefix spends as long on its partials (64 KB at 128 query rows)
   // as on its rows: one a CU then, twice as long
-  p.tiles_p = (int)std::max<int64_t>(1, ceil_div(rows <= kShortBlock ? 2 * rows : rows, ntp));
-  p.tiles_o = (int)std::max<int64_t>(1, ceil_div(rows, (ragged ? kFiner : 1) * nto));
-  // as many of each, of the same length (40 sequences of 2000 rows over 4096: 75 us, 70)
+  const int64_t rows_p = rows <= kShortBlock ? 2 * rows : rows;
   const int64_t tp = ceil_div(P, ntp), to = ceil_div(t, nto);
+  p.tiles_p = (int)std::max<int64_t>(1, ceil_div(rows_p, ntp));
+  if (!ragged)
+    p.tiles_o = (int)ceil_div(to, std::max<int64_t>(1, (t + rows / 2) / std::max<int64_t>(1, rows)));
+  else if (P > 0 && rows <= kShortBlock)
+    p.tiles_o = (int)ceil_div(rows_p, nto);
+  else
+    p.tiles_o = (int)std::max(std::min<int64_t>(2, ceil_div(rows, nto)), ceil_div(rows, kFiner * nto));
+  p.tiles_o = std::max(1, p.tiles_o);
+  // as many of each, of the same length (40 sequences of 2000 rows over 4096: 75 us, 70)
   p.splits = (int)ceil_div(tp, p.tiles_p);
   p.parts = (int)ceil_div(to, p.tiles_o);
   if (p.splits > 0) p.tiles_p = (int)ceil_div(tp, p.splits);
