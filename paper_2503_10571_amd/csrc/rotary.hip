@@ -6,8 +6,8 @@
 // Every element is read once and written once, so memory bounds it. The angle
 // is taken as turns, p f_i / 2 pi, in 64 bits (at position 2^20 a 32-bit angle
 // is off by 0.06 rad), its fraction then in 32 bits. Measured: 16384 tokens of 32 + 8
-// + 8 heads of 128 in bf16 into the cache 62 us, 6.5 TB/s, as a copy of that size;
-// one token of 32 + 8 heads 5 us, which the launch and the binding's 11 us hide.
+// + 8 heads of 128 in bf16 into the cache 71 us, 5.7 TB/s, where a copy reaches 6.4;
+// one token of 32 + 8 heads 4 us, which the launch and the binding's 11 us hide.
 #include "cache_impl.h"
 
 namespace radar_impl {
@@ -131,13 +131,12 @@ __device__ __forceinline__ uint4 pack16<bf16_t>(const float* f) {
 // a row computing its own would take eight); then every lane moves two 16-byte
 // chunks of a row: for half pairs a chunk of first dims and the matching chunk
 // of second dims, otherwise chunks u and u + U of the row's 2 U. kRotPasses heads
-// (of 1, 2 and 4 the best for large calls: 1 GB 202, 175, 178 us)
+// (of 1, 2 and 4 the best for large calls: 1 GB 208, 178, 182 us)
 // per lane are loaded before any is written, which also makes an output that
 // is its own input safe: nobody else reads a lane's chunks.
 constexpr int kRotPasses = 2;
 
-// STREAM: what passes the caches by, the stores (1) or both sides (2); see streamed()
-template <typename T, bool INTER, int STREAM>
+template <typename T, bool INTER, bool PAST>
 __global__ __launch_bounds__(256) void k_rotary(RotArgs a, int lpr_log2) {
   constexpr int EPL = Elem<T>::kPer16;
   __shared__ float2 turn_lds[4][kRopeMaxDim / 2];
@@ -177,8 +176,8 @@ __global__ __launch_bounds__(256) void k_rotary(RotArgs a, int lpr_log2) {
     const int h = h0 + p * hpp;
     on[p] = h < a.heads && side_rows(a, at, h, &src, &dst[p], &rot[p]);
     if (on[p]) {
-      x[p] = STREAM == 2 ? ld_stream(src + ca * 16) : *reinterpret_cast<const uint4*>(src + ca * 16);
-      y[p] = STREAM == 2 ? ld_stream(src + cb * 16) : *reinterpret_cast<const uint4*>(src + cb * 16);
+      x[p] = PAST ? ld_stream(src + ca * 16) : *reinterpret_cast<const uint4*>(src + ca * 16);
+      y[p] = PAST ? ld_stream(src + cb * 16) : *reinterpret_cast<const uint4*>(src + cb * 16);
     }
   }
 #pragma unroll
@@ -216,8 +215,8 @@ __global__ __launch_bounds__(256) void k_rotary(RotArgs a, int lpr_log2) {
         y[p] = pack16<T>(g);
       }
     }
-    put16<(STREAM > 0)>(dst[p] + ca * 16, x[p]);
-    put16<(STREAM > 0)>(dst[p] + cb * 16, y[p]);
+    put16<PAST>(dst[p] + ca * 16, x[p]);
+    put16<PAST>(dst[p] + cb * 16, y[p]);
   }
 }
 
@@ -277,13 +276,15 @@ radar_status check_rope(const radar_rope* rope, int head_dim, radar_dtype dt) {
   return RADAR_OK;
 }
 
-// What passes the caches by (256 MB), for the bytes that a call moves: nothing where
-// both sides fit, whose stores then cost nothing now and the next kernel's reads little
-// (84 MB: 15.9 us, 23.4 with the stores past them); the stores where the input alone
-// may lie there (400 MB: 82, 62; both sides 73); else both (1 GB: 192, 186, 175).
-int streamed(const RotArgs& a, int esz) {
-  const int64_t bytes = 2 * a.n_tok * a.heads * a.d * esz;
-  return bytes <= (256 << 20) ? 0 : bytes <= ((int64_t)512 << 20) ? 1 : 2;
+// Loads and stores pass the caches (256 MB) by where a call moves more than they hold
+// (three calls of 400 MB in turn: 82.7 us, 72.2; of 1 GB: 194, 178) and its stores are
+// of whole 128-byte lines (383 MB of rows with 16 rotated dims of 64 in fp32, whose lines
+// two stores share: 83 us, 127). Where both sides fit, the stores cost nothing now and
+// the next kernel's reads little (84 MB: 17.2 us, 27.3).
+bool past_caches(const RotArgs& a, bool inter, int epl) {
+  const int U = a.d / epl / 2, hp = a.pairs / epl;
+  return 2 * a.n_tok * a.heads * a.d * (16 / epl) > (256 << 20) && U % 8 == 0 &&
+         (inter || hp % 8 == 0);
 }
 
 template <typename T>
@@ -302,18 +303,14 @@ void launch_rotary(const RotArgs& a, const radar_rope& rope, hipStream_t st) {
   while ((1 << lpr_log2) < a.d / EPL / 2) ++lpr_log2;
   const int per_wave = (kWave >> lpr_log2) * kRotPasses;
   const dim3 grid(gx, (unsigned)ceil_div(a.heads, per_wave), gz);
-  auto go = [&](auto inter, auto stream) {
-    launch(RADAR_K_APPEND, k_rotary<T, decltype(inter)::value, decltype(stream)::value>, grid, dim3(256),
-           0, st, a, lpr_log2);
+  const bool past = past_caches(a, rope.interleaved, EPL);
+  auto go = [&](auto inter) {
+    constexpr bool kInter = decltype(inter)::value;
+    if (past) launch(RADAR_K_APPEND, k_rotary<T, kInter, true>, grid, dim3(256), 0, st, a, lpr_log2);
+    else launch(RADAR_K_APPEND, k_rotary<T, kInter, false>, grid, dim3(256), 0, st, a, lpr_log2);
   };
-  auto by_size = [&](auto inter) {
-    const int s = streamed(a, (int)sizeof(T));
-    if (s == 0) go(inter, std::integral_constant<int, 0>{});
-    else if (s == 1) go(inter, std::integral_constant<int, 1>{});
-    else go(inter, std::integral_constant<int, 2>{});
-  };
-  if (rope.interleaved) by_size(std::true_type{});
-  else by_size(std::false_type{});
+  if (rope.interleaved) go(std::true_type{});
+  else go(std::false_type{});
 }
 
 radar_status run_rotary(RotArgs& a, const radar_rope& rope, radar_dtype dt, hipStream_t st) {

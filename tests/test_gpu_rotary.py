@@ -153,9 +153,8 @@ def test_more_tokens_than_a_launch_has_threads(rot):
 @pytest.mark.parametrize("inter", [False, True])
 @pytest.mark.parametrize("dtype,T", [("bf16", 20000), ("bf16", 40000), ("f32", 10000), ("f32", 20000)])
 def test_large_calls(dtype, T, inter):
-    """Calls of 328 and 655 MB, whose stores (and loads) pass the caches by: the bits
-    of small ones."""
-    rope = _rope(96, inter)
+    """Calls of 328 and 655 MB, which pass the caches by: the bits of small ones."""
+    rope = _rope(96 if inter else 128, inter)
     x = torch.randn(1, T, 32, 128, device="cuda").to(DT[dtype])
     out = radar.rotary(rope, x, 7)
     for t in range(0, T, 5000):
