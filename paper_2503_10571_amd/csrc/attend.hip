@@ -365,8 +365,8 @@ struct Flash {
 
     u32x4_t kr[NCH], vr[NCH];
     constexpr int kRowBytes = D * (int)sizeof(T);
-    // rows behind the last are read as the last
-    // (BOTH: the own rows begin behind the prefix's last step)
+    // rows behind the last are read as the last; with BOTH the own rows begin behind
+    // the prefix's last step
     const int64_t own_at = BOTH ? (r1 + NTG - 1) / NTG * NTG : 0;
     const int64_t end = BOTH ? own_at + own_r1 : r1;
     auto rows_left = [&](int64_t at) { return (BOTH && at < own_at ? r1 : end) - at; };
@@ -413,10 +413,8 @@ struct Flash {
       unsigned char* vl = kl + kBytes;
       const int len = (int)min<int64_t>(NT, rows_left(at));
       if (kBuf == 1) sync();                     // the last tile is read
-      // V's rows behind the last become zeros here (their weight is 0, which an
-      // infinity would turn into NaN); done where they are loaded, it would wait
-      // for one load after the other
-      // (its registers are all in use: kept through the loop, the places spill; 5%)
+      // (32 rows in fp32 leave no register free: kept through the loop, the places in
+      // LDS spill; 5%)
       const int pt = RW == 2 && sizeof(T) == 4 ? here(ltid) : ltid;
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
@@ -424,6 +422,9 @@ struct Flash {
         *reinterpret_cast<u32x4_t*>(kl + (r * O::CPR + O::k_place(r, c)) * 16) = kr[i];
         *reinterpret_cast<u32x4_t*>(vl + (r * O::CPR + O::v_place(r, c)) * 16) = vr[i];
       }
+      // V's rows behind the last become zeros here (their weight is 0, which an
+      // infinity would turn into NaN); done where they are loaded, it would wait
+      // for one load after the other
       if (len < NT) {                            // uniform
         const int lt = here(ltid);
 #pragma unroll
