@@ -159,7 +159,8 @@ __global__ __launch_bounds__(256) void k_settle(FlashArgs a, T* out, float* __re
 // starts and partials (64K rows for 32 sequences of four heads, with the merge:
 // 68 us, 84, 97). Blocks of the prefix of up to kShortBlock rows are twice as long: 32
 // sequences over 8192 rows, 128 a block: 24.0 us, 19.9 this way; 16411, 257: 29.5,
-// 26.4; 32768, 512: 38.4, 37.1; but 65536, 1024: 60.7, 62.5.
+// 26.4; 32768, 512: 38.4, 37.1; but 65536, 1024: 60.7, 62.5; and where the matrix cores
+// bound (fp32, more than 16 query rows) 64 rows over 4000: 28.3, 30.8; 30000: 98.8, 102.4.
 //
 // A sequence's own rows take as many blocks as come nearest to that length (32
 // sequences of 700 rows over 16411, blocks of 607: one each 36, two 38 us). Of sequences
@@ -201,12 +202,14 @@ Plan plan_flash(const Shape& s, int64_t P, int64_t t, bool ragged) {
   const int64_t rows = ceil_div((int64_t)s.Hkv * p.mtiles * P + pairs * t, slots());
   // a block of a short prefix spends as long on its partials (64 KB at 128 query rows)
   // as on its rows: one a CU then, twice as long
-  const int64_t rows_p = rows <= kShortBlock ? 2 * rows : rows;
+  const bool matrix_bound = esize(s) == 4 && s.B * s.G > flash_rows(4, 1);
+  const bool is_long = rows > kShortBlock || matrix_bound;
+  const int64_t rows_p = is_long ? rows : 2 * rows;
   const int64_t tp = ceil_div(P, ntp), to = ceil_div(t, nto);
   p.tiles_p = (int)std::max<int64_t>(1, ceil_div(rows_p, ntp));
   if (!ragged)
     p.tiles_o = (int)ceil_div(to, std::max<int64_t>(1, (t + rows / 2) / std::max<int64_t>(1, rows)));
-  else if (P > 0 && rows <= kShortBlock)
+  else if (P > 0 && !is_long)
     p.tiles_o = (int)ceil_div(rows_p, nto);
   else
     p.tiles_o = (int)std::max(std::min<int64_t>(2, ceil_div(rows, nto)), ceil_div(rows, kFiner * nto));
