@@ -131,8 +131,9 @@ size_t radar_attend_accumulate_workspace_bytes(const radar_config* cfg, int64_t 
  * min(lens[b], n) (an invalid lens[b] as it is; it may be lens itself); kept
  * (nullable, device int32 [batch][n_kv_heads][min(n, t)]) the rows that were
  * kept, ascending, -1 behind them. 0 <= t <= capacity, t below 2^31 - 2^14;
- * heavy, recent >= 0; n below 2^31. The summaries of the index are not
- * touched: they hold for the old rows, and radar_build_index follows. */
+ * heavy, recent >= 0; n below 2^31; a head's kept rows of K at most 2^39 - 2^17
+ * bytes. The summaries of the index are not touched: they hold for the old
+ * rows, and radar_build_index follows. */
 radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass,
                          int64_t t, const int64_t* lens, int64_t heavy,
                          int64_t recent, int64_t* new_lens, int32_t* kept,

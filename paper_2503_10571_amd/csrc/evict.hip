@@ -1,6 +1,7 @@
 // Eviction by accumulated attention weight (include/radar_cache.h): which rows
 // stay, and their move to the front of K, V and the masses, in place.
 #include "cache_impl.h"
+#include "evict_slices.h"
 
 namespace radar_impl {
 namespace {
@@ -52,10 +53,6 @@ __device__ __forceinline__ uint32_t mass_key(float x) {
 // us, in slices 41; 200000 rows of 8 pairs 31; 16.8 MB of masses are read four times).
 // Listing the first bin's keys instead of two more histograms is 2 us faster where
 // they are few, and where most masses share a bin 1.5 ms slower (a million rows).
-constexpr int kSelThreads = 1024, kPer = 8;
-constexpr int kStep = kSelThreads * kPer;
-constexpr int kSlices = 32;                // at most
-constexpr int64_t kMostRows = INT32_MAX - 2 * kStep;   // row numbers of a step fit 32 bits
 // bits of the key below each histogram's
 __host__ __device__ constexpr int key_shift(int level) { return level == 0 ? 21 : level == 1 ? 10 : 0; }
 constexpr int kBins = 2048, kRank = 256;   // (1024 keys: 25 us to rank, 6 by two histograms)
@@ -99,7 +96,7 @@ __device__ __forceinline__ bool rows_of(const EvictArgs& a, int64_t bh, int slic
   r->lo = a.sink;
   r->hi = r->len - a.recent;
   r->begin = slice * slice_rows;
-  r->end = min(r->len, r->begin + slice_rows);
+  r->end = slice_end(r->len, r->begin, slice_rows);
   r->mass = a.mass + bh * a.cap;
   return r->begin < r->len;
 }
@@ -339,7 +336,7 @@ struct Level {
 };
 __device__ __forceinline__ Level read_level(const EvictArgs& a, const Rows& r, int level, int need, int mine,
                                             int* wsum, int* pick, int* before) {
-  const int slices = (r.len + a.slice_rows - 1) / a.slice_rows;
+  const int slices = slices_of(r.len, a.slice_rows);
   const int* hist = a.hist + (r.bh * 3 + level) * a.slices * kBins;
   const int nb = level < 2 ? kBins : kBins / 2;
   int2 first = make_int2(0, 0);                // of the slices before
@@ -456,9 +453,6 @@ __global__ __launch_bounds__(kSelThreads) void k_evict_list(EvictArgs a) {
 // for 48 pairs of 16K rows of 256 bytes, 173 this way: 4.7 TB/s).
 // The new lengths, which may replace the old ones, are written here, when nobody
 // reads those any more.
-constexpr int kMoveThreads = 1024, kMoveVecs = 8;
-constexpr int kMoveBytes = kMoveThreads * kMoveVecs * 16;
-
 template <int CPR, bool PAST>              // 16-byte chunks of a row; stores past the caches
 __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a) {
   constexpr int R = kMoveThreads * kMoveVecs / CPR;        // rows per chunk
@@ -475,7 +469,8 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a) {
   const int n = (int)a.n;
   if (blockIdx.z == 2) {                           // the masses, where slices listed them
     float* mass = a.mass + bh * a.cap;
-    for (int i = blockIdx.x * kMoveThreads + tid; i < a.cut[bh]; i += gridDim.x * kMoveThreads)
+    for (int64_t i = (int64_t)blockIdx.x * kMoveThreads + tid; i < a.cut[bh];
+         i += (int64_t)gridDim.x * kMoveThreads)
       mass[i] = i < n ? a.moved[bh * a.n + i] : 0.f;
     return;
   }
@@ -511,9 +506,6 @@ __global__ __launch_bounds__(kMoveThreads) void k_evict_move(EvictArgs a) {
   }
 }
 
-// rows of a slice: whole steps, and at most kSlices slices
-int64_t slice_rows(int64_t t) { return ceil_div(ceil_div(t, kSlices), kStep) * kStep; }
-
 struct EvictWs {
   size_t turn, arrived, src, hist, found, above, moved, total;
   int64_t chunks;
@@ -522,7 +514,7 @@ EvictWs evict_ws(const Shape& s, int64_t t, int64_t n) {
   const size_t pairs = (size_t)s.B * s.Hkv;
   const int row_bytes = s.d * (s.dt == RADAR_BF16 ? 2 : 4);
   EvictWs w;
-  w.chunks = ceil_div(n * row_bytes, kMoveBytes);
+  w.chunks = move_chunks(n, row_bytes);
   w.turn = align256(pairs * 4);
   w.arrived = w.turn + align256(pairs * 8);
   w.src = w.arrived + align256(pairs * 2 * w.chunks * 4);
@@ -553,7 +545,8 @@ size_t radar_evict_workspace_bytes(const radar_config* cfg, int64_t t, int64_t h
       t > kMostRows || heavy > INT32_MAX || recent > INT32_MAX ||
       s.n_sink + heavy + recent > INT32_MAX)
     return 0;
-  return evict_ws(s, t, std::min<int64_t>(s.n_sink + heavy + recent, t)).total;
+  const EvictWs w = evict_ws(s, t, std::min<int64_t>(s.n_sink + heavy + recent, t));
+  return w.chunks > kMostChunks ? 0 : w.total;
 }
 
 radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass, int64_t t,
@@ -587,7 +580,7 @@ radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass,
   a.found = reinterpret_cast<int2*>(ws + w.found);
   a.above = reinterpret_cast<int*>(ws + w.above);
   a.moved = reinterpret_cast<float*>(ws + w.moved);
-  a.slice_rows = (int)slice_rows(t);
+  a.slice_rows = (int)slice_rows_of(t);
   a.slices = t > 0 ? (int)ceil_div(t, a.slice_rows) : 1;
   a.B = s.B; a.Hkv = s.Hkv; a.t = t; a.cap = s.cap;
   a.sink = s.n_sink; a.heavy = (int)heavy; a.recent = (int)recent;
