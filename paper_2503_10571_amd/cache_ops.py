@@ -229,7 +229,8 @@ def rotary(rope: Rope, x, pos, out=None, inverse: bool = False, lens=None):
 
 def rotary_qk(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = False,
               lens=None):
-    """rotary() of q and k in one launch. Returns (q_out, k_out)."""
+    """rotary() of q and k in one launch; either may have no heads. Returns
+    (q_out, k_out)."""
     _float_type(q, "q")
     rq, B, T, Hq, d = _rows(q, "q", q.dtype)
     rk, Bk, Tk, Hk, dk = _rows(k, "k", q.dtype)
@@ -240,10 +241,15 @@ def rotary_qk(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = Fal
     p0, p, each = _positions(pos, B, T)
     lens = _lens_of(lens, B)
     _one_device(q, k, p, lens, rope.inv_freq)
-    if q.numel() and k.numel():
+    if B * T * d and (Hq or Hk):
         by = ctypes.byref
-        _call("radar_rotary", q, by(rope._c), B, T, d, _DTYPES[q.dtype], Hq, by(rq), by(qo),
-              Hk, by(rk), by(ko), p0, _ptr(p), each, _ptr(lens), 1 if inverse else 0)
+        first, second = (Hq, by(rq), by(qo)), (Hk, by(rk), by(ko))
+        if not Hq:                             # k is the only operand
+            first, second = second, first
+        if not second[0]:
+            second = (0, None, None)
+        _call("radar_rotary", q, by(rope._c), B, T, d, _DTYPES[q.dtype], *first, *second,
+              p0, _ptr(p), each, _ptr(lens), 1 if inverse else 0)
     return q_out, k_out
 
 
