@@ -166,10 +166,12 @@ def _rows(x, name, dtype):
     return _Rows(ptr, sb, st, sh), B, T, H, d
 
 
-def _out_rows(x, out, name):
-    """(out, struct) for the input x: a new dense tensor, or the given one."""
+def _out_rows(x, out, name, lens):
+    """(out, struct) for the input x: the given tensor, or a new dense one (zeros
+    where lengths leave tokens unwritten)."""
     if out is None:
-        out = torch.empty_like(x, memory_format=torch.contiguous_format)
+        new = torch.empty_like if lens is None else torch.zeros_like
+        out = new(x, memory_format=torch.contiguous_format)
         H, d = x.shape[-2:]
         if d * out.element_size() % 16 == 0:
             T = x.shape[1] if x.dim() == 4 else 1
@@ -213,10 +215,10 @@ def rotary(rope: Rope, x, pos, out=None, inverse: bool = False, lens=None):
     token), strided as it comes out of a projection. pos: the position of the
     first token (an int, or an int64 [B]) or of every token (int64 [B][T]).
     out may be x. inverse: the gradient of the rotation. lens (int64 [B]): only
-    tokens t < lens[b] are touched. Returns out."""
+    tokens t < lens[b] are touched (the others are 0 in a new out). Returns out."""
     _float_type(x, "x")
     rx, B, T, H, d = _rows(x, "x", x.dtype)
-    out, ro = _out_rows(x, out, "out")
+    out, ro = _out_rows(x, out, "out", lens)
     p0, p, each = _positions(pos, B, T)
     lens = _lens_of(lens, B)
     _one_device(x, p, lens, rope.inv_freq)
@@ -236,8 +238,8 @@ def rotary_qk(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = Fal
     rk, Bk, Tk, Hk, dk = _rows(k, "k", q.dtype)
     if (Bk, Tk, dk) != (B, T, d):
         raise ValueError("q and k must agree in batch, tokens and head_dim")
-    q_out, qo = _out_rows(q, q_out, "q_out")
-    k_out, ko = _out_rows(k, k_out, "k_out")
+    q_out, qo = _out_rows(q, q_out, "q_out", lens)
+    k_out, ko = _out_rows(k, k_out, "k_out", lens)
     p0, p, each = _positions(pos, B, T)
     lens = _lens_of(lens, B)
     _one_device(q, k, p, lens, rope.inv_freq)
@@ -258,8 +260,8 @@ def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_ou
     """radar_rotary_fill: the chunk k, v [B][T][Hkv][d] (or [B][Hkv][d], one
     token) into rows row + t of K and V, k rotated; with q, its rotation too,
     in the same launch. row: an int, or an int64 [B] (rows outside the capacity
-    are skipped); pos: as for rotary(), the row itself if None. lens: only
-    tokens t < lens[b]. Returns q_out (None without q)."""
+    are skipped); pos: as for rotary(), the row itself if None. lens: as for
+    rotary(). Returns q_out (None without q)."""
     _cache(cfg, K, V)
     rk, B, T, Hk, d = _rows(k, "k", cfg.dtype)
     rv, *shape_v = _rows(v, "v", cfg.dtype)
@@ -272,7 +274,7 @@ def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_ou
         rq, *shape_q = _rows(q, "q", cfg.dtype)
         if shape_q != [B, T, cfg.n_q_heads, d]:
             raise ValueError("q must be [batch][T][n_q_heads][head_dim] with k's tokens")
-        q_out, qo = _out_rows(q, q_out, "q_out")
+        q_out, qo = _out_rows(q, q_out, "q_out", lens)
         rq, qo = by(rq), by(qo)
     elif q_out is not None:
         raise ValueError("q_out without q")

@@ -30,3 +30,34 @@ def test_one_operand_without_heads(dtype):
         assert a.shape == (2, 5, 0, 64)
     a, b = radar.rotary_qk(rope, none, none, 3)
     assert a.shape == b.shape == (2, 5, 0, 64)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_new_outputs_are_zero_behind_the_lengths(dtype):
+    """Also where the memory they get held something else."""
+    B, T, Hq, Hkv, d = 3, 6, 4, 2, 64
+    rope = _rope(64)
+    q = torch.randn(B, T, Hq, d, device="cuda").to(DT[dtype])
+    k, v = (torch.randn(B, T, Hkv, d, device="cuda").to(DT[dtype]) for _ in range(2))
+    lens = torch.tensor([6, 0, 2], device="cuda")
+    cfg = radar.Config(B, Hq, Hkv, d, 64, 16, 16, 20, DT[dtype])
+    K, V = (torch.zeros(B, Hkv, 20, d, dtype=DT[dtype], device="cuda") for _ in range(2))
+    ref, tol = _ref(q, rope, _grid(4, B, T))
+
+    def calls():
+        yield radar.rotary(rope, q, 4, lens=lens)
+        yield radar.rotary_qk(rope, q, k, 4, lens=lens)[0]
+        yield radar.rotary_fill(cfg, rope, K, V, k, v, 4, q=q, lens=lens)
+        a, b = radar.rotary_qk(rope, k, q, 4, lens=lens)
+        assert bool((a[1] == 0).all())
+        yield b
+
+    it = calls()
+    for _ in range(4):
+        used = [torch.full_like(q, float("nan")) for _ in range(4)]
+        del used
+        got = next(it)
+        for b, n in enumerate((6, 0, 2)):
+            _close(got[b, :n], ref[b, :n], tol[b, :n])
+            assert bool((got[b, n:] == 0).all())
+        del got
