@@ -210,13 +210,64 @@ def _float_type(x, name):
         raise ValueError(f"{name} must be float32 or bfloat16, got {x.dtype}")
 
 
+def _records(rope, x, y=None):
+    """Whether autograd records a call on x (and y)."""
+    if not (x.requires_grad or y is not None and y.requires_grad or rope.inv_freq.requires_grad):
+        return False
+    if torch.is_grad_enabled() and rope.inv_freq.requires_grad:
+        raise RuntimeError("inv_freq has no gradient here: detach it")
+    return torch.is_grad_enabled()
+
+
+def _no_gradient(fn, *xs):
+    """For the calls that autograd does not know: refuses operands whose gradient
+    would be lost without a word."""
+    if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in xs):
+        raise RuntimeError(f"{fn} has no gradient: call it under torch.no_grad(), or detach "
+                           "its operands")
+
+
+class _Rotate(torch.autograd.Function):
+    """rotary (one operand) and rotary_qk (two) for autograd: the gradient is the
+    inverse rotation of the outputs' gradients."""
+
+    @staticmethod
+    def forward(ctx, rope, pos, inverse, lens, *xs):
+        ctx.set_materialize_grads(False)
+        ctx.rope, ctx.pos, ctx.inverse = rope, pos, inverse
+        # (saved so that a change in place before the backward pass is found)
+        ctx.save_for_backward(rope.inv_freq, lens, None if isinstance(pos, int) else pos)
+        if len(xs) == 1:
+            return rotary(rope, *xs, pos, inverse=inverse, lens=lens)
+        return rotary_qk(rope, *xs, pos, inverse=inverse, lens=lens)
+
+    @staticmethod
+    def backward(ctx, *grads):
+        _, lens, pos = ctx.saved_tensors
+        kw = dict(pos=ctx.pos if pos is None else pos, inverse=not ctx.inverse, lens=lens)
+        want = [g if need else None for g, need in zip(grads, ctx.needs_input_grad[4:])]
+        # gradients of any layout; the kernel takes dense rows on 16 bytes
+        want = [g if g is None else g.contiguous() for g in want]
+        want = [g.clone() if g is not None and g.data_ptr() & 15 else g for g in want]
+        if len(want) == 2 and want[0] is not None and want[1] is not None:
+            got = rotary_qk(ctx.rope, *want, **kw)
+        else:
+            got = [g if g is None else rotary(ctx.rope, g, **kw) for g in want]
+        return (None, None, None, None, *got)
+
+
 def rotary(rope: Rope, x, pos, out=None, inverse: bool = False, lens=None):
     """radar_rotary of one tensor x, [B][T][heads][d] or [B][heads][d] (one
     token), strided as it comes out of a projection. pos: the position of the
     first token (an int, or an int64 [B]) or of every token (int64 [B][T]).
     out may be x. inverse: the gradient of the rotation. lens (int64 [B]): only
-    tokens t < lens[b] are touched (the others are 0 in a new out). Returns out."""
+    tokens t < lens[b] are touched (the others are 0 in a new out). Autograd
+    differentiates it in x, where out is not given. Returns out."""
     _float_type(x, "x")
+    if _records(rope, x):
+        if out is not None:
+            raise RuntimeError("rotary takes no out where a gradient is recorded")
+        return _Rotate.apply(rope, pos, inverse, lens, x)
     rx, B, T, H, d = _rows(x, "x", x.dtype)
     out, ro = _out_rows(x, out, "out", lens)
     p0, p, each = _positions(pos, B, T)
@@ -234,6 +285,10 @@ def rotary_qk(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = Fal
     """rotary() of q and k in one launch; either may have no heads. Returns
     (q_out, k_out)."""
     _float_type(q, "q")
+    if _records(rope, q, k):
+        if q_out is not None or k_out is not None:
+            raise RuntimeError("rotary_qk takes no q_out and k_out where a gradient is recorded")
+        return _Rotate.apply(rope, pos, inverse, lens, q, k)
     rq, B, T, Hq, d = _rows(q, "q", q.dtype)
     rk, Bk, Tk, Hk, dk = _rows(k, "k", q.dtype)
     if (Bk, Tk, dk) != (B, T, d):
@@ -261,7 +316,9 @@ def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_ou
     token) into rows row + t of K and V, k rotated; with q, its rotation too,
     in the same launch. row: an int, or an int64 [B] (rows outside the capacity
     are skipped); pos: as for rotary(), the row itself if None. lens: as for
-    rotary(). Returns q_out (None without q)."""
+    rotary(). No gradient goes through the cache: operands that want one are
+    refused. Returns q_out (None without q)."""
+    _no_gradient("rotary_fill", k, v, q, q_out, K, V, rope.inv_freq)
     _cache(cfg, K, V)
     rk, B, T, Hk, d = _rows(k, "k", cfg.dtype)
     rv, *shape_v = _rows(v, "v", cfg.dtype)
@@ -327,7 +384,8 @@ def attend_prefix(cfg: Config, q, Kp, Vp, prefix_len: int, K=None, V=None, t: in
     """radar_attend_prefix: exact attention of every sequence's query (q
     [B][Hq][d]) over rows [0, prefix_len) of Kp, Vp [Hkv][rows][d], which the
     batch shares, and rows [0, t) (or [0, lens[b])) of its own K, V (None with
-    t = 0). Returns out."""
+    t = 0). Has no gradient: operands that want one are refused. Returns out."""
+    _no_gradient("attend_prefix", q, Kp, Vp, K, V, out)
     out, lens = _attended(cfg, q, out, lens)
     prefix_cap = 0
     if prefix_len > 0:
@@ -366,7 +424,8 @@ def attend_accumulate(cfg: Config, q, K, V, mass, t: int, out=None, lens=None,
     """radar_attend_accumulate: exact attention over rows [0, t) (or
     [0, lens[b])) of K and V; the softmax weight of every row, summed over the
     query heads of its kv head, is added to mass [B][Hkv][capacity] (fp32).
-    Returns out."""
+    Has no gradient: operands that want one are refused. Returns out."""
+    _no_gradient("attend_accumulate", q, K, V, mass, out)
     out, lens = _attended(cfg, q, out, lens)
     _cache(cfg, K, V)
     _mass(cfg, mass)
@@ -396,6 +455,7 @@ def evict(cfg: Config, K, V, mass, t: int, heavy: int, recent: int, lens=None,
     lens) receives the new lengths, kept (int32 [B][Hkv][min(n, t)]) the rows
     kept. The summaries hold for the old rows: build_index() follows. Returns
     the bound of the new lengths, min(t, n)."""
+    _no_gradient("evict", K, V, mass)
     _cache(cfg, K, V)
     _mass(cfg, mass)
     n = min(cfg.n_sink + heavy + recent, t)
