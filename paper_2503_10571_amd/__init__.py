@@ -585,15 +585,26 @@ class RadarLayer:
 
     def prefill(self, k, v, q=None, q_out=None):
         """A chunk of tokens behind the cache's rows: k, v [B][T][Hkv][d],
-        rotated with rope, and the index of all rows. With q [B][T][Hq][d] and
-        rope returns its rotation too (q itself without rope)."""
-        T = k.shape[1]
+        rotated with rope, and the index of all rows. With q [B][T][Hq][d]
+        returns its rotation too (without rope q itself, or q_out with q's
+        values)."""
+        cfg, T = self.cfg, k.shape[1]
+        for x, name in ((k, "k"), (v, "v")):
+            if x.dtype != cfg.dtype or x.shape != (cfg.batch, T, cfg.n_kv_heads, cfg.head_dim):
+                raise ValueError(f"{name} must be {cfg.dtype} [{cfg.batch}][T][{cfg.n_kv_heads}]"
+                                 f"[{cfg.head_dim}], got {x.dtype} {list(x.shape)}")
         if self.rope is not None:
-            q = rotary_fill(self.cfg, self.rope, self.K, self.V, k, v, self.t, pos=self.pos,
+            q = rotary_fill(cfg, self.rope, self.K, self.V, k, v, self.t, pos=self.pos,
                             q=q, q_out=q_out)
         else:
-            if self.t + T > self.cfg.capacity:
+            cache_ops._no_gradient("prefill", k, v, self.K, self.V)
+            if q_out is not None and (q is None or q_out.shape != q.shape or
+                                      q_out.dtype != q.dtype):
+                raise ValueError("q_out must have q's shape and type")
+            if self.t + T > cfg.capacity:
                 raise RadarError("prefill", 2)
+            if q_out is not None:
+                q = q_out.copy_(q)
             self.K[:, :, self.t:self.t + T].copy_(k.transpose(1, 2))
             self.V[:, :, self.t:self.t + T].copy_(v.transpose(1, 2))
         self.t += T
