@@ -141,7 +141,11 @@ def lib() -> ctypes.CDLL:
                    "radar_attend_selected",
                    "radar_profile_enable", "radar_profile_read"):
             getattr(L, fn).restype = ctypes.c_int
-        cache_ops.declare(L)
+        try:
+            cache_ops.declare(L)
+        except AttributeError as e:            # (the ABI grew by these calls alone)
+            raise RuntimeError(f"{LIB_PATH} lacks calls that this binding has: "
+                               f"rebuild it ({e})") from e
         _lib = L
     return _lib
 
