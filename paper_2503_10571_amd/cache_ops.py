@@ -80,7 +80,7 @@ def _call(fn, x, *args):
 
 
 # ---- rotary positions --------------------------------------------------------
-@dataclasses.dataclass(frozen=True)
+@dataclasses.dataclass(frozen=True, eq=False)   # (tensors have no truth value)
 class Rope:
     """Rotary positions of a head: inv_freq, a device float64 tensor
     [rot_dim / 2] of angles per position (see rope_frequencies); interleaved:
@@ -95,6 +95,9 @@ class Rope:
         object.__setattr__(self, "_c", _Rope(2 * self.inv_freq.numel(),
                                              1 if self.interleaved else 0, self.mscale,
                                              self.inv_freq.data_ptr()))
+
+    def __reduce__(self):                          # the pointer is not copied
+        return Rope, (self.inv_freq, self.interleaved, self.mscale)
 
     @property
     def rot_dim(self) -> int:

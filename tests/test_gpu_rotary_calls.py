@@ -1,6 +1,9 @@
 """Calls of the rotary operators beside those of test_gpu_rotary.py: operands
 without heads, new outputs behind the lengths, autograd."""
+import copy
+import dataclasses
 import os
+import pickle
 import sys
 
 import pytest
@@ -230,3 +233,22 @@ def test_autograd_captured():
         g.replay()
         torch.randn(1 << 20, device="cuda").sum().item()
         assert torch.equal(out, want) and torch.equal(dx, wdx), rep
+
+
+# ---- the operator's handle ---------------------------------------------------------
+def test_rope_copies():
+    """Copies and pickles hold frequencies of their own, and compare by identity."""
+    rope = _rope(48, True, "yarn", 4.0)
+    x = torch.randn(2, 3, 2, 64, device="cuda")
+    want = radar.rotary(rope, x, 99)
+    for other in (copy.copy(rope), copy.deepcopy(rope), pickle.loads(pickle.dumps(rope))):
+        assert (other.rot_dim, other.interleaved, other.mscale) == (48, True, rope.mscale)
+        assert torch.equal(radar.rotary(other, x, 99), want)
+        assert other != rope and other == other and len({rope, other}) == 2
+    deep = copy.deepcopy(rope)
+    assert deep.inv_freq.data_ptr() != rope.inv_freq.data_ptr()
+    rope.inv_freq.zero_()
+    assert torch.equal(radar.rotary(deep, x, 99), want)
+    # with a changed field, as a dataclass
+    flat = dataclasses.replace(deep, interleaved=False)
+    _close(radar.rotary(flat, x, 99), *_ref(x, flat, _grid(99, 2, 3)))
