@@ -127,11 +127,12 @@ __global__ __launch_bounds__(256) void k_settle(FlashArgs a, T* out, float* __re
     for (int i = lane; i < n_own; i += kWave) {
       const float2 v = *reinterpret_cast<const float2*>(ml + 2 * (int64_t)i * a.G);
       const float top = fmaxf(m, v.x);
-      if (top > -INFINITY) l = l * fast_exp2(m - top) + v.y * fast_exp2(v.x - top);
+      // (no maximum yet: the sums so far are 0, or NaN where a part's logits are)
+      l = top > -INFINITY ? l * fast_exp2(m - top) + v.y * fast_exp2(v.x - top) : l + v.y;
       m = top;
     }
     const float M = wave_max(m);
-    l = wave_sum(m == -INFINITY ? 0.f : l * fast_exp2(m - M));
+    l = wave_sum(m == -INFINITY ? l : l * fast_exp2(m - M));
     if (lane == 0) { m_lds[g] = M; r_lds[g] = 1.f / l; }
   }
   __syncthreads();
