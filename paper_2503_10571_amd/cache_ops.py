@@ -215,19 +215,21 @@ def _float_type(x, name):
 
 def _records(rope, x, y=None):
     """Whether autograd records a call on x (and y)."""
-    if not (x.requires_grad or y is not None and y.requires_grad or rope.inv_freq.requires_grad):
+    if not torch.is_grad_enabled():
         return False
-    if torch.is_grad_enabled() and rope.inv_freq.requires_grad:
+    if rope.inv_freq.requires_grad:
         raise RuntimeError("inv_freq has no gradient here: detach it")
-    return torch.is_grad_enabled()
+    return x.requires_grad or y is not None and y.requires_grad
 
 
 def _no_gradient(fn, *xs):
     """For the calls that autograd does not know: refuses operands whose gradient
     would be lost without a word."""
-    if torch.is_grad_enabled() and any(x is not None and x.requires_grad for x in xs):
-        raise RuntimeError(f"{fn} has no gradient: call it under torch.no_grad(), or detach "
-                           "its operands")
+    if torch.is_grad_enabled():
+        for x in xs:
+            if x is not None and x.requires_grad:
+                raise RuntimeError(f"{fn} has no gradient: call it under torch.no_grad(), or "
+                                   "detach its operands")
 
 
 class _Rotate(torch.autograd.Function):
@@ -321,7 +323,7 @@ def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_ou
     are skipped); pos: as for rotary(), the row itself if None. lens: as for
     rotary(). No gradient goes through the cache: operands that want one are
     refused. Returns q_out (None without q)."""
-    _no_gradient("rotary_fill", k, v, q, q_out, K, V, rope.inv_freq)
+    _no_gradient("rotary_fill", k, v, q, rope.inv_freq)
     _cache(cfg, K, V)
     rk, B, T, Hk, d = _rows(k, "k", cfg.dtype)
     rv, *shape_v = _rows(v, "v", cfg.dtype)
@@ -388,7 +390,7 @@ def attend_prefix(cfg: Config, q, Kp, Vp, prefix_len: int, K=None, V=None, t: in
     [B][Hq][d]) over rows [0, prefix_len) of Kp, Vp [Hkv][rows][d], which the
     batch shares, and rows [0, t) (or [0, lens[b])) of its own K, V (None with
     t = 0). Has no gradient: operands that want one are refused. Returns out."""
-    _no_gradient("attend_prefix", q, Kp, Vp, K, V, out)
+    _no_gradient("attend_prefix", q, Kp, Vp, K, V)
     out, lens = _attended(cfg, q, out, lens)
     prefix_cap = 0
     if prefix_len > 0:
@@ -428,7 +430,7 @@ def attend_accumulate(cfg: Config, q, K, V, mass, t: int, out=None, lens=None,
     [0, lens[b])) of K and V; the softmax weight of every row, summed over the
     query heads of its kv head, is added to mass [B][Hkv][capacity] (fp32).
     Has no gradient: operands that want one are refused. Returns out."""
-    _no_gradient("attend_accumulate", q, K, V, mass, out)
+    _no_gradient("attend_accumulate", q, K, V)
     out, lens = _attended(cfg, q, out, lens)
     _cache(cfg, K, V)
     _mass(cfg, mass)
@@ -458,7 +460,6 @@ def evict(cfg: Config, K, V, mass, t: int, heavy: int, recent: int, lens=None,
     lens) receives the new lengths, kept (int32 [B][Hkv][min(n, t)]) the rows
     kept. The summaries hold for the old rows: build_index() follows. Returns
     the bound of the new lengths, min(t, n)."""
-    _no_gradient("evict", K, V, mass)
     _cache(cfg, K, V)
     _mass(cfg, mass)
     n = min(cfg.n_sink + heavy + recent, t)

@@ -19,12 +19,9 @@ def _calls():
     for i in range(5):
         a = [v.clone().requires_grad_(i == j) for j, v in enumerate((y, c[0], c[0], c, c))]
         yield "prefix", lambda a=a: radar.attend_prefix(CFG, a[0], a[1], a[2], 3, a[3], a[4], 3)
-    for i in range(4):
-        a = [v.clone().requires_grad_(i == j) for j, v in enumerate((y, c, c, m))]
-        yield "accumulate", lambda a=a: radar.attend_accumulate(CFG, *a, 3)
     for i in range(3):
-        a = [v.clone().requires_grad_(i == j) for j, v in enumerate((c, c, m))]
-        yield "evict", lambda a=a: radar.evict(CFG, *a, 3, 1, 1)
+        a = [v.clone().requires_grad_(i == j) for j, v in enumerate((y, c, c))]
+        yield "accumulate", lambda a=a: radar.attend_accumulate(CFG, *a, m, 3)
 
 
 def test_operands_that_want_a_gradient_are_refused():
