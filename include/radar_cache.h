@@ -15,6 +15,11 @@
  * index and the selection are not read. Workspaces: contents on entry do not
  * matter, and one workspace must not be used by two calls at the same time
  * (two graphs that hold the same one must not be replayed concurrently).
+ *
+ * The measurement hook of radar.h books their kernels under the kinds that it
+ * has: rotations and the eviction's move as RADAR_K_APPEND, the attention's
+ * blocks as _ATTEND, what follows them (merge and masses) as _COMBINE, the
+ * eviction's choice of rows as _TOPK.
  */
 #ifndef RADAR_CACHE_H
 #define RADAR_CACHE_H
@@ -84,11 +89,15 @@ radar_status radar_rotary_fill(const radar_config* cfg, const radar_rope* rope,
  * Kp, Vp [n_kv_heads][prefix_capacity][head_dim], which all sequences share,
  * and rows [0, t) (with lens, nullable device int64 [batch], [0, lens[b]),
  * t their bound) of the sequence's own K and V: exact softmax attention with
- * the scale 1/sqrt(head_dim). A read of a prefix row serves up to 128 query
- * rows of its kv head (batch * n_q_heads / n_kv_heads). 0 <= prefix_len <= prefix_capacity < 2^31, 0 <= t <= capacity; Kp and
- * Vp may be NULL with prefix_len = 0, K and V with t = 0. A query that attends
- * no row gets a zero output; lens[b] outside [0, t] makes that sequence's
- * outputs NaN. */
+ * the scale 1/sqrt(head_dim). Of the batch * n_q_heads / n_kv_heads query rows
+ * of a kv head up to 128 share one read of a prefix row (fp32: 16, 64 or 128);
+ * more read it again. 0 <= prefix_len <= prefix_capacity < 2^31, 0 <= t <=
+ * capacity; Kp and Vp may be NULL with prefix_len = 0, K and V with t = 0. A
+ * query that attends no row gets a zero output; lens[b] outside [0, t] makes
+ * that sequence's outputs NaN. With a bf16 cache the weights enter the product
+ * with V in 16 bits where at most 16 query rows share a read, and rounded to
+ * bf16 where more do (the output's error is then up to 1.4 times that of its own
+ * rounding); everything else is fp32. */
 radar_status radar_attend_prefix(const radar_config* cfg, const void* q,
                                  const void* Kp, const void* Vp,
                                  int64_t prefix_len, int64_t prefix_capacity,

@@ -605,9 +605,11 @@ radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass,
   const bool moves = a.n > 0 && a.n < t;
   if (r != RADAR_OK || !(moves || sliced || new_lens)) return r;
   const dim3 grid(std::max(1u, moves ? (unsigned)w.chunks : 1u), pairs, sliced ? 3 : moves ? 2 : 1);
-  // The stores pass the caches by where the rows that stay are three times what those
-  // hold: 64 pairs of 21004 rows of 256 bytes 265 us, 238 this way; 16384, a third of
-  // them uncut: 183, 173; but 9004: 105, 110.
+  // The stores pass the caches by where the rows that stay, K's and V's, read and
+  // written, are more than 768 MB, three times what the caches hold; sequences that are
+  // not cut, which only the GPU knows, count too. 64 pairs of 21004 rows of 256 bytes
+  // (1376 MB): 265 us, 238 this way; 16384 (1074), a third of them uncut: 183, 173; but
+  // 9004 (590): 105, 110.
   const bool past = 4 * a.n * pairs * a.row_bytes > ((int64_t)768 << 20);
   auto go = [&](auto cpr) {
     constexpr int kCpr = decltype(cpr)::value;

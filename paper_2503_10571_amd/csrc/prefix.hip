@@ -158,10 +158,15 @@ __global__ __launch_bounds__(256) void k_settle(FlashArgs a, T* out, float* __re
 // How a call is cut: about as many workgroups as the chip holds at once (two per
 // CU), each with the same number of rows. Twice or three times as many only cost
 // starts and partials (64K rows for 32 sequences of four heads, with the merge:
-// 68 us, 84, 97). Blocks of the prefix of up to kShortBlock rows are twice as long: 32
-// sequences over 8192 rows, 128 a block: 24.0 us, 19.9 this way; 16411, 257: 29.5,
-// 26.4; 32768, 512: 38.4, 37.1; but 65536, 1024: 60.7, 62.5; and where the matrix cores
-// bound (fp32, more than 16 query rows) 64 rows over 4000: 28.3, 30.8; 30000: 98.8, 102.4.
+// 68 us, 84, 97). Blocks of the prefix of up to kShortBlock rows are twice as long, half
+// as many starts, partials and parts to merge: 32 sequences over 8192 rows, 128 a block:
+// 24.0 us, 19.9 this way; 16411, 257: 29.5, 26.4; 32768, 512: 38.4, 37.1; but 65536,
+// 1024: 60.7, 62.5. With few query rows, whose partials are small, it is the starts (GPU
+// time, eight kv heads, caches cold): four rows over 4096: 12.5, 11.3; over 16411: 22.1,
+// 19.0; sixteen: 13.0, 12.5 and 23.2, 20.5; in fp32 four rows over 8192: 22.5, 18.9; but
+// six sequences of 16 heads in fp32 over 8192 and 301 own rows 35.2, 40.0, and at head
+// dim 64 four rows over 8192: 9.9, 10.4. Where the matrix cores bound (fp32, more than 16
+// query rows) not: 64 rows over 4000: 28.3, 30.8; 30000: 98.8, 102.4.
 //
 // A sequence's own rows take as many blocks as come nearest to that length (32
 // sequences of 700 rows over 16411, blocks of 607: one each 36, two 38 us). Of sequences
@@ -201,8 +206,8 @@ Plan plan_flash(const Shape& s, int64_t P, int64_t t, bool ragged) {
   p.mtiles = row_tiles(s);
   const int ntp = flash_tile(esize(s), p.rw), nto = flash_tile(esize(s), 1);
   const int64_t rows = ceil_div((int64_t)s.Hkv * p.mtiles * P + pairs * t, slots());
-  // a block of a short prefix spends as long on its partials (64 KB at 128 query rows)
-  // as on its rows: one a CU then, twice as long
+  // a block of a short prefix spends as long on its start and its partials (64 KB at 128
+  // query rows) as on its rows: one a CU then, twice as long
   const bool matrix_bound = esize(s) == 4 && s.B * s.G > flash_rows(4, 1);
   const bool is_long = rows > kShortBlock || matrix_bound;
   const int64_t rows_p = is_long ? rows : 2 * rows;
