@@ -436,7 +436,8 @@ def profile_enable(on: bool) -> None:
 
 def profile_read() -> dict:
     """{kernel: (total ms, launches)} of the kernels recorded since the last
-    read; waits for them to finish."""
+    read; waits for them to finish. The cache operators' kernels count as the
+    kinds named in include/radar_cache.h (a rotation as "append")."""
     n = len(KERNELS)
     ms = (ctypes.c_double * n)()
     cnt = (ctypes.c_int64 * n)()
@@ -538,7 +539,9 @@ class RadarLayer:
     rope: rotary positions (Rope); queries and keys are then given unrotated.
     `pos` is the position of the next token: `t` until rows are evicted, the
     number of tokens seen from then on. accumulate() and evict() make room in
-    a full cache by the weights that its rows get."""
+    a full cache by the weights that its rows get; only accumulate() gathers
+    them, by an exact pass over the whole cache (step() and decode() read a few
+    segments and add nothing)."""
 
     def __init__(self, cfg: Config, omega, K=None, V=None, t: int = 0,
                  top_k: int = 16, device="cuda", schedule: str = "fixed",
@@ -591,7 +594,8 @@ class RadarLayer:
         """A chunk of tokens behind the cache's rows: k, v [B][T][Hkv][d],
         rotated with rope, and the index of all rows. With q [B][T][Hq][d]
         returns its rotation too (without rope q itself, or q_out with q's
-        values)."""
+        values). The index is built from row 0 every time: few long chunks cost
+        less than many short ones."""
         cfg, T = self.cfg, k.shape[1]
         for x, name in ((k, "k"), (v, "v")):
             if x.dtype != cfg.dtype or x.shape != (cfg.batch, T, cfg.n_kv_heads, cfg.head_dim):
@@ -665,7 +669,8 @@ class RadarLayer:
 
     def accumulate(self, q, out=None):
         """Exact attention of the last token's query over the whole cache,
-        adding the weight of every row to `mass`."""
+        adding the weight of every row to `mass` (which starts at zero with the
+        first call: a prompt's queries have added nothing)."""
         if self.mass is None:
             self.mass = new_mass(self.cfg, self.device)
         if self.rope is not None:
