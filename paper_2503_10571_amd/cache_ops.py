@@ -80,7 +80,7 @@ def _call(fn, x, *args):
 
 
 # ---- rotary positions --------------------------------------------------------
-@dataclasses.dataclass(frozen=True, eq=False)   # (tensors have no truth value)
+@dataclasses.dataclass(frozen=True, eq=False)
 class Rope:
     """Rotary positions of a head: inv_freq, a device float64 tensor
     [rot_dim / 2] of angles per position (see rope_frequencies); interleaved:
@@ -95,6 +95,16 @@ class Rope:
         object.__setattr__(self, "_c", _Rope(2 * self.inv_freq.numel(),
                                              1 if self.interleaved else 0, self.mscale,
                                              self.inv_freq.data_ptr()))
+
+    # (the same frequencies are the same tensor: two of equal values have no truth value)
+    def _key(self):
+        return id(self.inv_freq), self.interleaved, self.mscale
+
+    def __eq__(self, other):
+        return self._key() == other._key() if isinstance(other, Rope) else NotImplemented
+
+    def __hash__(self):
+        return hash(self._key())
 
     def __reduce__(self):                          # the pointer is not copied
         return Rope, (self.inv_freq, self.interleaved, self.mscale)

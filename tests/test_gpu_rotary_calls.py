@@ -237,14 +237,18 @@ def test_autograd_captured():
 
 # ---- the operator's handle ---------------------------------------------------------
 def test_rope_copies():
-    """Copies and pickles hold frequencies of their own, and compare by identity."""
+    """Deep copies and pickles hold frequencies of their own; equal are those of the
+    same tensor."""
     rope = _rope(48, True, "yarn", 4.0)
     x = torch.randn(2, 3, 2, 64, device="cuda")
     want = radar.rotary(rope, x, 99)
     for other in (copy.copy(rope), copy.deepcopy(rope), pickle.loads(pickle.dumps(rope))):
         assert (other.rot_dim, other.interleaved, other.mscale) == (48, True, rope.mscale)
         assert torch.equal(radar.rotary(other, x, 99), want)
-        assert other != rope and other == other and len({rope, other}) == 2
+        same = other.inv_freq is rope.inv_freq
+        assert (other == rope) is same and len({rope, other}) == (1 if same else 2)
+    assert copy.copy(rope) == rope == radar.Rope(rope.inv_freq, True, rope.mscale)
+    assert rope != radar.Rope(rope.inv_freq, False, rope.mscale) and rope != 1
     deep = copy.deepcopy(rope)
     assert deep.inv_freq.data_ptr() != rope.inv_freq.data_ptr()
     rope.inv_freq.zero_()
@@ -252,3 +256,34 @@ def test_rope_copies():
     # with a changed field, as a dataclass
     flat = dataclasses.replace(deep, interleaved=False)
     _close(radar.rotary(flat, x, 99), *_ref(x, flat, _grid(99, 2, 3)))
+
+
+@pytest.mark.parametrize("fill", [False, True])
+def test_captured_call_with_lengths_and_its_own_output(fill):
+    """Shorter lengths in a later replay: zeros where the one before wrote."""
+    B, T, H, d = 3, 6, 2, 64
+    rope = _rope(64)
+    cfg = radar.Config(B, H, H, d, 64, 16, 16, 20, torch.float32)
+    x, k, v = (torch.randn(B, T, H, d, device="cuda") for _ in range(3))
+    K, V = (torch.zeros(B, H, 20, d, device="cuda") for _ in range(2))
+    lens = torch.tensor([6, 5, 4], device="cuda")
+
+    def call():
+        if fill:
+            return radar.rotary_fill(cfg, rope, K, V, k, v, 4, q=x, lens=lens)
+        return radar.rotary(rope, x, 4, lens=lens)
+
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        out = call()
+    for now in ([6, 6, 6], [6, 0, 2], [1, 3, 0]):
+        lens.copy_(torch.tensor(now, device="cuda"))
+        want = call()
+        torch.cuda.synchronize()
+        g.replay()
+        torch.randn(1 << 20, device="cuda").sum().item()
+        assert torch.equal(out, want)
+        for b, n in enumerate(now):
+            assert not bool(out[b, n:].any())
