@@ -623,9 +623,6 @@ class RadarLayer:
     def append(self, k_new, v_new):
         if self.rope is not None:
             k_new = rotary(self.rope, k_new, self.pos)
-        self._append(k_new, v_new)
-
-    def _append(self, k_new, v_new):
         append(self.cfg, self.K, self.V, k_new, v_new, self.omega, self.t,
                self.summaries)
         self.t += 1
@@ -641,9 +638,6 @@ class RadarLayer:
     def decode(self, q, out=None, selected=None, scores=None):
         if self.rope is not None:                  # the last token's query
             q = rotary(self.rope, q, self.pos - 1)
-        return self._decode(q, out, selected, scores)
-
-    def _decode(self, q, out, selected, scores):
         self._fit_workspace()
         return decode(self.cfg, q, self.K, self.V, self.omega, self.summaries,
                       self.t, self.k, out=out, selected=selected, scores=scores,
@@ -652,11 +646,11 @@ class RadarLayer:
     def step(self, q, k_new, v_new, out=None, selected=None, scores=None):
         """append(k_new, v_new) then decode(q), as one radar_append_decode
         call unless the sqrt schedule restructures at this token."""
+        if self.schedule == "sqrt" and self._cfg_at(self.t + 1).seg_len != self.cfg.seg_len:
+            self.append(k_new, v_new)
+            return self.decode(q, out=out, selected=selected, scores=scores)
         if self.rope is not None:
             q, k_new = rotary_qk(self.rope, q, k_new, self.pos)
-        if self.schedule == "sqrt" and self._cfg_at(self.t + 1).seg_len != self.cfg.seg_len:
-            self._append(k_new, v_new)
-            return self._decode(q, out, selected, scores)
         if self.schedule == "sqrt":
             self.cfg = self._cfg_at(self.t + 1)
         self._fit_workspace()
