@@ -2,8 +2,9 @@
  * radar_cache.h -- C ABI of the cache operators beside the decode path of
  * radar.h: rotary positions for the rows on their way into the cache, exact
  * attention of a batch over a prefix that its sequences share, exact
- * attention that accumulates the weight of every cache row, and eviction of
- * the rows with the least of it.
+ * attention that accumulates the weight of every cache row, eviction of
+ * the rows with the least of it, the acceptance of a path of drafted tokens
+ * (a tree or a chain), and the forking of the cache's sequences.
  *
  * Conventions are those of radar.h: device pointers owned by the caller and
  * aligned to 16 bytes, dense row-major layouts unless strides are given, no
@@ -12,14 +13,14 @@
  * K and V may lie in pinned host memory mapped for the device. Of the
  * radar_config these calls read batch, n_q_heads, n_kv_heads, head_dim,
  * capacity, kv_dtype and n_sink, with radar.h's limits; the fields of the
- * index and the selection are not read. Workspaces: contents on entry do not
+ * index and the selection are not read but where a call says so. Workspaces: contents on entry do not
  * matter, and one workspace must not be used by two calls at the same time
  * (two graphs that hold the same one must not be replayed concurrently).
  *
  * The measurement hook of radar.h books their kernels under the kinds that it
- * has: rotations and the eviction's move as RADAR_K_APPEND, the attention's
- * blocks as _ATTEND, what follows them (merge and masses) as _COMBINE, the
- * eviction's choice of rows as _TOPK.
+ * has: rotations and what moves rows (eviction, acceptance, forking) as
+ * RADAR_K_APPEND, the attention's blocks as _ATTEND, what follows them (merge
+ * and masses) as _COMBINE, the eviction's choice of rows as _TOPK.
  */
 #ifndef RADAR_CACHE_H
 #define RADAR_CACHE_H
@@ -83,6 +84,29 @@ radar_status radar_rotary_fill(const radar_config* cfg, const radar_rope* rope,
                                int64_t row0, const int64_t* rows, int64_t pos0,
                                const int64_t* pos, int32_t pos_per_token,
                                const int64_t* lens, hipStream_t stream);
+
+/* The same two with positions on n_axes axes (time, height, width, ..): pair i
+ * turns by pos[axis[i]][b][t] * inv_freq[i], with axis a device int32
+ * [rot_dim / 2] and pos a device int64 [n_axes][batch][tokens]. An axis[i]
+ * outside [0, n_axes) makes the pair NaN. */
+radar_status radar_rotary_axes(const radar_rope* rope, int32_t n_axes,
+                               const int32_t* axis, int32_t batch,
+                               int64_t tokens, int32_t head_dim,
+                               radar_dtype dtype, int32_t n_q_heads,
+                               const radar_rows* q, const radar_rows* q_out,
+                               int32_t n_k_heads, const radar_rows* k,
+                               const radar_rows* k_out, const int64_t* pos,
+                               const int64_t* lens, int32_t inverse,
+                               hipStream_t stream);
+
+radar_status radar_rotary_fill_axes(const radar_config* cfg,
+                                    const radar_rope* rope, int32_t n_axes,
+                                    const int32_t* axis, int64_t tokens,
+                                    const radar_rows* q, const radar_rows* q_out,
+                                    const radar_rows* k, const radar_rows* v,
+                                    void* K, void* V, int64_t row0,
+                                    const int64_t* rows, const int64_t* pos,
+                                    const int64_t* lens, hipStream_t stream);
 
 /* ---- attention over a shared prefix --------------------------------------
  * One query per (b, q head) attends the prefix_len rows of the prefix
@@ -153,6 +177,82 @@ radar_status radar_evict(const radar_config* cfg, void* K, void* V, float* mass,
  * kept rows or fewer. */
 size_t radar_evict_workspace_bytes(const radar_config* cfg, int64_t t,
                                    int64_t heavy, int64_t recent);
+
+/* ---- drafted tokens ---------------------------------------------------------
+ * Sequence b has len = lens[b] rows (nullable device int64 [batch], at most t;
+ * else t) and, behind them, the rows len .. len + N_b - 1 of N_b drafted tokens,
+ * its nodes (counts, nullable device int64 [batch], 0 .. nodes; else nodes).
+ * parent names the node that each one follows, always one before it, or -1: it
+ * follows the sequence's last row (device int32, [batch][nodes], or one list
+ * [nodes] for all with parent_shared). parent NULL: a chain, node i follows
+ * node i - 1. */
+#define RADAR_MAX_TREE 512      /* most nodes where a parent list is given */
+
+/* The drafted tokens that the model agrees with: from the sequence's end, where
+ * it chose first[b], to the lowest of the nodes there whose token that is, from a
+ * node i on by choice[b][i] among those that follow it, until none fits (tokens
+ * and choice: device int64 [batch][nodes], first: [batch]). path (device int32
+ * [batch][nodes]) receives the nodes met, -1 behind them, accepted (int64
+ * [batch]) how many, next (int64 [batch]) the last choice, which no node held.
+ * The rows of K and V that the path's nodes have move to len, len + 1, ..; no
+ * other row changes. new_lens (nullable, int64 [batch]) receives len + accepted;
+ * it may be lens itself, and next first. 1 <= nodes <= RADAR_MAX_TREE, else as
+ * above; a sequence with an invalid length or count keeps its rows and gets an
+ * empty path, next -1 and new_lens its lens[b]. A node with an invalid parent is
+ * never met. The summaries of the index are not touched: radar_extend_index
+ * follows. */
+radar_status radar_accept_tree(const radar_config* cfg, void* K, void* V,
+                               int64_t t, const int64_t* lens, int64_t nodes,
+                               const int64_t* counts, const int32_t* parent,
+                               int32_t parent_shared, const int64_t* tokens,
+                               const int64_t* first, const int64_t* choice,
+                               int32_t* path, int64_t* accepted, int64_t* next,
+                               int64_t* new_lens, hipStream_t stream);
+
+/* The same move for a path that the caller chose: rows len + path[b][i], i < n_b,
+ * go to rows len + i (path: device int32 [batch][n], n_b = counts[b] in 0 .. n,
+ * nullable: n). new_lens receives len + n_b and may be lens itself. A sequence
+ * whose entries do not ascend from 0 or more, whose rows pass the capacity or
+ * whose lens[b] or counts[b] is invalid keeps its rows and gets new_lens -1. n >=
+ * 0, 0 <= t <= capacity. */
+radar_status radar_keep_path(const radar_config* cfg, void* K, void* V, int64_t t,
+                             const int64_t* lens, const int32_t* path, int64_t n,
+                             const int64_t* counts, int64_t* new_lens,
+                             hipStream_t stream);
+
+/* The summaries of the segments that rows [t0, t) complete, by the index build's
+ * own code (0 <= t0 <= t <= capacity); with lens0 and lens (both or neither,
+ * device int64 [batch]) rows [lens0[b], lens[b]) of each sequence, at most `most`
+ * of them (those behind are left out; an invalid pair, negative or above t,
+ * completes nothing). Reads the index's fields of the config too. The workspace
+ * is needed with lens only. */
+radar_status radar_extend_index(const radar_config* cfg, const void* K,
+                                const void* omega, int64_t t0, int64_t t,
+                                const int64_t* lens0, const int64_t* lens,
+                                int64_t most, float* summaries, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream);
+
+/* Scratch bytes for every call with this config and at most this `most`. */
+size_t radar_extend_index_workspace_bytes(const radar_config* cfg, int64_t most);
+
+/* ---- forking ------------------------------------------------------------------
+ * Sequence b becomes what sequence src[b] was before the call (device int64
+ * [batch]; any map: copies, swaps, cycles), in place: rows [first, len of src[b])
+ * of K and V, and where they are given the masses [0, len) and the summaries of
+ * the segments that hold rows from `first` on and are full (segments of
+ * cfg->seg_len rows after n_sink, rows of cfg->n_features; these fields are read
+ * with summaries only). Rows below `first` are taken to be the same already.
+ * src[b] = b changes nothing, -1 frees b: its length becomes 0. The masses of a
+ * sequence that was copied to or freed become 0 from its new length to its old.
+ * new_lens (nullable, int64 [batch]) receives the new lengths and may be lens
+ * itself. A src[b] outside [-1, batch) changes nothing of b but its new length,
+ * -1; a src[b] whose length is outside [0, t] gives b that length alone. batch
+ * at most RADAR_MAX_FORK; 0 <= first, 0 <= t <= capacity. */
+#define RADAR_MAX_FORK 2048
+radar_status radar_fork(const radar_config* cfg, void* K, void* V, float* mass,
+                        float* summaries, const int64_t* src, int64_t first,
+                        int64_t t, const int64_t* lens, int64_t* new_lens,
+                        hipStream_t stream);
 
 #ifdef __cplusplus
 }

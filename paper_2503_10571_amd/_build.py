@@ -19,7 +19,7 @@ LIB = os.path.join(HERE, "libradar.so")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ_DIR = os.path.join(HERE, "_build")
 # the cache operators: no kernel of the decode path is compiled from these
-CACHE_UNITS = ("rotary.hip", "prefix.hip", "attend.hip", "evict.hip")
+CACHE_UNITS = ("rotary.hip", "prefix.hip", "attend.hip", "evict.hip", "branch.hip")
 CACHE_HEADERS = ("cache_impl.h", "attend_impl.h", "evict_slices.h")
 FEATURE_COUNTS = (64, 128, 256, 512, 1024, 2048)
 

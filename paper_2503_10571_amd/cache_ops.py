@@ -1,6 +1,7 @@
 """The cache operators beside the decode path (include/radar_cache.h): rotary
 positions, attention over a shared prefix, attention that accumulates the
-rows' weights, eviction by those weights. Like the rest of the binding this
+rows' weights, eviction by those weights, attention of drafted tokens and
+their acceptance, forking of the sequences. Like the rest of the binding this
 only marshals arguments; the package re-exports every public name.
 """
 from __future__ import annotations
@@ -12,7 +13,7 @@ import math
 import torch
 
 from . import (RADAR_BF16, RADAR_F32, Config, RadarError, _cache, _check, _Config,
-               _need, _query, lib)
+               _need, _omega, _query, _summ, lib)
 
 _P = ctypes.c_void_p
 _DTYPES = {torch.float32: RADAR_F32, torch.bfloat16: RADAR_BF16}
@@ -37,6 +38,10 @@ def declare(L) -> None:
                                i32, rowsp, rowsp, i64, _P, i32, _P, i32, _P]
     L.radar_rotary_fill.argtypes = [cfgp, ropep, i64, rowsp, rowsp, rowsp, rowsp, _P, _P,
                                     i64, _P, i64, _P, i32, _P, _P]
+    L.radar_rotary_axes.argtypes = [ropep, i32, _P, i32, i64, i32, ctypes.c_int, i32, rowsp,
+                                    rowsp, i32, rowsp, rowsp, _P, _P, i32, _P]
+    L.radar_rotary_fill_axes.argtypes = [cfgp, ropep, i32, _P, i64, rowsp, rowsp, rowsp, rowsp,
+                                         _P, _P, i64, _P, _P, _P, _P]
     L.radar_attend_prefix.argtypes = [cfgp, _P, _P, _P, i64, i64, _P, _P, i64, _P, _P, _P,
                                       sz, _P]
     L.radar_attend_accumulate.argtypes = [cfgp, _P, _P, _P, _P, i64, _P, _P, _P, sz, _P]
@@ -44,11 +49,19 @@ def declare(L) -> None:
     L.radar_attend_accumulate_workspace_bytes.argtypes = [cfgp, i64]
     L.radar_evict.argtypes = [cfgp, _P, _P, _P, i64, _P, i64, i64, _P, _P, _P, sz, _P]
     L.radar_evict_workspace_bytes.argtypes = [cfgp, i64, i64, i64]
+    L.radar_accept_tree.argtypes = [cfgp, _P, _P, i64, _P, i64, _P, _P, i32, _P, _P, _P, _P, _P,
+                                    _P, _P, _P]
+    L.radar_keep_path.argtypes = [cfgp, _P, _P, i64, _P, _P, i64, _P, _P, _P]
+    L.radar_extend_index.argtypes = [cfgp, _P, _P, i64, i64, _P, _P, i64, _P, _P, sz, _P]
+    L.radar_extend_index_workspace_bytes.argtypes = [cfgp, i64]
+    L.radar_fork.argtypes = [cfgp, _P, _P, _P, _P, _P, i64, i64, _P, _P, _P]
     for fn in ("radar_attend_prefix_workspace_bytes",
-               "radar_attend_accumulate_workspace_bytes", "radar_evict_workspace_bytes"):
+               "radar_attend_accumulate_workspace_bytes", "radar_evict_workspace_bytes",
+               "radar_extend_index_workspace_bytes"):
         getattr(L, fn).restype = sz
-    for fn in ("radar_rotary", "radar_rotary_fill", "radar_attend_prefix",
-               "radar_attend_accumulate", "radar_evict"):
+    for fn in ("radar_rotary", "radar_rotary_fill", "radar_rotary_axes", "radar_rotary_fill_axes",
+               "radar_attend_prefix", "radar_attend_accumulate", "radar_evict",
+               "radar_accept_tree", "radar_keep_path", "radar_extend_index", "radar_fork"):
         getattr(L, fn).restype = ctypes.c_int
 
 
@@ -85,20 +98,26 @@ class Rope:
     """Rotary positions of a head: inv_freq, a device float64 tensor
     [rot_dim / 2] of angles per position (see rope_frequencies); interleaved:
     pairs (2 i, 2 i + 1) instead of (i, i + rot_dim / 2); mscale: a factor on
-    the rotated dims."""
+    the rotated dims. axis: a device int32 tensor [rot_dim / 2], the axis (time,
+    height, width, ..) whose position turns each pair (see rope_axes); positions
+    are then int64 [axes][B][T], and any other kind is the same on every axis."""
     inv_freq: torch.Tensor
     interleaved: bool = False
     mscale: float = 1.0
+    axis: torch.Tensor | None = None
 
     def __post_init__(self):
         _need(self.inv_freq, torch.float64, "inv_freq")
+        if self.axis is not None:
+            _need(self.axis, torch.int32, "axis", self.inv_freq.numel())
+            _one_device(self.inv_freq, self.axis)
         object.__setattr__(self, "_c", _Rope(2 * self.inv_freq.numel(),
                                              1 if self.interleaved else 0, self.mscale,
                                              self.inv_freq.data_ptr()))
 
     # (the same frequencies are the same tensor: two of equal values have no truth value)
     def _key(self):
-        return id(self.inv_freq), self.interleaved, self.mscale
+        return id(self.inv_freq), self.interleaved, self.mscale, id(self.axis)
 
     def __eq__(self, other):
         return self._key() == other._key() if isinstance(other, Rope) else NotImplemented
@@ -107,7 +126,7 @@ class Rope:
         return hash(self._key())
 
     def __reduce__(self):                          # the pointer is not copied
-        return Rope, (self.inv_freq, self.interleaved, self.mscale)
+        return Rope, (self.inv_freq, self.interleaved, self.mscale, self.axis)
 
     @property
     def rot_dim(self) -> int:
@@ -148,6 +167,20 @@ def rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none",
     turns = f * (trained_len / (2 * math.pi))
     keep = ((turns - alpha) / (beta - alpha)).clamp(0.0, 1.0)
     return keep * f + (1 - keep) * f / factor, 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+
+
+def rope_axes(sections, cycled: bool = False) -> torch.Tensor:
+    """The axis of every pair, an int32 CPU tensor: sections[a] pairs turn with
+    axis a. In runs, the first axis first; or, cycled, the axes take turns pair by
+    pair, each until its section is used up."""
+    left = [int(n) for n in sections]
+    if not left or min(left) < 0 or sum(left) < 1:
+        raise ValueError(f"sections must be counts of pairs, got {sections}")
+    if not cycled:
+        out = [a for a, n in enumerate(left) for _ in range(n)]
+    else:
+        out = [a for i in range(max(left)) for a, n in enumerate(left) if i < n]
+    return torch.tensor(out, dtype=torch.int32)
 
 
 def _rows(x, name, dtype):
@@ -199,9 +232,10 @@ def _out_rows(x, out, name, lens):
     return out, _rows(out, name, x.dtype)[0]
 
 
-def _positions(pos, B, T, name="pos"):
+def _positions(pos, B, T, name="pos", rope=None):
     """(first position, device tensor or None, one per token) of an int, an
-    int64 [B] (first tokens) or an int64 [B][T] (each token)."""
+    int64 [B] (first tokens) or an int64 [B][T] (each token); for a rope with
+    axes also an int64 [axes][B][T], with -axes in the last place."""
     if isinstance(pos, int):
         return pos, None, 0
     _need(pos, torch.int64, name)
@@ -209,7 +243,22 @@ def _positions(pos, B, T, name="pos"):
         return 0, pos, 0
     if tuple(pos.shape) == (B, T):
         return 0, pos, 1
+    if rope is not None and rope.axis is not None:
+        if pos.dim() == 3 and tuple(pos.shape[1:]) == (B, T) and pos.shape[0] > 0:
+            return 0, pos, -pos.shape[0]
+        raise ValueError(f"{name} must be an int or int64 [B], [B][T] or [axes][B][T]")
     raise ValueError(f"{name} must be an int, int64 [B] or int64 [B][T]")
+
+
+def _rotate(rope, x, B, T, d, first, second, p0, p, each, lens, inverse):
+    """radar_rotary, or radar_rotary_axes where the positions are of axes."""
+    by, head = ctypes.byref, (B, T, d, _DTYPES[x.dtype], *first, *second)
+    inverse = 1 if inverse else 0
+    if each < 0:
+        _call("radar_rotary_axes", x, by(rope._c), -each, _ptr(rope.axis), *head, _ptr(p),
+              _ptr(lens), inverse)
+    else:
+        _call("radar_rotary", x, by(rope._c), *head, p0, _ptr(p), each, _ptr(lens), inverse)
 
 
 def _lens_of(lens, B):
@@ -251,14 +300,14 @@ class _Rotate(torch.autograd.Function):
         ctx.set_materialize_grads(False)
         ctx.rope, ctx.pos, ctx.inverse = rope, pos, inverse
         # (saved so that a change in place before the backward pass is found)
-        ctx.save_for_backward(rope.inv_freq, lens, None if isinstance(pos, int) else pos)
+        ctx.save_for_backward(rope.inv_freq, lens, None if isinstance(pos, int) else pos, rope.axis)
         if len(xs) == 1:
             return rotary(rope, *xs, pos, inverse=inverse, lens=lens)
         return rotary_qk(rope, *xs, pos, inverse=inverse, lens=lens)
 
     @staticmethod
     def backward(ctx, *grads):
-        _, lens, pos = ctx.saved_tensors
+        _, lens, pos, _ = ctx.saved_tensors
         kw = dict(pos=ctx.pos if pos is None else pos, inverse=not ctx.inverse, lens=lens)
         want = [g if need else None for g, need in zip(grads, ctx.needs_input_grad[4:])]
         # gradients of any layout; the kernel takes dense rows on 16 bytes
@@ -274,7 +323,8 @@ class _Rotate(torch.autograd.Function):
 def rotary(rope: Rope, x, pos, out=None, inverse: bool = False, lens=None):
     """radar_rotary of one tensor x, [B][T][heads][d] or [B][heads][d] (one
     token), strided as it comes out of a projection. pos: the position of the
-    first token (an int, or an int64 [B]) or of every token (int64 [B][T]).
+    first token (an int, or an int64 [B]) or of every token (int64 [B][T]), or
+    for a rope with axes every token's on each of them (int64 [axes][B][T]).
     out may be x. inverse: the gradient of the rotation. lens (int64 [B]): only
     tokens t < lens[b] are touched (the others are 0 in a new out). Autograd
     differentiates it in x, where out is not given. Returns out."""
@@ -285,13 +335,12 @@ def rotary(rope: Rope, x, pos, out=None, inverse: bool = False, lens=None):
         return _Rotate.apply(rope, pos, inverse, lens, x)
     rx, B, T, H, d = _rows(x, "x", x.dtype)
     out, ro = _out_rows(x, out, "out", lens)
-    p0, p, each = _positions(pos, B, T)
+    p0, p, each = _positions(pos, B, T, rope=rope)
     lens = _lens_of(lens, B)
     _one_device(x, p, lens, rope.inv_freq)
     if x.numel():
         by = ctypes.byref
-        _call("radar_rotary", x, by(rope._c), B, T, d, _DTYPES[x.dtype], H, by(rx), by(ro),
-              0, None, None, p0, _ptr(p), each, _ptr(lens), 1 if inverse else 0)
+        _rotate(rope, x, B, T, d, (H, by(rx), by(ro)), (0, None, None), p0, p, each, lens, inverse)
     return out
 
 
@@ -310,7 +359,7 @@ def rotary_qk(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = Fal
         raise ValueError("q and k must agree in batch, tokens and head_dim")
     q_out, qo = _out_rows(q, q_out, "q_out", lens)
     k_out, ko = _out_rows(k, k_out, "k_out", lens)
-    p0, p, each = _positions(pos, B, T)
+    p0, p, each = _positions(pos, B, T, rope=rope)
     lens = _lens_of(lens, B)
     _one_device(q, k, p, lens, rope.inv_freq)
     if B * T * d and (Hq or Hk):
@@ -320,8 +369,7 @@ def rotary_qk(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = Fal
             first, second = second, first
         if not second[0]:
             second = (0, None, None)
-        _call("radar_rotary", q, by(rope._c), B, T, d, _DTYPES[q.dtype], *first, *second,
-              p0, _ptr(p), each, _ptr(lens), 1 if inverse else 0)
+        _rotate(rope, q, B, T, d, first, second, p0, p, each, lens, inverse)
     return q_out, k_out
 
 
@@ -353,10 +401,13 @@ def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_ou
     r0, rows, each = _positions(row, B, T, "row")
     if each:
         raise ValueError("row must be an int or int64 [B]")
-    p0, p, each = (r0, rows, 0) if pos is None else _positions(pos, B, T)
+    p0, p, each = (r0, rows, 0) if pos is None else _positions(pos, B, T, rope=rope)
     lens = _lens_of(lens, B)
     _one_device(k, v, q, rows, p, lens, rope.inv_freq, K, V)
-    if T:
+    if T and each < 0:
+        _call("radar_rotary_fill_axes", k, by(cfg.c_struct()), by(rope._c), -each, _ptr(rope.axis),
+              T, rq, qo, by(rk), by(rv), _ptr(K), _ptr(V), r0, _ptr(rows), _ptr(p), _ptr(lens))
+    elif T:
         _call("radar_rotary_fill", k, by(cfg.c_struct()), by(rope._c), T, rq, qo, by(rk), by(rv),
               _ptr(K), _ptr(V), r0, _ptr(rows), p0, _ptr(p), each, _ptr(lens))
     return q_out
@@ -486,3 +537,129 @@ def evict(cfg: Config, K, V, mass, t: int, heavy: int, recent: int, lens=None,
     _call("radar_evict", mass, c, _ptr(K), _ptr(V), _ptr(mass), t, _ptr(lens), heavy, recent,
           _ptr(new_lens), _ptr(kept), _ptr(workspace), size)
     return n
+
+
+# ---- drafted tokens -----------------------------------------------------------------
+def _nodes(cfg, parent, counts, N):
+    """(parent, one list for the batch, counts) of N drafted tokens."""
+    shared = 0
+    if parent is not None:
+        _need(parent, torch.int32, "parent")
+        shared = 1 if parent.dim() == 1 else 0
+        if tuple(parent.shape) not in ((N,), (cfg.batch, N)):
+            raise ValueError(f"parent must be [{N}] or [{cfg.batch}][{N}], got {list(parent.shape)}")
+    if counts is not None:
+        _need(counts, torch.int64, "counts", cfg.batch)
+    return parent, shared, counts
+
+
+def _given_or_new(x, name, dtype, shape, device):
+    if x is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    _need(x, dtype, name, math.prod(shape))
+    return x
+
+
+def accept_tree(cfg: Config, K, V, t: int, tokens, first, choice, parent=None, counts=None,
+                lens=None, new_lens=None, path=None, accepted=None, next_token=None):
+    """radar_accept_tree: of N drafted tokens behind every sequence (tokens int64
+    [B][N], their rows t .. t + N - 1 of K and V, or lens[b] ..) the path that the
+    model agrees with: first (int64 [B]) is what it chose after the sequence,
+    choice (int64 [B][N]) what after each node. parent (int32 [N] for all, or
+    [B][N]; None: a chain) and counts (int64 [B]) as for attend_tree(). The rows
+    of the path move up to the sequence's end; new_lens (int64 [B], may be lens)
+    receives the new lengths. Returns (path int32 [B][N], -1 behind its nodes;
+    how many int64 [B]; the model's next token int64 [B]). The summaries do not
+    follow: extend_index()."""
+    _cache(cfg, K, V)
+    if tokens.dim() != 2 or tokens.shape[0] != cfg.batch:
+        raise ValueError(f"tokens must be [{cfg.batch}][nodes], got {list(tokens.shape)}")
+    B, N = tokens.shape
+    _need(tokens, torch.int64, "tokens")
+    _need(first, torch.int64, "first", B)
+    _need(choice, torch.int64, "choice", B * N)
+    parent, shared, counts = _nodes(cfg, parent, counts, N)
+    lens = _lens_of(lens, B)
+    if new_lens is not None:
+        _need(new_lens, torch.int64, "new_lens", B)
+    dev = tokens.device
+    path = _given_or_new(path, "path", torch.int32, (B, N), dev)
+    accepted = _given_or_new(accepted, "accepted", torch.int64, (B,), dev)
+    next_token = _given_or_new(next_token, "next_token", torch.int64, (B,), dev)
+    _one_device(tokens, first, choice, parent, counts, lens, new_lens, path, accepted, next_token,
+                K, V)
+    _call("radar_accept_tree", tokens, ctypes.byref(cfg.c_struct()), _ptr(K), _ptr(V), t, _ptr(lens),
+          N, _ptr(counts), _ptr(parent), shared, _ptr(tokens), _ptr(first), _ptr(choice), _ptr(path),
+          _ptr(accepted), _ptr(next_token), _ptr(new_lens))
+    return path, accepted, next_token
+
+
+def keep_path(cfg: Config, K, V, t: int, path, counts=None, lens=None, new_lens=None) -> None:
+    """radar_keep_path: the rows t + path[b][i] (or lens[b] + ..) of K and V move
+    to t + i (path: int32 [B][n], ascending from 0 or more; counts int64 [B]: how
+    many of them). new_lens (int64 [B], may be lens) receives the new lengths, -1
+    for a sequence whose path was refused."""
+    _cache(cfg, K, V)
+    _need(path, torch.int32, "path")
+    if path.dim() != 2 or path.shape[0] != cfg.batch:
+        raise ValueError(f"path must be [{cfg.batch}][n], got {list(path.shape)}")
+    lens = _lens_of(lens, cfg.batch)
+    for x, name in ((counts, "counts"), (new_lens, "new_lens")):
+        if x is not None:
+            _need(x, torch.int64, name, cfg.batch)
+    _one_device(path, counts, lens, new_lens, K, V)
+    _call("radar_keep_path", path, ctypes.byref(cfg.c_struct()), _ptr(K), _ptr(V), t, _ptr(lens),
+          _ptr(path), path.shape[1], _ptr(counts), _ptr(new_lens))
+
+
+def extend_index_workspace_bytes(cfg: Config, most: int) -> int:
+    """Scratch for every call with this config and at most this `most`."""
+    return int(lib().radar_extend_index_workspace_bytes(ctypes.byref(cfg.c_struct()), most))
+
+
+def extend_index(cfg: Config, K, omega, t0: int, t: int, summaries, lens0=None, lens=None,
+                 most: int | None = None, workspace=None) -> None:
+    """radar_extend_index: the summaries of the segments that rows [t0, t) of K
+    complete; or, with lens0 and lens (int64 [B], at most t), rows [lens0[b],
+    lens[b]) of every sequence, of which there are `most` at most (t - t0 if
+    None)."""
+    _cache(cfg, K)
+    _omega(cfg, omega)
+    _summ(cfg, summaries)
+    if (lens0 is None) != (lens is None):
+        raise ValueError("lens0 and lens come together")
+    if lens is not None:
+        _need(lens0, torch.int64, "lens0", cfg.batch)
+        _need(lens, torch.int64, "lens", cfg.batch)
+    _one_device(summaries, K, omega, lens0, lens, workspace)
+    c, n = ctypes.byref(cfg.c_struct()), 0
+    if most is None:
+        most = t - t0
+    if lens is not None:
+        need = lib().radar_extend_index_workspace_bytes(c, most) if workspace is None else 0
+        workspace, n = _workspace(workspace, need, summaries.device)
+    _call("radar_extend_index", summaries, c, _ptr(K), _ptr(omega), t0, t, _ptr(lens0), _ptr(lens),
+          most, _ptr(summaries), _ptr(workspace), n)
+
+
+# ---- forking ------------------------------------------------------------------------
+def fork(cfg: Config, K, V, src, t: int, first: int = 0, lens=None, new_lens=None, mass=None,
+         summaries=None) -> None:
+    """radar_fork: sequence b becomes what sequence src[b] (int64 [B]) was, in
+    place, for any map: one prompt's rows for many samples, beams, the places of
+    ended sequences taken by others; -1 frees a place. Rows below `first` are
+    taken to be the same already. new_lens (int64 [B], may be lens) receives the
+    new lengths, 0 of a freed place. mass and summaries move along where they are
+    given."""
+    _cache(cfg, K, V)
+    _need(src, torch.int64, "src", cfg.batch)
+    lens = _lens_of(lens, cfg.batch)
+    if new_lens is not None:
+        _need(new_lens, torch.int64, "new_lens", cfg.batch)
+    if mass is not None:
+        _mass(cfg, mass)
+    if summaries is not None:
+        _summ(cfg, summaries)
+    _one_device(src, K, V, lens, new_lens, mass, summaries)
+    _call("radar_fork", src, ctypes.byref(cfg.c_struct()), _ptr(K), _ptr(V), _ptr(mass),
+          _ptr(summaries), _ptr(src), first, t, _ptr(lens), _ptr(new_lens))

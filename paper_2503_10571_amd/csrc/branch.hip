@@ -1,0 +1,503 @@
+// What moves rows when a sequence branches (include/radar_cache.h): the
+// acceptance of a path of drafted tokens, the index of the rows it added, and the
+// forking of the cache's sequences.
+#include "cache_impl.h"
+
+namespace radar_impl {
+namespace {
+
+constexpr int kMaxTree = RADAR_MAX_TREE;
+
+struct PathArgs {
+  unsigned char *K, *V;
+  const int64_t *lens, *counts;
+  int64_t t, cap, nodes;   // keep: nodes is the row length of path
+  int Hkv, row_bytes;
+  const int* parent;
+  int parent_shared;
+  const int64_t *tokens, *first, *choice;
+  const int* given;        // keep: the path
+  int* path;
+  int64_t *accepted, *next, *new_lens;
+};
+
+// Rows len + path(i) of a sequence's heads to len + i, i < n, in place: path(i) >= i
+// ascends, so rows read later are not among those written, and of kRows rows at a time
+// all are read before one is written. A wave per head; a row's 16-byte chunks on the
+// lanes.
+template <typename PathOf>
+__device__ __forceinline__ void move_rows(const PathArgs& a, int64_t b, int64_t len, int n,
+                                          PathOf&& path) {
+  constexpr int kPasses = 4;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int per = a.row_bytes / 16, rows = kWave / per;
+  const int r = lane / per, c = lane % per;
+  for (int h = wave; h < a.Hkv; h += waves) {
+    const int64_t at = ((b * a.Hkv + h) * a.cap + len) * a.row_bytes + c * 16;
+    for (int i0 = 0; i0 < n; i0 += kPasses * rows) {
+      uint4 k[kPasses], v[kPasses];
+      int from[kPasses];
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        const int i = i0 + p * rows + r;
+        from[p] = i < n ? path(i) : i;
+        if (from[p] != i) {                // (a row that stays is not written)
+          k[p] = *reinterpret_cast<const uint4*>(a.K + at + (int64_t)from[p] * a.row_bytes);
+          v[p] = *reinterpret_cast<const uint4*>(a.V + at + (int64_t)from[p] * a.row_bytes);
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < kPasses; ++p) {
+        const int i = i0 + p * rows + r;
+        if (from[p] != i) {
+          *reinterpret_cast<uint4*>(a.K + at + (int64_t)i * a.row_bytes) = k[p];
+          *reinterpret_cast<uint4*>(a.V + at + (int64_t)i * a.row_bytes) = v[p];
+        }
+      }
+    }
+  }
+}
+
+// A workgroup per sequence. Its first wave holds the nodes, U to a lane, and walks
+// down: of the nodes behind the current one whose parent it is and whose token is the
+// one wanted, the lowest, by a ballot for each 64 (a step is some 100 cycles; the
+// loads, all at once, are most of the kernel's time). All waves then move the rows.
+// The sequence's length is read by the first wave only and before anything is
+// written, so that the new length may take its place.
+template <int U>
+__global__ __launch_bounds__(1024) void k_accept(PathArgs a) {
+  __shared__ int path[kMaxTree];
+  __shared__ int64_t at;
+  __shared__ int n_path;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t b = blockIdx.x;
+  if (tid < kWave) {
+    const int64_t len = a.lens ? a.lens[b] : a.t;
+    const int64_t cnt = a.counts ? a.counts[b] : a.nodes;
+    const bool ok = len >= 0 && len <= a.t && cnt >= 0 && cnt <= a.nodes && len + cnt <= a.cap;
+    const int nodes = ok ? (int)cnt : 0;
+    int par[U];
+    int64_t tok[U], pick[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = u * kWave + lane;
+      par[u] = -2;                         // no node's
+      tok[u] = pick[u] = 0;
+      if (i < nodes) {
+        par[u] = a.parent ? a.parent[(a.parent_shared ? 0 : b * a.nodes) + i] : i - 1;
+        tok[u] = a.tokens[b * a.nodes + i];
+        pick[u] = a.choice[b * a.nodes + i];
+      }
+    }
+    int64_t want = a.first[b];
+    int cur = -1, n = 0;
+    for (;;) {                             // cur ascends
+      int hit = -1;
+      int64_t then = 0;
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        if (hit >= 0) continue;            // uniform
+        const int i = u * kWave + lane;
+        const u64 fits = __ballot(par[u] == cur && i > cur && tok[u] == want);
+        if (fits) {
+          const int l = __ffsll(fits) - 1;
+          hit = u * kWave + l;
+          const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)(u64)pick[u], l);
+          const uint32_t hi = __builtin_amdgcn_readlane((int)(uint32_t)((u64)pick[u] >> 32), l);
+          then = (int64_t)(((u64)hi << 32) | lo);
+        }
+      }
+      if (hit < 0) break;
+      if (lane == 0) path[n] = hit;
+      ++n;
+      cur = hit;
+      want = then;
+    }
+    if (lane == 0) {
+      at = ok ? len : -1;
+      n_path = n;
+      a.accepted[b] = n;
+      a.next[b] = ok ? want : -1;
+      if (a.new_lens) a.new_lens[b] = len + n;
+    }
+  }
+  __syncthreads();
+  const int n = n_path;
+  for (int i = tid; i < a.nodes; i += blockDim.x) a.path[b * a.nodes + i] = i < n ? path[i] : -1;
+  move_rows(a, b, at, n, [&](int i) { return path[i]; });
+}
+
+// The same move along a given path: the first wave looks it over.
+__global__ __launch_bounds__(1024) void k_keep(PathArgs a) {
+  __shared__ int64_t at;
+  __shared__ int n_path;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int64_t b = blockIdx.x;
+  const int* given = a.given + b * a.nodes;
+  if (tid < kWave) {
+    const int64_t len = a.lens ? a.lens[b] : a.t;
+    const int64_t cnt = a.counts ? a.counts[b] : a.nodes;
+    bool ok = len >= 0 && len <= a.t && cnt >= 0 && cnt <= a.nodes;
+    const int n = ok ? (int)cnt : 0;
+    for (int i = lane; i < n; i += kWave) {
+      const int x = given[i];
+      if (x <= (i ? given[i - 1] : -1) || len + x >= a.cap) ok = false;
+    }
+    ok = __all(ok);
+    if (lane == 0) {
+      at = len;
+      n_path = ok ? n : 0;
+      if (a.new_lens) a.new_lens[b] = ok ? len + n : -1;
+    }
+  }
+  __syncthreads();
+  move_rows(a, b, at, n_path, [&](int i) { return given[i]; });
+}
+
+// Row j of pos: each sequence's j-th row of [lens0, lens) that ends a segment, -1 if
+// there is none.
+__global__ __launch_bounds__(256) void k_closings(const int64_t* lens0, const int64_t* lens, int64_t t,
+                                                  int64_t most, int B, int c, int n_sink, int n,
+                                                  int64_t* pos) {
+  const int b = blockIdx.x * 256 + threadIdx.x;
+  if (b >= B) return;
+  const int64_t from = lens0[b], len = lens[b];
+  const bool ok = from >= 0 && from <= len && len <= t;
+  const int64_t end = min(len, from + most), x = max(from - n_sink, (int64_t)0);
+  int64_t row = n_sink + (x / c + 1) * c - 1;
+  for (int j = 0; j < n; ++j, row += c) pos[(int64_t)j * B + b] = ok && row < end ? row : -1;
+}
+
+// ---------------------------------------------------------------------------
+// forking
+// ---------------------------------------------------------------------------
+struct ForkArgs {
+  unsigned char *K, *V, *mass, *summ;
+  const int64_t *src, *lens;
+  int64_t* new_lens;       // written here, unless it is lens
+  int B, Hkv;
+  int64_t t, first, cap;
+  int row_bytes;
+  int c, n_sink, summ_bytes;         // of a summary
+  int64_t summ_rows;
+  int64_t tiles[3];        // of K (and V), masses and summaries, per head
+};
+
+__device__ __forceinline__ int64_t fork_len(const ForkArgs& a, int64_t s) {
+  return s == -1 ? 0 : s < -1 || s >= a.B ? -1 : a.lens ? a.lens[s] : a.t;
+}
+
+// A workgroup moves the same 16 bytes of a head's rows in every sequence, so no other
+// one meets the bytes that it overwrites, and the map needs an order within it only.
+// Each workgroup makes the list of the moves once: those whose destination no move
+// still has to read come first, then those that this sets free, and so on; what is
+// left are cycles, whose first sequence is saved. kBatch moves at a time are read
+// before they are written, which any order of reads ahead allows; moves from one
+// sequence that follow one another read it once.
+constexpr int kBatch = 16, kForkTile = 256;
+constexpr uint32_t kNone = 0xffffu, kZero = 0xfffeu;   // as a source: saved one, zeros
+static_assert(RADAR_MAX_FORK < kZero, "sequences in 16 bits");
+constexpr int kStay = -1, kFreed = -2;
+
+template <typename V>
+__device__ __forceinline__ V zeros() { return V{}; }
+
+// MASS: behind the source's length zeros, up to the destination's
+template <typename V, bool MASS, typename Units>
+__device__ __forceinline__ void fork_column(unsigned char* base, int64_t stride, int64_t x,
+                                            const uint32_t* list, int n, const int* len,
+                                            Units&& units) {
+  V saved = zeros<V>();
+  int64_t saved_units = 0;
+  for (int e0 = 0; e0 < n; e0 += kBatch) {
+    V v[kBatch];
+    uint32_t before = kNone;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      v[j] = zeros<V>();
+      if (e0 + j >= n) continue;           // uniform
+      const uint32_t s = __builtin_amdgcn_readfirstlane(list[e0 + j]) & 0xffffu;
+      const bool again = j > 0 && s == before;
+      before = s;
+      if (s == kNone || s == kZero) continue;
+      if (again)
+        v[j] = v[j > 0 ? j - 1 : 0];
+      else if (x < units(len[s]))
+        v[j] = *reinterpret_cast<const V*>(base + s * stride + x * (int64_t)sizeof(V));
+    }
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) {
+      if (e0 + j >= n) continue;
+      const uint32_t e = __builtin_amdgcn_readfirstlane(list[e0 + j]);
+      const uint32_t s = e & 0xffffu, dst = e >> 16;
+      int64_t have = s == kNone ? saved_units : s == kZero ? 0 : units(len[s]);
+      if (dst == kNone) {
+        saved = v[j];
+        saved_units = have;
+        continue;
+      }
+      if (MASS) have = max(have, units(len[dst]));
+      if (x < have)
+        *reinterpret_cast<V*>(base + dst * stride + x * (int64_t)sizeof(V)) = s == kNone ? saved : v[j];
+    }
+  }
+}
+
+__global__ __launch_bounds__(kForkTile) void k_fork(ForkArgs a) {
+  extern __shared__ int fork_lds[];
+  int* src = fork_lds;                     // or kStay, kFreed
+  int* left = src + a.B;                   // moves that still read it; -1: listed
+  int* len = left + a.B;
+  uint32_t* list = reinterpret_cast<uint32_t*>(len + a.B);   // dst << 16 | src
+  __shared__ int n_list;
+  const int tid = threadIdx.x;
+  for (int b = tid; b < a.B; b += kForkTile) {
+    const int64_t n = a.lens ? a.lens[b] : a.t;
+    len[b] = n >= 0 && n <= a.t ? (int)n : -1;
+    left[b] = 0;
+  }
+  if (tid == 0) n_list = 0;
+  __syncthreads();
+  for (int b = tid; b < a.B; b += kForkTile) {
+    const int64_t s = a.src[b];
+    const bool moves = s >= 0 && s < a.B && s != b && len[s] >= 0;
+    src[b] = moves ? (int)s : s == -1 ? kFreed : kStay;
+    if (moves) atomicAdd(&left[s], 1);
+    if (a.new_lens && blockIdx.x == 0) a.new_lens[b] = fork_len(a, s);
+  }
+  // (a move takes its place in the list before it frees its source for others)
+  for (bool more = true; more;) {
+    __syncthreads();
+    bool any = false;
+    for (int b = tid; b < a.B; b += kForkTile) {
+      if (src[b] == kStay || __atomic_load_n(&left[b], __ATOMIC_RELAXED) != 0) continue;
+      const uint32_t s = src[b] == kFreed ? kZero : (uint32_t)src[b];
+      list[atomicAdd(&n_list, 1)] = (uint32_t)b << 16 | s;
+      __threadfence_block();
+      left[b] = -1;
+      if (src[b] >= 0) atomicSub(&left[src[b]], 1);
+      any = true;
+    }
+    more = __syncthreads_or(any);
+  }
+  // cycles: the lowest sequence of each writes it down
+  for (int b = tid; b < a.B; b += kForkTile) {
+    if (src[b] == kStay || left[b] < 0) continue;
+    int size = 1, low = b;
+    for (int x = src[b]; x != b; x = src[x]) {
+      low = min(low, x);
+      ++size;
+    }
+    if (low != b) continue;
+    uint32_t* out = list + atomicAdd(&n_list, size + 1);
+    *out++ = kNone << 16 | (uint32_t)b;
+    int x = b;
+    for (; src[x] != b; x = src[x]) *out++ = (uint32_t)x << 16 | (uint32_t)src[x];
+    *out = (uint32_t)x << 16 | kNone;
+  }
+  __syncthreads();
+  const int n = n_list;
+  if (n == 0) return;
+  const int64_t kv_tiles = 2 * a.Hkv * a.tiles[0], mass_tiles = a.Hkv * a.tiles[1];
+  const int64_t all = kv_tiles + mass_tiles + a.Hkv * a.tiles[2];
+  const int per = a.row_bytes / 16;
+  const int64_t seg0 = max((int64_t)0, a.first - a.n_sink) / max(a.c, 1);
+  for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
+    if (i < kv_tiles) {
+      const int64_t h = i / a.tiles[0] >> 1, x = i % a.tiles[0] * kForkTile + tid;
+      unsigned char* base = (i / a.tiles[0] & 1 ? a.V : a.K) + (h * a.cap + a.first) * a.row_bytes;
+      fork_column<uint4, false>(base, a.Hkv * a.cap * a.row_bytes, x, list, n, len, [&](int m) {
+        return max((int64_t)0, m - a.first) * per;
+      });
+    } else if (i < kv_tiles + mass_tiles) {
+      const int64_t k = i - kv_tiles, h = k / a.tiles[1], x = k % a.tiles[1] * kForkTile + tid;
+      fork_column<uint32_t, true>(a.mass + h * a.cap * 4, a.Hkv * a.cap * 4, x, list, n, len,
+                                  [](int m) { return (int64_t)m; });
+    } else {
+      const int64_t k = i - kv_tiles - mass_tiles, h = k / a.tiles[2];
+      const int64_t x = k % a.tiles[2] * kForkTile + tid;
+      fork_column<uint4, false>(a.summ + (h * a.summ_rows + seg0) * a.summ_bytes,
+                                a.Hkv * a.summ_rows * a.summ_bytes, x, list, n, len, [&](int m) {
+        return max((int64_t)0, max(m - a.n_sink, 0) / a.c - seg0) * (a.summ_bytes / 16);
+      });
+    }
+  }
+}
+
+// the new lengths in the place of the old ones, once no workgroup reads those
+__global__ __launch_bounds__(1024) void k_fork_lens(ForkArgs a) {
+  constexpr int kPer = RADAR_MAX_FORK / 1024;
+  int64_t n[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int b = i * 1024 + threadIdx.x;
+    n[i] = b < a.B ? fork_len(a, a.src[b]) : 0;
+  }
+  __builtin_amdgcn_s_waitcnt(0);           // every load of this wave has returned
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kPer; ++i) {
+    const int b = i * 1024 + threadIdx.x;
+    if (b < a.B) a.new_lens[b] = n[i];
+  }
+}
+
+bool bad16(const void* p) { return !p || !aligned16(p); }
+bool odd16(const void* p) { return p && !aligned16(p); }
+int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
+
+// the index's fields of the config, with radar.h's limits
+radar_status check_index(const radar_config* cfg, Shape* s) {
+  const radar_status r = check_cache(cfg, s);
+  if (r != RADAR_OK) return r;
+  const int n = cfg->n_features;
+  if (cfg->seg_len < 1) return RADAR_EINVAL;
+  if (n != 64 && n != 128 && n != 256 && n != 512 && n != 1024 && n != 2048) return RADAR_EUNSUPPORTED;
+  s->n = n; s->c = cfg->seg_len; s->s_cap = cfg->capacity / cfg->seg_len;
+  return RADAR_OK;
+}
+
+PathArgs path_args(const Shape& s, void* K, void* V, int64_t t, const int64_t* lens, int64_t nodes,
+                   const int64_t* counts, int64_t* new_lens) {
+  PathArgs a{};
+  a.K = static_cast<unsigned char*>(K); a.V = static_cast<unsigned char*>(V);
+  a.lens = lens; a.counts = counts; a.t = t; a.cap = s.cap; a.nodes = nodes;
+  a.Hkv = s.Hkv; a.row_bytes = s.d * esize(s);
+  a.new_lens = new_lens;
+  return a;
+}
+
+int path_threads(const Shape& s) { return kWave * std::min(16, s.Hkv); }
+
+int64_t closings(const Shape& s, int64_t most) { return ceil_div(most, s.c); }
+int64_t closings_bytes(const Shape& s, int64_t most) {
+  return (int64_t)align256((size_t)(closings(s, most) * s.B * 8));
+}
+
+}  // namespace
+}  // namespace radar_impl
+
+using namespace radar_impl;
+
+extern "C" {
+
+radar_status radar_accept_tree(const radar_config* cfg, void* K, void* V, int64_t t,
+                               const int64_t* lens, int64_t nodes, const int64_t* counts,
+                               const int32_t* parent, int32_t parent_shared,
+                               const int64_t* tokens, const int64_t* first, const int64_t* choice,
+                               int32_t* path, int64_t* accepted, int64_t* next, int64_t* new_lens,
+                               hipStream_t stream) {
+  Shape s;
+  const radar_status r = check_cache(cfg, &s);
+  if (r != RADAR_OK) return r;
+  if (bad16(K) || bad16(V) || bad16(tokens) || bad16(first) || bad16(choice) || bad16(path) ||
+      bad16(accepted) || bad16(next) || odd16(lens) || odd16(counts) || odd16(parent) ||
+      odd16(new_lens) || nodes < 1)
+    return RADAR_EINVAL;
+  if (nodes > kMaxTree) return RADAR_EUNSUPPORTED;
+  if (t < 0 || t > s.cap || (!lens && nodes > s.cap - t)) return RADAR_ECAPACITY;
+  PathArgs a = path_args(s, K, V, t, lens, nodes, counts, new_lens);
+  a.parent = parent; a.parent_shared = parent_shared != 0;
+  a.tokens = tokens; a.first = first; a.choice = choice;
+  a.path = path; a.accepted = accepted; a.next = next;
+  const dim3 grid((unsigned)s.B), block((unsigned)path_threads(s));
+  if (nodes <= kWave) launch(RADAR_K_APPEND, k_accept<1>, grid, block, 0, stream, a);
+  else launch(RADAR_K_APPEND, k_accept<kMaxTree / kWave>, grid, block, 0, stream, a);
+  return launch_status();
+}
+
+radar_status radar_keep_path(const radar_config* cfg, void* K, void* V, int64_t t,
+                             const int64_t* lens, const int32_t* path, int64_t n,
+                             const int64_t* counts, int64_t* new_lens, hipStream_t stream) {
+  Shape s;
+  const radar_status r = check_cache(cfg, &s);
+  if (r != RADAR_OK) return r;
+  if (bad16(K) || bad16(V) || n < 0 || (n > 0 && bad16(path)) || odd16(lens) || odd16(counts) ||
+      odd16(new_lens))
+    return RADAR_EINVAL;
+  if (t < 0 || t > s.cap || n > s.cap) return RADAR_ECAPACITY;
+  PathArgs a = path_args(s, K, V, t, lens, n, counts, new_lens);
+  a.given = path;
+  launch(RADAR_K_APPEND, k_keep, dim3((unsigned)s.B), dim3((unsigned)path_threads(s)), 0, stream, a);
+  return launch_status();
+}
+
+size_t radar_extend_index_workspace_bytes(const radar_config* cfg, int64_t most) {
+  Shape s;
+  if (check_index(cfg, &s) != RADAR_OK || most < 0 || most > s.cap) return 0;
+  return (size_t)std::max<int64_t>(256, closings_bytes(s, most));
+}
+
+radar_status radar_extend_index(const radar_config* cfg, const void* K, const void* omega,
+                                int64_t t0, int64_t t, const int64_t* lens0, const int64_t* lens,
+                                int64_t most, float* summaries, void* workspace,
+                                size_t workspace_bytes, hipStream_t stream) {
+  Shape s;
+  radar_status r = check_index(cfg, &s);
+  if (r != RADAR_OK) return r;
+  if (cfg->omega_dtype != RADAR_F32 && cfg->omega_dtype != RADAR_BF16) return RADAR_EINVAL;
+  if (cfg->omega_dtype == RADAR_BF16 && cfg->kv_dtype != RADAR_BF16) return RADAR_EINVAL;
+  s.obf = cfg->omega_dtype == RADAR_BF16;
+  if (bad16(K) || bad16(omega) || bad16(summaries) || odd16(lens0) || odd16(lens) || !lens0 != !lens)
+    return RADAR_EINVAL;
+  if (t < 0 || t > s.cap) return RADAR_ECAPACITY;
+  if (!lens) {
+    if (t0 < 0 || t0 > t) return RADAR_ECAPACITY;
+    const int64_t s0 = std::max<int64_t>(0, t0 - s.n_sink) / s.c;
+    const int64_t s1 = std::max<int64_t>(0, t - s.n_sink) / s.c;
+    if (s1 == s0) return RADAR_OK;
+    return launch_build(s, after_sinks(s, K), omega, summaries, (int)s0, (int)(s1 - s0), nullptr, stream);
+  }
+  if (most < 0 || most > s.cap) return RADAR_ECAPACITY;
+  if (bad16(workspace) || workspace_bytes < (size_t)std::max<int64_t>(256, closings_bytes(s, most)))
+    return RADAR_EWORKSPACE;
+  const int n = (int)closings(s, most);
+  if (n == 0) return RADAR_OK;
+  int64_t* pos = static_cast<int64_t*>(workspace);
+  launch(RADAR_K_BUILD, k_closings, dim3((unsigned)ceil_div(s.B, 256)), dim3(256), 0, stream, lens0, lens, t,
+         most, s.B, s.c, s.n_sink, n, pos);
+  r = launch_status();
+  for (int j = 0; j < n && r == RADAR_OK; ++j)
+    r = launch_build(s, after_sinks(s, K), omega, summaries, 0, 1, pos + (int64_t)j * s.B, stream);
+  return r;
+}
+
+radar_status radar_fork(const radar_config* cfg, void* K, void* V, float* mass, float* summaries,
+                        const int64_t* src, int64_t first, int64_t t, const int64_t* lens,
+                        int64_t* new_lens, hipStream_t stream) {
+  Shape s;
+  const radar_status r = summaries ? check_index(cfg, &s) : check_cache(cfg, &s);
+  if (r != RADAR_OK) return r;
+  if (bad16(K) || bad16(V) || odd16(mass) || odd16(summaries) || bad16(src) || odd16(lens) ||
+      odd16(new_lens) || src == new_lens || first < 0)
+    return RADAR_EINVAL;
+  if (t < 0 || t > s.cap) return RADAR_ECAPACITY;
+  if (s.B > RADAR_MAX_FORK) return RADAR_EUNSUPPORTED;
+  const bool in_place = new_lens && new_lens == lens;
+  ForkArgs a{};
+  a.K = static_cast<unsigned char*>(K); a.V = static_cast<unsigned char*>(V);
+  a.mass = reinterpret_cast<unsigned char*>(mass); a.summ = reinterpret_cast<unsigned char*>(summaries);
+  a.src = src; a.lens = lens; a.new_lens = in_place ? nullptr : new_lens;
+  a.B = s.B; a.Hkv = s.Hkv; a.t = t; a.first = std::min(first, t); a.cap = s.cap;
+  a.row_bytes = s.d * esize(s);
+  a.n_sink = s.n_sink;
+  a.tiles[0] = std::max<int64_t>(1, ceil_div((t - a.first) * (a.row_bytes / 16), kForkTile));
+  if (mass) a.tiles[1] = ceil_div(t, kForkTile);
+  if (summaries) {
+    a.c = s.c; a.summ_bytes = s.n * 4; a.summ_rows = std::max<int64_t>(1, s.s_cap);
+    const int64_t seg0 = std::max<int64_t>(0, a.first - s.n_sink) / s.c;
+    const int64_t seg1 = std::max<int64_t>(0, t - s.n_sink) / s.c;
+    a.tiles[2] = ceil_div((seg1 - seg0) * (a.summ_bytes / 16), kForkTile);
+  }
+  const int64_t items = s.Hkv * (2 * a.tiles[0] + a.tiles[1] + a.tiles[2]);
+  const size_t lds = (size_t)s.B * 18;     // three words a sequence, and up to 3/2 in the list
+  const unsigned grid = (unsigned)std::min<int64_t>(items, 8 * num_cu());
+  launch(RADAR_K_APPEND, k_fork, dim3(grid), dim3(kForkTile), (lds + 15) / 16 * 16, stream, a);
+  const radar_status st = launch_status();
+  if (st != RADAR_OK || !in_place) return st;
+  a.new_lens = new_lens;
+  launch(RADAR_K_APPEND, k_fork_lens, dim3(1), dim3(1024), 0, stream, a);
+  return launch_status();
+}
+
+}  // extern "C"

@@ -36,6 +36,8 @@ struct RotArgs {
   int64_t pos0;
   const int64_t* pos;
   int per_token, inverse;
+  const int* axis;         // of each pair, or null; pos is [n_axes][B][T] then
+  int n_axes;
   const int64_t* lens;
   int64_t row0;
   const int64_t* rows;
@@ -53,7 +55,8 @@ __device__ __forceinline__ bool token_at(const RotArgs& a, int64_t i, TokenAt* o
   o->b = (int)i / a.T;
   o->t = (int)i - o->b * a.T;
   if (a.lens && o->t >= a.lens[o->b]) return false;
-  o->pos = a.pos ? (a.per_token ? a.pos[i] : a.pos[o->b] + o->t) : a.pos0 + o->t;
+  // (with axes the token itself: its pairs' positions differ)
+  o->pos = a.axis ? i : a.pos ? (a.per_token ? a.pos[i] : a.pos[o->b] + o->t) : a.pos0 + o->t;
   o->row = (a.rows ? a.rows[o->b] : a.row0) + o->t;
   return true;
 }
@@ -68,6 +71,14 @@ __device__ __forceinline__ int64_t first_token() {
 // (cos, sin) of a pair, times mscale; the sign of the direction in sin
 __device__ __forceinline__ float2 turn_of(const RotArgs& a, int pair, int64_t pos) {
   constexpr double kInv2Pi = 0.15915494309189533577;
+  if (a.axis) {                            // uniform
+    const int x = a.axis[pair];
+    if ((unsigned)x >= (unsigned)a.n_axes) {
+      const float nan = __uint_as_float(0x7fc00000u);
+      return make_float2(nan, nan);
+    }
+    pos = a.pos[x * a.n_tok + pos];
+  }
   const double turns = (double)pos * a.freq[pair] * kInv2Pi;
   float s, c;
   sincospif(2.f * (float)(turns - __builtin_rint(turns)), &s, &c);
@@ -313,6 +324,11 @@ void launch_rotary(const RotArgs& a, const radar_rope& rope, hipStream_t st) {
   else go(std::false_type{});
 }
 
+radar_status check_axes(int n_axes, const int32_t* axis, const int64_t* pos) {
+  return n_axes < 1 || !axis || !pos || !aligned16(axis) || !aligned16(pos) ? RADAR_EINVAL
+                                                                           : RADAR_OK;
+}
+
 radar_status run_rotary(RotArgs& a, const radar_rope& rope, radar_dtype dt, hipStream_t st) {
   a.freq = rope.inv_freq;
   a.pairs = rope.rot_dim / 2;
@@ -331,19 +347,13 @@ radar_status check_tokens(int64_t batch, int64_t tokens) {
   return RADAR_OK;
 }
 
-}  // namespace
-}  // namespace radar_impl
-
-using namespace radar_impl;
-
-extern "C" {
-
-radar_status radar_rotary(const radar_rope* rope, int32_t batch, int64_t tokens,
-                          int32_t head_dim, radar_dtype dtype, int32_t n_q_heads,
-                          const radar_rows* q, const radar_rows* q_out, int32_t n_k_heads,
-                          const radar_rows* k, const radar_rows* k_out, int64_t pos0,
-                          const int64_t* pos, int32_t pos_per_token, const int64_t* lens,
-                          int32_t inverse, hipStream_t stream) {
+// (axis null: positions as radar_rotary takes them)
+radar_status rotate_rows(const radar_rope* rope, int n_axes, const int32_t* axis, int32_t batch,
+                         int64_t tokens, int32_t head_dim, radar_dtype dtype, int32_t n_q_heads,
+                         const radar_rows* q, const radar_rows* q_out, int32_t n_k_heads,
+                         const radar_rows* k, const radar_rows* k_out, int64_t pos0,
+                         const int64_t* pos, int32_t pos_per_token, const int64_t* lens,
+                         int32_t inverse, hipStream_t stream) {
   radar_status r = check_rope(rope, head_dim, dtype);
   if (r != RADAR_OK) return r;
   const int esz = dtype == RADAR_BF16 ? 2 : 4;
@@ -361,16 +371,18 @@ radar_status radar_rotary(const radar_rope* rope, int32_t batch, int64_t tokens,
   a.T = (int)tokens;
   a.n_tok = batch * tokens;
   a.pos0 = pos0; a.pos = pos; a.per_token = pos_per_token != 0; a.lens = lens;
+  a.axis = axis; a.n_axes = n_axes;
   a.inverse = inverse != 0;
   a.d = head_dim;
   return run_rotary(a, *rope, dtype, stream);
 }
 
-radar_status radar_rotary_fill(const radar_config* cfg, const radar_rope* rope, int64_t tokens,
-                               const radar_rows* q, const radar_rows* q_out, const radar_rows* k,
-                               const radar_rows* v, void* K, void* V, int64_t row0,
-                               const int64_t* rows, int64_t pos0, const int64_t* pos,
-                               int32_t pos_per_token, const int64_t* lens, hipStream_t stream) {
+radar_status fill_rows(const radar_config* cfg, const radar_rope* rope, int n_axes,
+                       const int32_t* axis, int64_t tokens, const radar_rows* q,
+                       const radar_rows* q_out, const radar_rows* k, const radar_rows* v, void* K,
+                       void* V, int64_t row0, const int64_t* rows, int64_t pos0,
+                       const int64_t* pos, int32_t pos_per_token, const int64_t* lens,
+                       hipStream_t stream) {
   Shape s;
   radar_status r = check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
@@ -397,9 +409,60 @@ radar_status radar_rotary_fill(const radar_config* cfg, const radar_rope* rope, 
   a.T = (int)tokens;
   a.n_tok = s.B * tokens;
   a.pos0 = pos0; a.pos = pos; a.per_token = pos_per_token != 0; a.lens = lens;
+  a.axis = axis; a.n_axes = n_axes;
   a.row0 = row0; a.rows = rows; a.cap = s.cap;
   a.d = s.d;
   return run_rotary(a, *rope, s.dt, stream);
+}
+
+}  // namespace
+}  // namespace radar_impl
+
+using namespace radar_impl;
+
+extern "C" {
+
+radar_status radar_rotary(const radar_rope* rope, int32_t batch, int64_t tokens,
+                          int32_t head_dim, radar_dtype dtype, int32_t n_q_heads,
+                          const radar_rows* q, const radar_rows* q_out, int32_t n_k_heads,
+                          const radar_rows* k, const radar_rows* k_out, int64_t pos0,
+                          const int64_t* pos, int32_t pos_per_token, const int64_t* lens,
+                          int32_t inverse, hipStream_t stream) {
+  return rotate_rows(rope, 0, nullptr, batch, tokens, head_dim, dtype, n_q_heads, q, q_out,
+                     n_k_heads, k, k_out, pos0, pos, pos_per_token, lens, inverse, stream);
+}
+
+radar_status radar_rotary_axes(const radar_rope* rope, int32_t n_axes, const int32_t* axis,
+                               int32_t batch, int64_t tokens, int32_t head_dim,
+                               radar_dtype dtype, int32_t n_q_heads, const radar_rows* q,
+                               const radar_rows* q_out, int32_t n_k_heads, const radar_rows* k,
+                               const radar_rows* k_out, const int64_t* pos, const int64_t* lens,
+                               int32_t inverse, hipStream_t stream) {
+  const radar_status r = check_axes(n_axes, axis, pos);
+  if (r != RADAR_OK) return r;
+  return rotate_rows(rope, n_axes, axis, batch, tokens, head_dim, dtype, n_q_heads, q, q_out,
+                     n_k_heads, k, k_out, 0, pos, 1, lens, inverse, stream);
+}
+
+radar_status radar_rotary_fill(const radar_config* cfg, const radar_rope* rope, int64_t tokens,
+                               const radar_rows* q, const radar_rows* q_out, const radar_rows* k,
+                               const radar_rows* v, void* K, void* V, int64_t row0,
+                               const int64_t* rows, int64_t pos0, const int64_t* pos,
+                               int32_t pos_per_token, const int64_t* lens, hipStream_t stream) {
+  return fill_rows(cfg, rope, 0, nullptr, tokens, q, q_out, k, v, K, V, row0, rows, pos0, pos,
+                   pos_per_token, lens, stream);
+}
+
+radar_status radar_rotary_fill_axes(const radar_config* cfg, const radar_rope* rope,
+                                    int32_t n_axes, const int32_t* axis, int64_t tokens,
+                                    const radar_rows* q, const radar_rows* q_out,
+                                    const radar_rows* k, const radar_rows* v, void* K, void* V,
+                                    int64_t row0, const int64_t* rows, const int64_t* pos,
+                                    const int64_t* lens, hipStream_t stream) {
+  const radar_status r = check_axes(n_axes, axis, pos);
+  if (r != RADAR_OK) return r;
+  return fill_rows(cfg, rope, n_axes, axis, tokens, q, q_out, k, v, K, V, row0, rows, 0, pos, 1,
+                   lens, stream);
 }
 
 }  // extern "C"
