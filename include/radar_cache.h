@@ -3,8 +3,9 @@
  * radar.h: rotary positions for the rows on their way into the cache, exact
  * attention of a batch over a prefix that its sequences share, exact
  * attention that accumulates the weight of every cache row, eviction of
- * the rows with the least of it, the acceptance of a path of drafted tokens
- * (a tree or a chain), and the forking of the cache's sequences.
+ * the rows with the least of it, attention of drafted tokens (a tree or a
+ * chain) over the cache and the acceptance of one of their paths, and the
+ * forking of the cache's sequences.
  *
  * Conventions are those of radar.h: device pointers owned by the caller and
  * aligned to 16 bytes, dense row-major layouts unless strides are given, no
@@ -187,6 +188,33 @@ size_t radar_evict_workspace_bytes(const radar_config* cfg, int64_t t,
  * [nodes] for all with parent_shared). parent NULL: a chain, node i follows
  * node i - 1. */
 #define RADAR_MAX_TREE 512      /* most nodes where a parent list is given */
+
+/* Query row (b, i, q head) attends rows [0, len) of K and V and the rows of node
+ * i and of the nodes above it (its parent, the parent's, ..): exact softmax
+ * attention with the scale 1/sqrt(head_dim). q and out are rows [batch][nodes]
+ * [n_q_heads][head_dim] (see radar_rows); out may be q (the same address and
+ * strides), there is no other overlap. Nodes from N_b on are
+ * neither read nor written, and what the rows hold that a node does not attend,
+ * NaN and infinities too, does not matter to it. A node whose list of parents leaves the tree
+ * (a parent below -1 or not before its child) gets NaN outputs; so does every
+ * node of a sequence with lens[b] outside [0, t], counts[b] outside [0, nodes]
+ * or len + N_b above the capacity. Requires 1 <= nodes (at most RADAR_MAX_TREE
+ * with parent), 0 <= t, t + nodes <= capacity where lens is NULL, t <= capacity
+ * where it is not; batch * nodes * n_q_heads < 2^27. With a bf16 cache the weights enter the product with V in 16
+ * bits where a kv head has at most 16 query rows (nodes n_q_heads / n_kv_heads),
+ * and rounded to bf16 where it has more; everything else is fp32. */
+radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q,
+                               const void* K, const void* V, int64_t t,
+                               const int64_t* lens, int64_t nodes,
+                               const int64_t* counts, const int32_t* parent,
+                               int32_t parent_shared, const radar_rows* out,
+                               void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
+
+/* Scratch bytes for every call with this config, at most this many nodes and at
+ * most this t (0 if the arguments are invalid). */
+size_t radar_attend_tree_workspace_bytes(const radar_config* cfg, int64_t nodes,
+                                         int64_t t);
 
 /* The drafted tokens that the model agrees with: from the sequence's end, where
  * it chose first[b], to the lowest of the nodes there whose token that is, from a

@@ -19,8 +19,12 @@ LIB = os.path.join(HERE, "libradar.so")
 INCLUDE = os.path.join(ROOT, "include")
 OBJ_DIR = os.path.join(HERE, "_build")
 # the cache operators: no kernel of the decode path is compiled from these
-CACHE_UNITS = ("rotary.hip", "prefix.hip", "attend.hip", "evict.hip", "branch.hip")
-CACHE_HEADERS = ("cache_impl.h", "attend_impl.h", "evict_slices.h")
+CACHE_UNITS = ("rotary.hip", "prefix.hip", "attend.hip", "evict.hip", "branch.hip",
+               "draft.hip", "tree.hip")
+# those compiled once per element type and head dim
+ATTEND_UNITS = ("attend.hip", "tree.hip")
+CACHE_HEADERS = ("cache_impl.h", "attend_impl.h", "flash_impl.h", "tree_impl.h",
+                 "evict_slices.h")
 FEATURE_COUNTS = (64, 128, 256, 512, 1024, 2048)
 
 HIPCC_FLAGS = [
@@ -42,10 +46,9 @@ def units():
     """(object name, source, extra flags) of every translation unit."""
     out = [("radar.o", "radar.hip", []), ("build.o", "build.hip", []),
            ("split.o", "split.hip", [])]
-    out += [(f[:-4] + ".o", f, []) for f in CACHE_UNITS if f != "attend.hip"]
-    out += [(f"attend_{n}_{d}.o", "attend.hip",
-             [f"-DRADAR_ATTEND_F32={f32}", f"-DRADAR_ATTEND_D={d}"])
-            for f32, n in ((0, "bf16"), (1, "f32")) for d in (64, 128)]
+    out += [(f[:-4] + ".o", f, []) for f in CACHE_UNITS if f not in ATTEND_UNITS]
+    out += [(f"{f[:-4]}_{n}_{d}.o", f, [f"-DRADAR_ATTEND_F32={f32}", f"-DRADAR_ATTEND_D={d}"])
+            for f in ATTEND_UNITS for f32, n in ((0, "bf16"), (1, "f32")) for d in (64, 128)]
     out += [(f"fused_n{n}.o", "fused.hip", [f"-DRADAR_FUSED_N={n}"])
             for n in FEATURE_COUNTS]
     return out

@@ -49,6 +49,9 @@ def declare(L) -> None:
     L.radar_attend_accumulate_workspace_bytes.argtypes = [cfgp, i64]
     L.radar_evict.argtypes = [cfgp, _P, _P, _P, i64, _P, i64, i64, _P, _P, _P, sz, _P]
     L.radar_evict_workspace_bytes.argtypes = [cfgp, i64, i64, i64]
+    L.radar_attend_tree.argtypes = [cfgp, rowsp, _P, _P, i64, _P, i64, _P, _P, i32, rowsp, _P, sz,
+                                    _P]
+    L.radar_attend_tree_workspace_bytes.argtypes = [cfgp, i64, i64]
     L.radar_accept_tree.argtypes = [cfgp, _P, _P, i64, _P, i64, _P, _P, i32, _P, _P, _P, _P, _P,
                                     _P, _P, _P]
     L.radar_keep_path.argtypes = [cfgp, _P, _P, i64, _P, _P, i64, _P, _P, _P]
@@ -57,11 +60,11 @@ def declare(L) -> None:
     L.radar_fork.argtypes = [cfgp, _P, _P, _P, _P, _P, i64, i64, _P, _P, _P]
     for fn in ("radar_attend_prefix_workspace_bytes",
                "radar_attend_accumulate_workspace_bytes", "radar_evict_workspace_bytes",
-               "radar_extend_index_workspace_bytes"):
+               "radar_attend_tree_workspace_bytes", "radar_extend_index_workspace_bytes"):
         getattr(L, fn).restype = sz
     for fn in ("radar_rotary", "radar_rotary_fill", "radar_rotary_axes", "radar_rotary_fill_axes",
                "radar_attend_prefix", "radar_attend_accumulate", "radar_evict",
-               "radar_accept_tree", "radar_keep_path", "radar_extend_index", "radar_fork"):
+               "radar_attend_tree", "radar_accept_tree", "radar_keep_path", "radar_extend_index", "radar_fork"):
         getattr(L, fn).restype = ctypes.c_int
 
 
@@ -551,6 +554,42 @@ def _nodes(cfg, parent, counts, N):
     if counts is not None:
         _need(counts, torch.int64, "counts", cfg.batch)
     return parent, shared, counts
+
+
+def attend_tree_workspace_bytes(cfg: Config, nodes: int, t: int) -> int:
+    """Scratch for every call with this config, at most this many nodes and at most
+    this t."""
+    return int(lib().radar_attend_tree_workspace_bytes(ctypes.byref(cfg.c_struct()), nodes, t))
+
+
+def attend_tree(cfg: Config, q, K, V, t: int, parent=None, counts=None, out=None, lens=None,
+                workspace=None):
+    """radar_attend_tree: exact attention of N drafted tokens' queries (q
+    [B][N][Hq][d], or [B][Hq][d] for one token; strided as it comes out of a
+    projection) over rows [0, t) (or [0, lens[b])) of K and V and, of the N rows
+    behind them, the token's own and those of the tokens it follows. parent: the
+    one that each follows, int32 [N] for all sequences or [B][N], at most 512, -1
+    behind the sequence's last row; None: a chain of any length (a chunk of a
+    prompt; N = 1 a decode step). counts (int64 [B]): only so many of them (the
+    others are 0 in a new out, untouched in a given one). out may be q. Has no
+    gradient: operands that want one are refused. Returns out."""
+    _no_gradient("attend_tree", q, K, V)
+    rq, B, N, H, d = _rows(q, "q", cfg.dtype)
+    if (B, H, d) != (cfg.batch, cfg.n_q_heads, cfg.head_dim):
+        raise ValueError("q must be [batch][N][n_q_heads][head_dim], the config's "
+                         f"{cfg.batch}, {cfg.n_q_heads} heads of {cfg.head_dim}")
+    _cache(cfg, K, V)
+    parent, shared, counts = _nodes(cfg, parent, counts, N)
+    lens = _lens_of(lens, B)
+    out, ro = _out_rows(q, out, "out", counts)
+    _one_device(q, K, V, parent, counts, lens, out, workspace)
+    by = ctypes.byref
+    c = by(cfg.c_struct())
+    need = lib().radar_attend_tree_workspace_bytes(c, N, t) if workspace is None else 0
+    workspace, n = _workspace(workspace, need, q.device)
+    _call("radar_attend_tree", q, c, by(rq), _ptr(K), _ptr(V), t, _ptr(lens), N, _ptr(counts),
+          _ptr(parent), shared, by(ro), _ptr(workspace), n)
+    return out
 
 
 def _given_or_new(x, name, dtype, shape, device):

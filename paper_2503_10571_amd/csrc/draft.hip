@@ -1,0 +1,233 @@
+// Attention of drafted tokens over the cache (include/radar_cache.h): how a call is cut
+// into blocks and the merge of their partials. The blocks are tree.hip's.
+#include "tree_impl.h"
+
+namespace radar_impl {
+namespace {
+
+constexpr int kSlots = 512;                // workgroups that the chip holds at once
+constexpr int kFiner = 3;                  // of sequences of different lengths
+// partials of a row: a block has a step at least, and there are at most 3/2 kSlots kFiner
+// blocks where rows have more than one
+constexpr int kMaxPartials = kSlots * kFiner * 3 / 2;
+
+// A query row's output from its partials by NW waves: D / 4 lanes on four dims each of one
+// partial, the others on the next.
+//   out = sum_i acc_i 2^(m_i - m) / sum_i l_i 2^(m_i - m),  m = max_i m_i
+template <typename T, int D, int NW>
+__global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_tile, int64_t step) {
+  constexpr int kThreads = NW * kWave, kTpp = D / 4, kGroups = kThreads / kTpp;
+  constexpr int kPer = 4 / NW, kMost = NW == 1 ? kWave : kMaxPartials;
+  __shared__ float f_lds[kPer][kMost];
+  __shared__ float red[8];
+  __shared__ __attribute__((aligned(16))) f32x4_t acc_lds[256];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int own = wave / NW, tid = threadIdx.x % kThreads;
+  auto sync = [] {
+    if constexpr (NW == 1) {
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    } else {
+      __syncthreads();
+    }
+  };
+  const int64_t n_rows = (int64_t)a.B * a.nodes * a.Hq;
+  for (int64_t x = (int64_t)blockIdx.x * kPer + own; x < n_rows; x += (int64_t)gridDim.x * kPer) {
+    const int hq = (int)(x % a.Hq), node = (int)(x / a.Hq % a.nodes), hk = hq / a.G;
+    const int64_t b = x / a.Hq / a.nodes, bh = b * a.Hkv + hk;
+    const TreeSeq s = tree_seq(a, b);
+    T* o = static_cast<T*>(a.out) + b * a.o_seq + node * a.o_node + hq * a.o_head;
+    if (s.rows < 0) {
+      for (int i = tid; i < D; i += kThreads) o[i] = from_f32<T>(__uint_as_float(0x7fc00000u));
+      continue;
+    }
+    if (node >= s.nodes) continue;
+    const int row = node * a.G + hq % a.G;
+    const int n = (int)((tree_end(a, s, (row / rows_per_tile + 1) * rows_per_tile) + step - 1) / step);
+    const int64_t first = bh * a.splits * a.M + row;
+    float mx = -INFINITY;
+    for (int i = tid; i < n; i += kThreads) {
+      const float m = a.ml[2 * (first + (int64_t)i * a.M)];
+      f_lds[own][i] = m;
+      mx = fmaxf(mx, m);
+    }
+    mx = wave_max(mx);
+    if constexpr (NW > 1) {
+      if (lane == 0) red[wave] = mx;
+      sync();
+      mx = fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3]));
+    }
+    float ls = 0.f;
+    for (int i = tid; i < n; i += kThreads) {
+      const float f = f_lds[own][i] == -INFINITY ? 0.f : fast_exp2(f_lds[own][i] - mx);
+      f_lds[own][i] = f;
+      ls = fmaf(a.ml[2 * (first + (int64_t)i * a.M) + 1], f, ls);
+    }
+    ls = wave_sum(ls);
+    if constexpr (NW > 1) {
+      if (lane == 0) red[4 + wave] = ls;
+    }
+    sync();
+    if constexpr (NW > 1) ls = (red[4] + red[5]) + (red[6] + red[7]);
+    const int grp = tid / kTpp, e = tid % kTpp;
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = grp; i < n; i += kGroups) {
+      const f32x4_t p = *reinterpret_cast<const f32x4_t*>(a.acc + (first + (int64_t)i * a.M) * D + 4 * e);
+      const float f = f_lds[own][i];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = fmaf(p[k], f, v[k]);
+    }
+    acc_lds[threadIdx.x] = v;
+    sync();
+    const float* y = reinterpret_cast<const float*>(acc_lds + own * kThreads);
+    for (int i = tid; i < D; i += kThreads) {
+      float r = 0.f;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) r += y[g * D + i];
+      o[i] = from_f32<T>(r / ls);
+    }
+    sync();                                // (the next row writes where this one reads)
+  }
+}
+
+int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
+int slots() { return std::min(kSlots, 2 * num_cu()); }
+
+// row waves of M query rows a pair
+int tree_waves(const Shape& s, int64_t M) {
+  if (M <= (esize(s) == 4 ? 48 : flash_rows(esize(s), 1))) return 1;
+  if (esize(s) == 4) return ceil_div(M, 64) * 64 < ceil_div(M, 128) * 128 ? 2 : 4;
+  return M <= 64 ? 2 : 4;
+}
+
+struct TreePlan {
+  int rw, mtiles, splits, rows_per_tile;
+  int64_t tiles, step;
+};
+
+TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
+  TreePlan p;
+  const int64_t M = nodes * s.G, units = (int64_t)s.B * s.Hkv;
+  p.rw = tree_waves(s, M);
+  p.rows_per_tile = flash_rows(esize(s), p.rw);
+  p.mtiles = (int)ceil_div(M, p.rows_per_tile);
+  const int ntg = flash_tile(esize(s), p.rw);
+  const int64_t steps = ceil_div(t + nodes, ntg), blocks = units * p.mtiles;
+  int64_t n = (slots() * (ragged ? kFiner : 1) + blocks / 2) / blocks;
+  n = std::max<int64_t>(1, std::min(n, steps));
+  if (steps <= 4) n = 1;
+  p.tiles = ceil_div(steps, n);
+  p.splits = (int)ceil_div(steps, p.tiles);
+  p.step = p.tiles * ntg;
+  return p;
+}
+
+// Partial rows of every call with at most these nodes and t: blocks of more than one split
+// are at most 3/2 of the slots (two splits where rounding gives them), with min(M, 128)
+// rows each; and no more than one for each 32 rows.
+int64_t most_partials(const Shape& s, int64_t nodes, int64_t t) {
+  const int64_t M = nodes * s.G, units = (int64_t)s.B * s.Hkv;
+  const int64_t by_slots = (int64_t)slots() * kFiner * 3 / 2 * std::min<int64_t>(M, 128);
+  return std::min(by_slots, units * ceil_div(t + nodes, 32) * M);
+}
+struct TreeWs {
+  size_t acc, ml, total;
+};
+TreeWs tree_ws(const Shape& s, int64_t nodes, int64_t t) {
+  TreeWs w;
+  const size_t n = (size_t)most_partials(s, nodes, t);
+  w.acc = 0;
+  w.ml = align256(n * s.d * 4);
+  w.total = std::max<size_t>(256, w.ml + align256(n * 8));
+  return w;
+}
+
+radar_status check_nodes(const Shape& s, int64_t nodes, bool tree) {
+  if (nodes < 1) return RADAR_EINVAL;
+  if (tree && nodes > RADAR_MAX_TREE) return RADAR_EUNSUPPORTED;
+  if (nodes > s.cap) return RADAR_ECAPACITY;
+  return (int64_t)s.B * s.Hq * nodes < (1 << 27) ? RADAR_OK : RADAR_EUNSUPPORTED;
+}
+
+bool bad16(const void* p) { return !p || !aligned16(p); }
+bool odd16(const void* p) { return p && !aligned16(p); }
+bool good_rows(const radar_rows* r, int esz) {
+  return r && r->data && aligned16(r->data) && r->seq * esz % 16 == 0 && r->token * esz % 16 == 0 &&
+         r->head * esz % 16 == 0;
+}
+
+}  // namespace
+}  // namespace radar_impl
+
+using namespace radar_impl;
+
+extern "C" {
+
+size_t radar_attend_tree_workspace_bytes(const radar_config* cfg, int64_t nodes, int64_t t) {
+  Shape s;
+  if (check_cache(cfg, &s) != RADAR_OK || check_nodes(s, nodes, false) != RADAR_OK || t < 0 || t > s.cap)
+    return 0;
+  return tree_ws(s, nodes, t).total;
+}
+
+radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, const void* K,
+                               const void* V, int64_t t, const int64_t* lens, int64_t nodes,
+                               const int64_t* counts, const int32_t* parent,
+                               int32_t parent_shared, const radar_rows* out, void* workspace,
+                               size_t workspace_bytes, hipStream_t stream) {
+  Shape s;
+  radar_status r = check_cache(cfg, &s);
+  if (r != RADAR_OK) return r;
+  const int esz = esize(s);
+  if (!good_rows(q, esz) || !good_rows(out, esz) || bad16(K) || bad16(V) || odd16(lens) || odd16(counts) ||
+      odd16(parent))
+    return RADAR_EINVAL;
+  r = check_nodes(s, nodes, parent != nullptr);
+  if (r != RADAR_OK) return r;
+  if (t < 0 || t > s.cap || (!lens && nodes > s.cap - t)) return RADAR_ECAPACITY;
+  const TreeWs w = tree_ws(s, nodes, t);
+  if (bad16(workspace) || workspace_bytes < w.total) return RADAR_EWORKSPACE;
+  const TreePlan p = plan_tree(s, nodes, t, lens != nullptr);
+  TreeArgs a{};
+  a.q = q->data; a.q_seq = q->seq; a.q_node = q->token; a.q_head = q->head;
+  a.out = out->data; a.o_seq = out->seq; a.o_node = out->token; a.o_head = out->head;
+  a.B = s.B; a.Hq = s.Hq; a.Hkv = s.Hkv; a.G = s.G;
+  a.qscale = kLog2e / std::sqrt((float)s.d);
+  a.K = K; a.V = V; a.lens = lens; a.counts = counts; a.t = t; a.cap = s.cap;
+  a.nodes = (int)nodes; a.parent = parent; a.parent_shared = parent_shared != 0;
+  a.splits = p.splits; a.mtiles = p.mtiles; a.M = (int)(nodes * s.G); a.tiles = p.tiles;
+  a.acc = static_cast<float*>(workspace);
+  a.ml = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + w.ml);
+  if (s.dt == RADAR_BF16) {
+    if (s.d == 64) launch_tree_bf16_64(a, p.rw, stream);
+    else launch_tree_bf16_128(a, p.rw, stream);
+  } else {
+    if (s.d == 64) launch_tree_f32_64(a, p.rw, stream);
+    else launch_tree_f32_128(a, p.rw, stream);
+  }
+  r = launch_status();
+  if (r != RADAR_OK || p.splits == 1) return r;
+  const int64_t rows = (int64_t)s.B * s.Hq * nodes;
+  auto merge = [&](auto tag, auto d) {
+    typedef decltype(tag) T;
+    constexpr int D = decltype(d)::value;
+    if (p.splits <= kWave && rows > 4 * num_cu())
+      launch(RADAR_K_COMBINE, k_tree_merge<T, D, 1>, dim3((unsigned)std::min<int64_t>(ceil_div(rows, 4), 1 << 16)),
+             dim3(256), 0, stream, a, p.rows_per_tile, p.step);
+    else
+      launch(RADAR_K_COMBINE, k_tree_merge<T, D, 4>, dim3((unsigned)std::min<int64_t>(rows, 1 << 16)), dim3(256), 0,
+             stream, a, p.rows_per_tile, p.step);
+  };
+  if (s.dt == RADAR_BF16) {
+    if (s.d == 64) merge(bf16_t{}, std::integral_constant<int, 64>{});
+    else merge(bf16_t{}, std::integral_constant<int, 128>{});
+  } else {
+    if (s.d == 64) merge(float{}, std::integral_constant<int, 64>{});
+    else merge(float{}, std::integral_constant<int, 128>{});
+  }
+  return launch_status();
+}
+
+}  // extern "C"

@@ -1,0 +1,177 @@
+// Attention of drafted tokens, a tree or a chain, over the cache (compiled once per
+// element type and head dim: -DRADAR_ATTEND_F32=0|1 -DRADAR_ATTEND_D=64|128). The pass
+// over the rows is flash_impl.h's: a pair's query rows are those of all its nodes, and
+// only the steps that hold drafted rows look at who attends which.
+#include "flash_impl.h"
+#include "tree_impl.h"
+
+#ifndef RADAR_ATTEND_D
+#define RADAR_ATTEND_D 128
+#endif
+#ifndef RADAR_ATTEND_F32
+#define RADAR_ATTEND_F32 0
+#endif
+
+namespace radar_impl {
+namespace {
+
+constexpr int kTreeWords = RADAR_MAX_TREE / 32;
+// a node's words in LDS: ones, its nodes' bits, zeros, zeros, whether its list of
+// parents leaves the tree; an odd number, for the banks
+constexpr int kNodeWords = (kTreeWords + 4) | 1;
+
+struct TreeMask {
+  static constexpr bool kOn = true;
+  int64_t from, rows;        // the first row that not all attend; the sequence's rows
+  const uint32_t* bits;      // of the tile's nodes; null: a chain
+  int node0, g_log2;         // the tile's first node
+  int* odd;                  // LDS
+  bool direct;
+  unsigned char* out;        // of the tile's first node, in bytes
+  int64_t o_node, o_head;
+
+  __device__ __forceinline__ uint32_t word(int i, int64_t x) const {
+    const int n = i >> g_log2;
+    if (!bits) {                           // uniform
+      const int64_t last = rows + node0 + n - x;
+      return last < 0 ? 0u : last >= 31 ? ~0u : (2u << last) - 1;
+    }
+    const int rel = (int)max(x - rows, (int64_t)-32);
+    const uint32_t* w = bits + n * kNodeWords + min(rel >> 5, kTreeWords) + 1;
+    return __builtin_amdgcn_alignbit(w[1], w[0], rel & 31);
+  }
+  __device__ __forceinline__ void found() const { *odd = 1; }
+  __device__ __forceinline__ bool any_found() const {
+    __syncthreads();
+    return *odd != 0;
+  }
+  __device__ __forceinline__ float finish(int i, float l) const {
+    return bits && bits[(i >> g_log2) * kNodeWords + kTreeWords + 3] ? __uint_as_float(0x7fc00000u) : l;
+  }
+  __device__ __forceinline__ void* out_row(int i) const {
+    return out + (i >> g_log2) * o_node + (i & ((1 << g_log2) - 1)) * o_head;
+  }
+};
+
+// The bits of nodes [node0, node0 + n): node i's are its own, its parent's, .. up to a
+// root. A thread walks up from each, and takes a run of nodes that each follow the one
+// before (up to 32, a word's) at once: `runs` marks those nodes.
+__device__ __forceinline__ void tree_bits(const TreeArgs& a, int64_t b, int nodes, int node0, int n,
+                                          unsigned char* lds, uint32_t* bits) {
+  int* par = reinterpret_cast<int*>(lds);
+  u64* runs = reinterpret_cast<u64*>(lds + RADAR_MAX_TREE * 4);
+  const int tid = threadIdx.x;
+  const int* list = a.parent + (a.parent_shared ? 0 : b * a.nodes);
+  for (int i = tid; i < (nodes + 63) / 64 * 64; i += 256) {
+    const int p = i < nodes ? list[i] : -2;
+    const bool good = p >= -1 && p < i;
+    par[i] = good ? p : -2;
+    const u64 run = __ballot(good && p == i - 1);
+    if ((tid & 63) == 0) runs[i / 64] = run;
+  }
+  __syncthreads();
+  const uint32_t* run = reinterpret_cast<const uint32_t*>(runs);
+  for (int k = tid; k < n; k += 256) {
+    uint32_t* o = bits + k * kNodeWords;
+    o[0] = ~0u;
+    for (int i = 1; i < kTreeWords + 3; ++i) o[i] = 0;
+    int p = node0 + k;
+    while (p >= 0) {                       // p descends
+      const uint32_t upto = (2u << (p & 31)) - 1, breaks = ~run[p >> 5] & upto;
+      const int s = breaks ? 31 - __clz(breaks) : 0;
+      o[1 + (p >> 5)] |= upto & ~((1u << s) - 1);
+      p = par[(p & ~31) + s];
+    }
+    o[kTreeWords + 3] = p == -2;
+  }
+  __syncthreads();
+}
+
+// Workgroups i and i + 8 share an XCD and its L2: an XCD gets a run of the blocks, in
+// which the row tiles of one (b, kv head, split), who read the same rows, follow one
+// another, the last of them, who in a chain attend the most, first.
+template <typename T, int D, int RW>
+__global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
+  using F = Flash<T, D, RW>;
+  constexpr int kRows = F::O::kRows * RW;
+  using RowArray = float (*)[kRows];
+  __shared__ __attribute__((aligned(16))) unsigned char lds[F::kLds];
+  __shared__ float wm[F::TW * kRows], wl[F::TW * kRows];
+  __shared__ uint32_t bits[kRows * kNodeWords];
+  __shared__ int odd;
+  const int total = a.B * a.Hkv * a.splits * a.mtiles, chunk = (total + 7) / 8;
+  const int i = blockIdx.x % 8 * chunk + blockIdx.x / 8;
+  if ((int)(blockIdx.x / 8) >= chunk || i >= total) return;
+  const int unit = i / a.mtiles, mt = a.mtiles - 1 - i % a.mtiles;
+  const int64_t bh = unit / a.splits, sp = unit % a.splits, b = bh / a.Hkv, hk = bh % a.Hkv;
+  const TreeSeq s = tree_seq(a, b);
+  const int row0 = mt * kRows, node0 = row0 / a.G;
+  const bool direct = a.splits == 1;
+  TreeMask mask;
+  mask.g_log2 = 31 - __clz(a.G);
+  mask.out = static_cast<unsigned char*>(a.out) +
+             (b * a.o_seq + node0 * a.o_node + hk * a.G * a.o_head) * (int64_t)sizeof(T);
+  mask.o_node = a.o_node * (int64_t)sizeof(T);
+  mask.o_head = a.o_head * (int64_t)sizeof(T);
+  if (s.rows < 0) {
+    if (!direct) return;
+    for (int x = threadIdx.x; x < min(kRows, a.M - row0) * D; x += 256)
+      static_cast<T*>(mask.out_row(x / D))[x % D] = from_f32<T>(__uint_as_float(0x7fc00000u));
+    return;
+  }
+  const int rows = min(kRows, s.nodes * a.G - row0);
+  if (rows <= 0) return;
+  const int64_t end = tree_end(a, s, row0 + rows), step = a.tiles * F::NTG;
+  const int64_t r0 = sp * step, r1 = min(end, r0 + step);
+  if (r0 >= end) return;
+  mask.from = s.rows + (a.parent ? 0 : node0 + 1);
+  mask.rows = s.rows;
+  mask.bits = a.parent ? bits : nullptr;
+  mask.node0 = node0;
+  mask.odd = &odd;
+  mask.direct = direct;
+  if (r1 > mask.from) {                    // uniform
+    if (threadIdx.x == 0) odd = 0;
+    if (a.parent) tree_bits(a, b, s.nodes, node0, (rows + a.G - 1) / a.G, lds, bits);
+    else __syncthreads();
+  }
+  const T* q = static_cast<const T*>(a.q) + b * a.q_seq + node0 * a.q_node + hk * a.G * a.q_head;
+  const int64_t at = (bh * a.splits + sp) * a.M + row0;
+  auto block = [&](auto once) {
+    F::template block<false, false, decltype(once)::value>(
+        static_cast<const T*>(a.K) + bh * a.cap * D, static_cast<const T*>(a.V) + bh * a.cap * D, r0, r1, rows,
+        a.qscale,
+        [&](int r) { return q + (r >> mask.g_log2) * a.q_node + (r & (a.G - 1)) * a.q_head; },
+        a.acc + at * D, a.ml + at * 2, nullptr, 0, lds, reinterpret_cast<RowArray>(wm),
+        reinterpret_cast<RowArray>(wl), nullptr, nullptr, 0, nullptr, mask);
+  };
+  // (past the caches where no other row tile reads the rows)
+  if constexpr (RW == 4) {
+    block(std::false_type{});
+  } else {
+    if (a.mtiles == 1) block(std::true_type{});
+    else block(std::false_type{});
+  }
+}
+
+template <typename T, int D>
+void launch_tree(const TreeArgs& a, int rw, hipStream_t st) {
+  const dim3 grid((unsigned)(ceil_div((int64_t)a.B * a.Hkv * a.splits * a.mtiles, 8) * 8)), block(256);
+  if (rw == 1) launch(RADAR_K_ATTEND, k_tree<T, D, 1>, grid, block, 0, st, a);
+  else if (rw == 2) launch(RADAR_K_ATTEND, k_tree<T, D, 2>, grid, block, 0, st, a);
+  else launch(RADAR_K_ATTEND, k_tree<T, D, 4>, grid, block, 0, st, a);
+}
+
+}  // namespace
+
+#if RADAR_ATTEND_F32 && RADAR_ATTEND_D == 64
+void launch_tree_f32_64(const TreeArgs& a, int rw, hipStream_t st) { launch_tree<float, 64>(a, rw, st); }
+#elif RADAR_ATTEND_F32
+void launch_tree_f32_128(const TreeArgs& a, int rw, hipStream_t st) { launch_tree<float, 128>(a, rw, st); }
+#elif RADAR_ATTEND_D == 64
+void launch_tree_bf16_64(const TreeArgs& a, int rw, hipStream_t st) { launch_tree<bf16_t, 64>(a, rw, st); }
+#else
+void launch_tree_bf16_128(const TreeArgs& a, int rw, hipStream_t st) { launch_tree<bf16_t, 128>(a, rw, st); }
+#endif
+
+}  // namespace radar_impl

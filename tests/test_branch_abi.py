@@ -62,6 +62,32 @@ def test_axes_refusals(L):
     assert fill(tokens=0) == 0
 
 
+def test_tree_refusals(L):
+    rows = by(cache_ops._Rows(0x1000, 32768, 4096, 128))
+
+    def call(cfg=_cfg(), q=rows, K=GOOD, V=GOOD, t=100, lens=None, nodes=9, counts=None, parent=GOOD, out=rows, ws=GOOD,
+             n=1 << 30):
+        return L.radar_attend_tree(by(cfg), q, K, V, t, lens, nodes, counts, parent, 0, out, ws, n, None)
+
+    for kw, want in BAD:
+        assert call(cfg=_cfg(**kw)) == want, kw
+    assert call(nodes=0) == 1 and call(nodes=513) == 3 and call(nodes=4097, parent=None) == 2
+    assert call(cfg=_cfg(capacity=1 << 20), nodes=1 << 19, parent=None) == 3       # 2^27 query rows
+    assert call(t=-1) == 2 and call(t=4097) == 2 and call(t=4090) == 2 and call(t=4097, lens=GOOD) == 2
+    for name in ("q", "K", "V", "out"):
+        assert call(**{name: None}) == 1, name
+    for name in ("K", "V", "lens", "counts", "parent"):
+        assert call(**{name: ODD}) == 1, name
+    for bad in ((0, 0, 0, 128), (0x1008, 4096, 4096, 128), (0x1000, 4, 4096, 128), (0x1000, 4096, 4, 128),
+                (0x1000, 4096, 4096, 4)):
+        assert call(q=by(cache_ops._Rows(*bad))) == 1 and call(out=by(cache_ops._Rows(*bad))) == 1, bad
+    need = L.radar_attend_tree_workspace_bytes(by(_cfg()), 9, 100)
+    assert need > 0 and call(n=need - 1) == 5 and call(ws=None) == 5 and call(ws=ODD) == 5
+    for nodes, t in ((0, 100), (9, -1), (9, 4097), (4097, 0)):
+        assert L.radar_attend_tree_workspace_bytes(by(_cfg()), nodes, t) == 0
+    assert L.radar_attend_tree_workspace_bytes(by(_cfg(head_dim=96)), 9, 100) == 0
+
+
 def test_accept_refusals(L):
     def call(cfg=_cfg(), K=GOOD, V=GOOD, t=100, lens=None, nodes=9, counts=None, parent=GOOD, tokens=GOOD, first=GOOD,
              choice=GOOD, path=GOOD, accepted=GOOD, nxt=GOOD, new=None):
