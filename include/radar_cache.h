@@ -16,7 +16,9 @@
  * capacity, kv_dtype and n_sink, with radar.h's limits; the fields of the
  * index and the selection are not read but where a call says so. Workspaces: contents on entry do not
  * matter, and one workspace must not be used by two calls at the same time
- * (two graphs that hold the same one must not be replayed concurrently).
+ * (two graphs that hold the same one must not be replayed concurrently). The
+ * lists of numbers of radar_rotary_axes (axis, pos) and of the calls for drafted
+ * tokens and forking lie on their elements' size instead of 16 bytes.
  *
  * The measurement hook of radar.h books their kernels under the kinds that it
  * has: rotations and what moves rows (eviction, acceptance, forking) as

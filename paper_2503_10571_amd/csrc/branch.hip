@@ -35,23 +35,23 @@ __device__ __forceinline__ void move_rows(const PathArgs& a, int64_t b, int64_t 
   for (int h = wave; h < a.Hkv; h += waves) {
     const int64_t at = ((b * a.Hkv + h) * a.cap + len) * a.row_bytes + c * 16;
     for (int i0 = 0; i0 < n; i0 += kPasses * rows) {
-      uint4 k[kPasses], v[kPasses];
+      u32x4_t k[kPasses], v[kPasses];      // (arrays of uint4 go to scratch memory)
       int from[kPasses];
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         const int i = i0 + p * rows + r;
         from[p] = i < n ? path(i) : i;
         if (from[p] != i) {                // (a row that stays is not written)
-          k[p] = *reinterpret_cast<const uint4*>(a.K + at + (int64_t)from[p] * a.row_bytes);
-          v[p] = *reinterpret_cast<const uint4*>(a.V + at + (int64_t)from[p] * a.row_bytes);
+          k[p] = *reinterpret_cast<const u32x4_t*>(a.K + at + (int64_t)from[p] * a.row_bytes);
+          v[p] = *reinterpret_cast<const u32x4_t*>(a.V + at + (int64_t)from[p] * a.row_bytes);
         }
       }
 #pragma unroll
       for (int p = 0; p < kPasses; ++p) {
         const int i = i0 + p * rows + r;
         if (from[p] != i) {
-          *reinterpret_cast<uint4*>(a.K + at + (int64_t)i * a.row_bytes) = k[p];
-          *reinterpret_cast<uint4*>(a.V + at + (int64_t)i * a.row_bytes) = v[p];
+          *reinterpret_cast<u32x4_t*>(a.K + at + (int64_t)i * a.row_bytes) = k[p];
+          *reinterpret_cast<u32x4_t*>(a.V + at + (int64_t)i * a.row_bytes) = v[p];
         }
       }
     }
@@ -180,147 +180,347 @@ struct ForkArgs {
   int row_bytes;
   int c, n_sink, summ_bytes;         // of a summary
   int64_t summ_rows;
-  int64_t tiles[3];        // of K (and V), masses and summaries, per head
+  int64_t units[3];        // columns of K (and V), masses and summaries, per head
 };
 
 __device__ __forceinline__ int64_t fork_len(const ForkArgs& a, int64_t s) {
   return s == -1 ? 0 : s < -1 || s >= a.B ? -1 : a.lens ? a.lens[s] : a.t;
 }
 
-// A workgroup moves the same 16 bytes of a head's rows in every sequence, so no other
+// A workgroup moves the same bytes of a head's rows in every sequence, so no other
 // one meets the bytes that it overwrites, and the map needs an order within it only.
 // Each workgroup makes the list of the moves once: those whose destination no move
 // still has to read come first, then those that this sets free, and so on; what is
-// left are cycles, whose first sequence is saved. kBatch moves at a time are read
-// before they are written, which any order of reads ahead allows; moves from one
-// sequence that follow one another read it once.
-constexpr int kBatch = 16, kForkTile = 256;
-constexpr uint32_t kNone = 0xffffu, kZero = 0xfffeu;   // as a source: saved one, zeros
-static_assert(RADAR_MAX_FORK < kZero, "sequences in 16 bits");
+// left are cycles, whose first sequence is saved.
+constexpr int kInFlight = 8, kForkThreads = 256;
+// a move is dst << 16 | src; kNone as dst: src is saved; kSaved in src: src as it was saved;
+// kZero as src: zeros
+constexpr uint32_t kNone = 0xffffu, kSaved = 0x8000u, kZero = 0x7fffu;
+static_assert(RADAR_MAX_FORK <= kZero, "sequences in 15 bits");
 constexpr int kStay = -1, kFreed = -2;
 
-template <typename V>
-__device__ __forceinline__ V zeros() { return V{}; }
+struct ForkList {
+  const uint32_t* moves;   // LDS
+  const int* len;          // LDS
+  int n;
+};
 
-// MASS: behind the source's length zeros, up to the destination's
-template <typename V, bool MASS, typename Units>
-__device__ __forceinline__ void fork_column(unsigned char* base, int64_t stride, int64_t x,
-                                            const uint32_t* list, int n, const int* len,
-                                            Units&& units) {
-  V saved = zeros<V>();
-  int64_t saved_units = 0;
-  for (int e0 = 0; e0 < n; e0 += kBatch) {
-    V v[kBatch];
+// One kind of memory: a head's columns of V in a sequence, so many for its length
+struct ForkPlane {
+  unsigned char* base;     // of head 0 (v_off: of K, and V's lies v_off behind)
+  int64_t v_off, head, seq;          // bytes
+  int64_t units, lo;
+  int sub, div, per;
+  int64_t tiles;
+  // columns of a sequence of m rows
+  __device__ __forceinline__ int64_t columns(int m) const {
+    return max((int64_t)0, (int64_t)((max(m, sub) - sub) / div) - lo) * per;
+  }
+};
+
+// Up to kBatch moves of one tile, read together; what they read is written a step later,
+// behind the next step's loads (a wait for loads is one for the stores before them too).
+// The lanes hold 64 moves of the list, and how many of the tile's columns their sources
+// have; moves of none are passed over. Moves from one sequence that follow one another
+// read it once.
+template <typename V, int COLS, bool MASS, bool NT>
+struct ForkStep {
+  static constexpr int kBatch = kInFlight / COLS, kTile = kForkThreads * COLS;
+  V v[kBatch][COLS];
+  unsigned char* at;       // this thread's first column in sequence 0
+  int64_t seq;
+  uint32_t lane_move;
+  int lane_have, lane_old;
+  u64 take;                // the lanes whose moves these are
+
+  // the moves [e1, e1 + 64) of tile i: which of them do anything
+  __device__ __forceinline__ u64 set(const ForkPlane& p, const ForkList& l, int64_t i, int e1) {
+    const int64_t tile = i % p.tiles, plane = i / p.tiles, head = p.v_off ? plane >> 1 : plane;
+    const int64_t x0 = tile * kTile;
+    at = p.base + (p.v_off && (plane & 1) ? p.v_off : 0) + head * p.head +
+         (x0 + threadIdx.x) * (int64_t)sizeof(V);
+    seq = p.seq;
+    const int e = e1 + (int)(threadIdx.x & 63);
+    lane_move = l.moves[min(e, l.n - 1)];
+    auto have = [&](uint32_t s) {
+      return s < kZero ? (int)min(max(p.columns(l.len[s]) - x0, (int64_t)0), (int64_t)kTile) : 0;
+    };
+    lane_have = have(lane_move & 0x7fffu);
+    lane_old = MASS ? have(lane_move >> 16) : 0;
+    return __ballot(e < l.n && (lane_have > 0 || lane_old > 0));
+  }
+  // the first of them, and those that are left
+  __device__ __forceinline__ u64 pick(u64 moves) {
+    u64 rest = moves;
+#pragma unroll
+    for (int j = 0; j < kBatch; ++j) rest &= rest - (rest != 0);
+    take = moves ^ rest;
+    return rest;
+  }
+  __device__ __forceinline__ void like(const ForkStep& o) {
+    at = o.at;
+    seq = o.seq;
+    lane_move = o.lane_move;
+    lane_have = o.lane_have;
+    lane_old = o.lane_old;
+  }
+  __device__ __forceinline__ void load() {
+    u64 t = take;
     uint32_t before = kNone;
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      v[j] = zeros<V>();
-      if (e0 + j >= n) continue;           // uniform
-      const uint32_t s = __builtin_amdgcn_readfirstlane(list[e0 + j]) & 0xffffu;
-      const bool again = j > 0 && s == before;
+      if (!t) continue;                    // uniform
+      const int k = __ffsll(t) - 1;
+      t &= t - 1;
+      const uint32_t s = __builtin_amdgcn_readlane(lane_move, k) & 0xffffu;
+      const bool again = s == before;
       before = s;
-      if (s == kNone || s == kZero) continue;
-      if (again)
-        v[j] = v[j > 0 ? j - 1 : 0];
-      else if (x < units(len[s]))
-        v[j] = *reinterpret_cast<const V*>(base + s * stride + x * (int64_t)sizeof(V));
+      if (again || s >= kZero) continue;
+      const int have = __builtin_amdgcn_readlane(lane_have, k);
+      const unsigned char* from = at + s * seq;
+#pragma unroll
+      for (int c = 0; c < COLS; ++c) {
+        if (MASS) v[j][c] = V{};
+        if ((int)threadIdx.x + c * kForkThreads < have) {
+          const V* q = reinterpret_cast<const V*>(from + c * kForkThreads * sizeof(V));
+          v[j][c] = NT ? __builtin_nontemporal_load(q) : *q;
+        }
+      }
     }
+  }
+  // MASS: zeros behind what the source has, up to the destination's length
+  __device__ __forceinline__ void store(V (&saved)[COLS]) {
+    u64 t = take;
+    uint32_t before = kNone;
+    V w[COLS];
 #pragma unroll
     for (int j = 0; j < kBatch; ++j) {
-      if (e0 + j >= n) continue;
-      const uint32_t e = __builtin_amdgcn_readfirstlane(list[e0 + j]);
-      const uint32_t s = e & 0xffffu, dst = e >> 16;
-      int64_t have = s == kNone ? saved_units : s == kZero ? 0 : units(len[s]);
+      if (!t) continue;
+      const int k = __ffsll(t) - 1;
+      t &= t - 1;
+      const uint32_t e = __builtin_amdgcn_readlane(lane_move, k), s = e & 0xffffu, dst = e >> 16;
+      if (s != before) {
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) w[c] = s & kSaved ? saved[c] : s == kZero ? V{} : v[j][c];
+        // (one of no columns here was passed over when it should have been saved)
+        if (MASS && (s & kSaved) && __builtin_amdgcn_readlane(lane_have, k) == 0)
+#pragma unroll
+          for (int c = 0; c < COLS; ++c) w[c] = V{};
+      }
+      before = s;
       if (dst == kNone) {
-        saved = v[j];
-        saved_units = have;
+#pragma unroll
+        for (int c = 0; c < COLS; ++c) saved[c] = w[c];
         continue;
       }
-      if (MASS) have = max(have, units(len[dst]));
-      if (x < have)
-        *reinterpret_cast<V*>(base + dst * stride + x * (int64_t)sizeof(V)) = s == kNone ? saved : v[j];
+      int upto = __builtin_amdgcn_readlane(lane_have, k);
+      if (MASS) upto = max(upto, __builtin_amdgcn_readlane(lane_old, k));
+      unsigned char* to = at + dst * seq;
+#pragma unroll
+      for (int c = 0; c < COLS; ++c)
+        if ((int)threadIdx.x + c * kForkThreads < upto) {
+          V* q = reinterpret_cast<V*>(to + c * kForkThreads * sizeof(V));
+          if (NT) __builtin_nontemporal_store(w[c], q);
+          else *q = w[c];
+        }
     }
+  }
+};
+
+// Every tile of a plane, a step ahead.
+template <typename V, int COLS, bool MASS, bool NT>
+__device__ __forceinline__ void fork_plane(ForkPlane p, const ForkList& l, int64_t planes) {
+  using Step = ForkStep<V, COLS, MASS, NT>;
+  p.tiles = (p.units + Step::kTile - 1) / Step::kTile;
+  const int64_t all = planes * p.tiles;
+  int64_t i = (int64_t)blockIdx.x - gridDim.x;
+  int e1 = l.n;
+  u64 rest = 0;
+  V saved[COLS];
+#pragma unroll
+  for (int c = 0; c < COLS; ++c) saved[c] = V{};
+  // the step behind `before`; false: there is none
+  auto next = [&](Step& s, const Step& before) {
+    if (rest) {
+      s.like(before);
+    } else {
+      do {
+        e1 += kWave;
+        if (e1 >= l.n) {
+          e1 = 0;
+          i += gridDim.x;
+          if (i >= all) return false;
+        }
+        rest = s.set(p, l, i, e1);
+      } while (!rest);
+    }
+    rest = s.pick(rest);
+    s.load();
+    return true;
+  };
+  Step a, b;
+  if (!next(a, b)) return;
+  for (;;) {
+    const bool more_b = next(b, a);
+    a.store(saved);
+    if (!more_b) break;
+    const bool more_a = next(a, b);
+    b.store(saved);
+    if (!more_a) break;
   }
 }
 
-__global__ __launch_bounds__(kForkTile) void k_fork(ForkArgs a) {
+template <int COLS, bool NT>
+__device__ __forceinline__ void fork_all(const ForkArgs& a, const ForkList& l) {
+  const ForkPlane kv{a.K + a.first * a.row_bytes, a.V - a.K, a.cap * a.row_bytes, a.Hkv * a.cap * a.row_bytes,
+                     a.units[0], a.first, 0, 1, a.row_bytes / 16, 0};
+  fork_plane<u32x4_t, COLS, false, NT>(kv, l, 2 * a.Hkv);
+  if (a.units[1]) {
+    const ForkPlane mass{a.mass, 0, a.cap * 4, a.Hkv * a.cap * 4, a.units[1], 0, 0, 1, 1, 0};
+    fork_plane<uint32_t, COLS, true, false>(mass, l, a.Hkv);
+  }
+  if (a.units[2]) {
+    const int64_t seg0 = max((int64_t)0, a.first - a.n_sink) / a.c;
+    const ForkPlane summ{a.summ + seg0 * a.summ_bytes, 0, a.summ_rows * a.summ_bytes,
+                         a.Hkv * a.summ_rows * a.summ_bytes, a.units[2], seg0, a.n_sink, a.c, a.summ_bytes / 16, 0};
+    fork_plane<u32x4_t, COLS, false, false>(summ, l, a.Hkv);
+  }
+}
+
+// The list of up to 64 sequences' moves by one wave, a sequence a lane: what a round's
+// moves read is marked in LDS, by the round's number.
+__device__ __forceinline__ int list_moves(const ForkArgs& a, int64_t s, int src, int* mark, uint32_t* list) {
+  const int lane = threadIdx.x & 63;
+  auto order = [] {                        // the wave's LDS operations, as written
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
+  bool open = src != kStay;
+  int n = 0;
+  for (int round = 1;; ++round) {
+    mark[lane] = 0;
+    order();
+    if (open && src >= 0) mark[src] = round;
+    order();
+    const bool ready = open && mark[lane] != round;
+    const u64 now = __ballot(ready);
+    if (!now) break;
+    if (ready) list[n + __popcll(now & ((1ull << lane) - 1))] = (uint32_t)lane << 16 | (src == kFreed ? kZero : src);
+    n += __popcll(now);
+    open = open && !ready;
+  }
+  u64 left = __ballot(open);               // cycles
+  while (left) {
+    const int b = __ffsll(left) - 1;
+    if (lane == 0) list[n] = kNone << 16 | (uint32_t)b;
+    ++n;
+    for (int x = b;;) {
+      const int y = __builtin_amdgcn_readlane(src, x);
+      if (lane == 0) list[n] = (uint32_t)x << 16 | (uint32_t)y | (y == b ? kSaved : 0);
+      ++n;
+      left &= ~(1ull << x);
+      if (y == b) break;
+      x = y;
+    }
+  }
+  return n;
+}
+
+__global__ __launch_bounds__(kForkThreads) void k_fork(ForkArgs a) {
   extern __shared__ int fork_lds[];
+  const int lds_b = max(a.B, kWave);
   int* src = fork_lds;                     // or kStay, kFreed
-  int* left = src + a.B;                   // moves that still read it; -1: listed
-  int* len = left + a.B;
-  uint32_t* list = reinterpret_cast<uint32_t*>(len + a.B);   // dst << 16 | src
+  int* left = src + lds_b;                 // moves that still read it; -1: listed
+  int* len = left + lds_b;
+  uint32_t* list = reinterpret_cast<uint32_t*>(len + lds_b);   // dst << 16 | src
   __shared__ int n_list;
+  __shared__ u64 moved;                    // rows of K
   const int tid = threadIdx.x;
-  for (int b = tid; b < a.B; b += kForkTile) {
-    const int64_t n = a.lens ? a.lens[b] : a.t;
-    len[b] = n >= 0 && n <= a.t ? (int)n : -1;
-    left[b] = 0;
+  if (tid == 0) {
+    n_list = 0;
+    moved = 0;
   }
-  if (tid == 0) n_list = 0;
-  __syncthreads();
-  for (int b = tid; b < a.B; b += kForkTile) {
-    const int64_t s = a.src[b];
-    const bool moves = s >= 0 && s < a.B && s != b && len[s] >= 0;
-    src[b] = moves ? (int)s : s == -1 ? kFreed : kStay;
-    if (moves) atomicAdd(&left[s], 1);
-    if (a.new_lens && blockIdx.x == 0) a.new_lens[b] = fork_len(a, s);
-  }
-  // (a move takes its place in the list before it frees its source for others)
-  for (bool more = true; more;) {
+  auto kind = [&](int64_t s, int b) {
+    return s >= 0 && s < a.B && s != b && len[s] >= 0 ? (int)s : s == -1 ? kFreed : kStay;
+  };
+  if (a.B <= kWave) {
+    if (tid < kWave) {
+      const bool on = tid < a.B;
+      const int64_t n = on && a.lens ? a.lens[tid] : a.t, s = on ? a.src[tid] : tid;
+      len[tid] = on && n >= 0 && n <= a.t ? (int)n : -1;
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+      const int m = list_moves(a, s, on ? kind(s, tid) : kStay, left, list);
+      if (on && a.new_lens && blockIdx.x == 0) a.new_lens[tid] = fork_len(a, s);
+      if (tid == 0) n_list = m;
+    }
     __syncthreads();
-    bool any = false;
-    for (int b = tid; b < a.B; b += kForkTile) {
-      if (src[b] == kStay || __atomic_load_n(&left[b], __ATOMIC_RELAXED) != 0) continue;
-      const uint32_t s = src[b] == kFreed ? kZero : (uint32_t)src[b];
-      list[atomicAdd(&n_list, 1)] = (uint32_t)b << 16 | s;
-      __threadfence_block();
-      left[b] = -1;
-      if (src[b] >= 0) atomicSub(&left[src[b]], 1);
-      any = true;
+  } else {
+    for (int b = tid; b < a.B; b += kForkThreads) {
+      const int64_t n = a.lens ? a.lens[b] : a.t;
+      len[b] = n >= 0 && n <= a.t ? (int)n : -1;
+      left[b] = 0;
     }
-    more = __syncthreads_or(any);
-  }
-  // cycles: the lowest sequence of each writes it down
-  for (int b = tid; b < a.B; b += kForkTile) {
-    if (src[b] == kStay || left[b] < 0) continue;
-    int size = 1, low = b;
-    for (int x = src[b]; x != b; x = src[x]) {
-      low = min(low, x);
-      ++size;
+    __syncthreads();
+    for (int b = tid; b < a.B; b += kForkThreads) {
+      const int64_t s = a.src[b];
+      src[b] = kind(s, b);
+      if (src[b] >= 0) atomicAdd(&left[src[b]], 1);
+      if (a.new_lens && blockIdx.x == 0) a.new_lens[b] = fork_len(a, s);
     }
-    if (low != b) continue;
-    uint32_t* out = list + atomicAdd(&n_list, size + 1);
-    *out++ = kNone << 16 | (uint32_t)b;
-    int x = b;
-    for (; src[x] != b; x = src[x]) *out++ = (uint32_t)x << 16 | (uint32_t)src[x];
-    *out = (uint32_t)x << 16 | kNone;
+    // (a move takes its place in the list before it frees its source for others)
+    for (bool more = true; more;) {
+      __syncthreads();
+      bool any = false;
+      for (int b = tid; b < a.B; b += kForkThreads) {
+        if (src[b] == kStay || __atomic_load_n(&left[b], __ATOMIC_RELAXED) != 0) continue;
+        const uint32_t s = src[b] == kFreed ? kZero : (uint32_t)src[b];
+        list[atomicAdd(&n_list, 1)] = (uint32_t)b << 16 | s;
+        __threadfence_block();
+        left[b] = -1;
+        if (src[b] >= 0) atomicSub(&left[src[b]], 1);
+        any = true;
+      }
+      more = __syncthreads_or(any);
+    }
+    // cycles: the lowest sequence of each writes it down
+    for (int b = tid; b < a.B; b += kForkThreads) {
+      if (src[b] == kStay || left[b] < 0) continue;
+      int size = 1, low = b;
+      for (int x = src[b]; x != b; x = src[x]) {
+        low = min(low, x);
+        ++size;
+      }
+      if (low != b) continue;
+      uint32_t* out = list + atomicAdd(&n_list, size + 1);
+      *out++ = kNone << 16 | (uint32_t)b;
+      int x = b;
+      for (; src[x] != b; x = src[x]) *out++ = (uint32_t)x << 16 | (uint32_t)src[x];
+      *out = (uint32_t)x << 16 | (uint32_t)b | kSaved;
+    }
+    __syncthreads();
   }
-  __syncthreads();
   const int n = n_list;
   if (n == 0) return;
-  const int64_t kv_tiles = 2 * a.Hkv * a.tiles[0], mass_tiles = a.Hkv * a.tiles[1];
-  const int64_t all = kv_tiles + mass_tiles + a.Hkv * a.tiles[2];
-  const int per = a.row_bytes / 16;
-  const int64_t seg0 = max((int64_t)0, a.first - a.n_sink) / max(a.c, 1);
-  for (int64_t i = blockIdx.x; i < all; i += gridDim.x) {
-    if (i < kv_tiles) {
-      const int64_t h = i / a.tiles[0] >> 1, x = i % a.tiles[0] * kForkTile + tid;
-      unsigned char* base = (i / a.tiles[0] & 1 ? a.V : a.K) + (h * a.cap + a.first) * a.row_bytes;
-      fork_column<uint4, false>(base, a.Hkv * a.cap * a.row_bytes, x, list, n, len, [&](int m) {
-        return max((int64_t)0, m - a.first) * per;
-      });
-    } else if (i < kv_tiles + mass_tiles) {
-      const int64_t k = i - kv_tiles, h = k / a.tiles[1], x = k % a.tiles[1] * kForkTile + tid;
-      fork_column<uint32_t, true>(a.mass + h * a.cap * 4, a.Hkv * a.cap * 4, x, list, n, len,
-                                  [](int m) { return (int64_t)m; });
-    } else {
-      const int64_t k = i - kv_tiles - mass_tiles, h = k / a.tiles[2];
-      const int64_t x = k % a.tiles[2] * kForkTile + tid;
-      fork_column<uint4, false>(a.summ + (h * a.summ_rows + seg0) * a.summ_bytes,
-                                a.Hkv * a.summ_rows * a.summ_bytes, x, list, n, len, [&](int m) {
-        return max((int64_t)0, max(m - a.n_sink, 0) / a.c - seg0) * (a.summ_bytes / 16);
-      });
-    }
+  // past the caches, of 256 MB, where the call moves more than they hold
+  int64_t rows = 0;
+  for (int e = tid; e < n; e += kForkThreads) {
+    const uint32_t from = list[e] & 0x7fffu;
+    rows += from == kZero ? 0 : max((int64_t)0, len[from] - a.first);
+  }
+  atomicAdd(&moved, (u64)rows);
+  __syncthreads();
+  const bool past = 4 * a.Hkv * (int64_t)moved * a.row_bytes > (256 << 20);
+  const ForkList l{list, len, n};
+  // few moves: two columns of each in flight
+  if (n <= 4) {
+    if (past) fork_all<2, true>(a, l);
+    else fork_all<2, false>(a, l);
+  } else {
+    if (past) fork_all<1, true>(a, l);
+    else fork_all<1, false>(a, l);
   }
 }
 
@@ -344,6 +544,12 @@ __global__ __launch_bounds__(1024) void k_fork_lens(ForkArgs a) {
 
 bool bad16(const void* p) { return !p || !aligned16(p); }
 bool odd16(const void* p) { return p && !aligned16(p); }
+// lists of numbers, read one by one, lie on their elements' size: a row of one may
+// begin anywhere
+template <typename T>
+bool off(const T* p) { return reinterpret_cast<uintptr_t>(p) % sizeof(T) != 0; }
+template <typename... T>
+bool any_off(const T*... p) { return (off(p) || ...); }
 int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
 
 // the index's fields of the config, with radar.h's limits
@@ -390,9 +596,8 @@ radar_status radar_accept_tree(const radar_config* cfg, void* K, void* V, int64_
   Shape s;
   const radar_status r = check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
-  if (bad16(K) || bad16(V) || bad16(tokens) || bad16(first) || bad16(choice) || bad16(path) ||
-      bad16(accepted) || bad16(next) || odd16(lens) || odd16(counts) || odd16(parent) ||
-      odd16(new_lens) || nodes < 1)
+  if (bad16(K) || bad16(V) || !tokens || !first || !choice || !path || !accepted || !next ||
+      any_off(tokens, first, choice, path, accepted, next, lens, counts, parent, new_lens) || nodes < 1)
     return RADAR_EINVAL;
   if (nodes > kMaxTree) return RADAR_EUNSUPPORTED;
   if (t < 0 || t > s.cap || (!lens && nodes > s.cap - t)) return RADAR_ECAPACITY;
@@ -412,8 +617,7 @@ radar_status radar_keep_path(const radar_config* cfg, void* K, void* V, int64_t 
   Shape s;
   const radar_status r = check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
-  if (bad16(K) || bad16(V) || n < 0 || (n > 0 && bad16(path)) || odd16(lens) || odd16(counts) ||
-      odd16(new_lens))
+  if (bad16(K) || bad16(V) || n < 0 || (n > 0 && !path) || any_off(path, lens, counts, new_lens))
     return RADAR_EINVAL;
   if (t < 0 || t > s.cap || n > s.cap) return RADAR_ECAPACITY;
   PathArgs a = path_args(s, K, V, t, lens, n, counts, new_lens);
@@ -438,7 +642,7 @@ radar_status radar_extend_index(const radar_config* cfg, const void* K, const vo
   if (cfg->omega_dtype != RADAR_F32 && cfg->omega_dtype != RADAR_BF16) return RADAR_EINVAL;
   if (cfg->omega_dtype == RADAR_BF16 && cfg->kv_dtype != RADAR_BF16) return RADAR_EINVAL;
   s.obf = cfg->omega_dtype == RADAR_BF16;
-  if (bad16(K) || bad16(omega) || bad16(summaries) || odd16(lens0) || odd16(lens) || !lens0 != !lens)
+  if (bad16(K) || bad16(omega) || bad16(summaries) || any_off(lens0, lens) || !lens0 != !lens)
     return RADAR_EINVAL;
   if (t < 0 || t > s.cap) return RADAR_ECAPACITY;
   if (!lens) {
@@ -468,8 +672,8 @@ radar_status radar_fork(const radar_config* cfg, void* K, void* V, float* mass, 
   Shape s;
   const radar_status r = summaries ? check_index(cfg, &s) : check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
-  if (bad16(K) || bad16(V) || odd16(mass) || odd16(summaries) || bad16(src) || odd16(lens) ||
-      odd16(new_lens) || src == new_lens || first < 0)
+  if (bad16(K) || bad16(V) || odd16(mass) || odd16(summaries) || !src ||
+      any_off(src, lens, new_lens) || src == new_lens || first < 0)
     return RADAR_EINVAL;
   if (t < 0 || t > s.cap) return RADAR_ECAPACITY;
   if (s.B > RADAR_MAX_FORK) return RADAR_EUNSUPPORTED;
@@ -481,18 +685,20 @@ radar_status radar_fork(const radar_config* cfg, void* K, void* V, float* mass, 
   a.B = s.B; a.Hkv = s.Hkv; a.t = t; a.first = std::min(first, t); a.cap = s.cap;
   a.row_bytes = s.d * esize(s);
   a.n_sink = s.n_sink;
-  a.tiles[0] = std::max<int64_t>(1, ceil_div((t - a.first) * (a.row_bytes / 16), kForkTile));
-  if (mass) a.tiles[1] = ceil_div(t, kForkTile);
+  a.units[0] = (t - a.first) * (a.row_bytes / 16);
+  if (mass) a.units[1] = t;
   if (summaries) {
     a.c = s.c; a.summ_bytes = s.n * 4; a.summ_rows = std::max<int64_t>(1, s.s_cap);
     const int64_t seg0 = std::max<int64_t>(0, a.first - s.n_sink) / s.c;
     const int64_t seg1 = std::max<int64_t>(0, t - s.n_sink) / s.c;
-    a.tiles[2] = ceil_div((seg1 - seg0) * (a.summ_bytes / 16), kForkTile);
+    a.units[2] = (seg1 - seg0) * (a.summ_bytes / 16);
   }
-  const int64_t items = s.Hkv * (2 * a.tiles[0] + a.tiles[1] + a.tiles[2]);
-  const size_t lds = (size_t)s.B * 18;     // three words a sequence, and up to 3/2 in the list
-  const unsigned grid = (unsigned)std::min<int64_t>(items, 8 * num_cu());
-  launch(RADAR_K_APPEND, k_fork, dim3(grid), dim3(kForkTile), (lds + 15) / 16 * 16, stream, a);
+  const int64_t items = s.Hkv * (2 * ceil_div(a.units[0], kForkThreads) + ceil_div(a.units[1], kForkThreads) +
+                                 ceil_div(a.units[2], kForkThreads));
+  // three words a sequence (of a wave's, at least), and up to 3/2 in the list
+  const size_t lds = (size_t)std::max(s.B, kWave) * 18;
+  const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(items, 4 * num_cu()));
+  launch(RADAR_K_APPEND, k_fork, dim3(grid), dim3(kForkThreads), (lds + 15) / 16 * 16, stream, a);
   const radar_status st = launch_status();
   if (st != RADAR_OK || !in_place) return st;
   a.new_lens = new_lens;

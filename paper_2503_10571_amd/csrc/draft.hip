@@ -152,7 +152,8 @@ radar_status check_nodes(const Shape& s, int64_t nodes, bool tree) {
 }
 
 bool bad16(const void* p) { return !p || !aligned16(p); }
-bool odd16(const void* p) { return p && !aligned16(p); }
+template <typename T>
+bool off(const T* p) { return reinterpret_cast<uintptr_t>(p) % sizeof(T) != 0; }
 bool good_rows(const radar_rows* r, int esz) {
   return r && r->data && aligned16(r->data) && r->seq * esz % 16 == 0 && r->token * esz % 16 == 0 &&
          r->head * esz % 16 == 0;
@@ -181,8 +182,8 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, con
   radar_status r = check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
   const int esz = esize(s);
-  if (!good_rows(q, esz) || !good_rows(out, esz) || bad16(K) || bad16(V) || odd16(lens) || odd16(counts) ||
-      odd16(parent))
+  if (!good_rows(q, esz) || !good_rows(out, esz) || bad16(K) || bad16(V) || off(lens) || off(counts) ||
+      off(parent))
     return RADAR_EINVAL;
   r = check_nodes(s, nodes, parent != nullptr);
   if (r != RADAR_OK) return r;

@@ -325,8 +325,8 @@ void launch_rotary(const RotArgs& a, const radar_rope& rope, hipStream_t st) {
 }
 
 radar_status check_axes(int n_axes, const int32_t* axis, const int64_t* pos) {
-  return n_axes < 1 || !axis || !pos || !aligned16(axis) || !aligned16(pos) ? RADAR_EINVAL
-                                                                           : RADAR_OK;
+  const bool off = reinterpret_cast<uintptr_t>(axis) % 4 || reinterpret_cast<uintptr_t>(pos) % 8;
+  return n_axes < 1 || !axis || !pos || off ? RADAR_EINVAL : RADAR_OK;
 }
 
 radar_status run_rotary(RotArgs& a, const radar_rope& rope, radar_dtype dt, hipStream_t st) {
@@ -361,7 +361,7 @@ radar_status rotate_rows(const radar_rope* rope, int n_axes, const int32_t* axis
     return RADAR_EINVAL;
   if (n_k_heads > 0 && (!good_rows(k, esz) || !good_rows(k_out, esz))) return RADAR_EINVAL;
   if ((int64_t)n_q_heads + n_k_heads > 65535) return RADAR_EUNSUPPORTED;
-  if ((pos && !aligned16(pos)) || (lens && !aligned16(lens))) return RADAR_EINVAL;
+  if ((!axis && pos && !aligned16(pos)) || (lens && !aligned16(lens))) return RADAR_EINVAL;
   r = check_tokens(batch, tokens);
   if (r != RADAR_OK || tokens == 0) return r;
   RotArgs a{};
@@ -392,7 +392,7 @@ radar_status fill_rows(const radar_config* cfg, const radar_rope* rope, int n_ax
   if (!good_rows(k, esz) || !good_rows(v, esz) || !K || !V || !aligned16(K) || !aligned16(V))
     return RADAR_EINVAL;
   if (q && (!good_rows(q, esz) || !good_rows(q_out, esz))) return RADAR_EINVAL;
-  if ((pos && !aligned16(pos)) || (lens && !aligned16(lens)) || (rows && !aligned16(rows)))
+  if ((!axis && pos && !aligned16(pos)) || (lens && !aligned16(lens)) || (rows && !aligned16(rows)))
     return RADAR_EINVAL;
   if (s.Hq + 2 * s.Hkv > 65535) return RADAR_EUNSUPPORTED;
   r = check_tokens(s.B, tokens);

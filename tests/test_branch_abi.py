@@ -11,7 +11,7 @@ import paper_2503_10571_amd as radar
 from paper_2503_10571_amd import _build, cache_ops
 
 P = ctypes.c_void_p
-GOOD, ODD = P(0x1000), P(0x1008)
+GOOD, ODD, OFF = P(0x1000), P(0x1008), P(0x1002)
 by = ctypes.byref
 
 
@@ -44,7 +44,7 @@ def test_axes_refusals(L):
         return L.radar_rotary_axes(rope, axes, axis, batch, tokens, d, dtype, hq, q, qo, hk, k, ko, pos, lens, 0, None)
 
     assert call(axes=0) == 1 and call(axes=-1) == 1
-    assert call(axis=None) == 1 and call(axis=ODD) == 1 and call(pos=None) == 1 and call(pos=ODD) == 1
+    assert call(axis=None) == 1 and call(axis=OFF) == 1 and call(pos=None) == 1 and call(pos=P(0x1004)) == 1
     assert call(rope=None) == 1 and call(dtype=2) == 1 and call(d=136) == 3 and call(d=272) == 3
     assert call(batch=0) == 1 and call(tokens=-1) == 1 and call(tokens=1 << 31) == 3
     assert call(q=None) == 1 and call(ko=None) == 1 and call(lens=ODD) == 1
@@ -57,7 +57,7 @@ def test_axes_refusals(L):
 
     for kw, want in BAD:
         assert fill(cfg=_cfg(**kw)) == want, kw
-    assert fill(axes=0) == 1 and fill(axis=ODD) == 1 and fill(pos=None) == 1
+    assert fill(axes=0) == 1 and fill(axis=OFF) == 1 and fill(pos=None) == 1
     assert fill(row0=-1) == 2 and fill(row0=4094) == 2 and fill(K=None) == 1 and fill(rows_=ODD) == 1
     assert fill(tokens=0) == 0
 
@@ -76,8 +76,10 @@ def test_tree_refusals(L):
     assert call(t=-1) == 2 and call(t=4097) == 2 and call(t=4090) == 2 and call(t=4097, lens=GOOD) == 2
     for name in ("q", "K", "V", "out"):
         assert call(**{name: None}) == 1, name
-    for name in ("K", "V", "lens", "counts", "parent"):
+    for name in ("K", "V"):
         assert call(**{name: ODD}) == 1, name
+    for name in ("lens", "counts", "parent"):
+        assert call(**{name: OFF}) == 1, name
     for bad in ((0, 0, 0, 128), (0x1008, 4096, 4096, 128), (0x1000, 4, 4096, 128), (0x1000, 4096, 4, 128),
                 (0x1000, 4096, 4096, 4)):
         assert call(q=by(cache_ops._Rows(*bad))) == 1 and call(out=by(cache_ops._Rows(*bad))) == 1, bad
@@ -100,9 +102,10 @@ def test_accept_refusals(L):
     assert call(t=-1) == 2 and call(t=4097) == 2 and call(t=4090) == 2
     assert call(t=4097, lens=GOOD) == 2
     for name in ("K", "V", "tokens", "first", "choice", "path", "accepted", "nxt"):
-        assert call(**{name: None}) == 1 and call(**{name: ODD}) == 1, name
+        assert call(**{name: None}) == 1 and call(**{name: OFF}) == 1, name
     for name in ("lens", "counts", "parent", "new"):
-        assert call(**{name: ODD}) == 1, name
+        assert call(**{name: OFF}) == 1, name
+    assert call(K=ODD) == 1 and call(tokens=P(0x1004)) == 1
 
 
 def test_keep_refusals(L):
@@ -113,9 +116,10 @@ def test_keep_refusals(L):
         assert call(cfg=_cfg(**kw)) == want, kw
     assert call(n=-1) == 1 and call(n=4097) == 2 and call(t=-1) == 2 and call(t=4097) == 2
     for name in ("K", "V", "path"):
-        assert call(**{name: None}) == 1 and call(**{name: ODD}) == 1, name
+        assert call(**{name: None}) == 1 and call(**{name: OFF}) == 1, name
     for name in ("lens", "counts", "new"):
-        assert call(**{name: ODD}) == 1, name
+        assert call(**{name: OFF}) == 1, name
+    assert call(V=ODD) == 1
 
 
 def test_extend_index_refusals(L):
@@ -127,7 +131,7 @@ def test_extend_index_refusals(L):
     assert call(t0=-1) == 2 and call(t0=101) == 2 and call(t=4097) == 2
     for name in ("K", "omega", "summ"):
         assert call(**{name: None}) == 1 and call(**{name: ODD}) == 1, name
-    assert call(lens=GOOD) == 1 and call(lens0=GOOD) == 1 and call(lens0=ODD, lens=GOOD) == 1
+    assert call(lens=GOOD) == 1 and call(lens0=GOOD) == 1 and call(lens0=OFF, lens=GOOD) == 1
     assert call(t=255) == 0 and call(t0=256, t=511) == 0         # no segment ends there
     ragged = dict(lens0=GOOD, lens=GOOD)
     assert call(most=-1, **ragged) == 2 and call(most=4097, **ragged) == 2
@@ -152,9 +156,10 @@ def test_fork_refusals(L):
     assert call(cfg=_cfg(batch=2049, n_kv_heads=8)) == 3
     assert call(first=-1) == 1 and call(t=-1) == 2 and call(t=4097) == 2
     for name in ("K", "V", "src"):
-        assert call(**{name: None}) == 1 and call(**{name: ODD}) == 1, name
+        assert call(**{name: None}) == 1 and call(**{name: OFF}) == 1, name
     for name in ("mass", "summ", "lens", "new"):
-        assert call(**{name: ODD}) == 1, name
+        assert call(**{name: OFF}) == 1, name
+    assert call(K=ODD) == 1 and call(mass=ODD) == 1 and call(summ=ODD) == 1
     assert call(new=GOOD) == 1                                   # the new lengths over the map
 
 
