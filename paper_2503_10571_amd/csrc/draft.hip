@@ -6,18 +6,15 @@ namespace radar_impl {
 namespace {
 
 constexpr int kSlots = 512;                // workgroups that the chip holds at once
-constexpr int kFiner = 3;                  // of sequences of different lengths
-// partials of a row: a block has a step at least, and there are at most 3/2 kSlots kFiner
-// blocks where rows have more than one
-constexpr int kMaxPartials = kSlots * kFiner * 3 / 2;
+constexpr int kFew = 128;                  // partials of a row that one wave merges
 
 // A query row's output from its partials by NW waves: D / 4 lanes on four dims each of one
 // partial, the others on the next.
 //   out = sum_i acc_i 2^(m_i - m) / sum_i l_i 2^(m_i - m),  m = max_i m_i
 template <typename T, int D, int NW>
-__global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_tile, int64_t step) {
+__global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_tile) {
   constexpr int kThreads = NW * kWave, kTpp = D / 4, kGroups = kThreads / kTpp;
-  constexpr int kPer = 4 / NW, kMost = NW == 1 ? kWave : kMaxPartials;
+  constexpr int kPer = 4 / NW, kMost = NW == 1 ? kFew : kSlots + 1;
   __shared__ float f_lds[kPer][kMost];
   __shared__ float red[8];
   __shared__ __attribute__((aligned(16))) f32x4_t acc_lds[256];
@@ -33,6 +30,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
     }
   };
   const int64_t n_rows = (int64_t)a.B * a.nodes * a.Hq;
+  const int each = a.parts ? (int)((a.t + a.nodes + a.step - 1) / a.step + a.parts - 1) / a.parts : tree_each(a);
   for (int64_t x = (int64_t)blockIdx.x * kPer + own; x < n_rows; x += (int64_t)gridDim.x * kPer) {
     const int hq = (int)(x % a.Hq), node = (int)(x / a.Hq % a.nodes), hk = hq / a.G;
     const int64_t b = x / a.Hq / a.nodes, bh = b * a.Hkv + hk;
@@ -44,8 +42,13 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
     }
     if (node >= s.nodes) continue;
     const int row = node * a.G + hq % a.G;
-    const int n = (int)((tree_end(a, s, (row / rows_per_tile + 1) * rows_per_tile) + step - 1) / step);
-    const int64_t first = bh * a.splits * a.M + row;
+    int seq = (int)b;
+    const TreeCut cut = a.parts ? TreeCut{each, a.parts, (int)b * a.Hkv * a.parts} : tree_cut(a, each, false, 0, &seq);
+    if (cut.parts == 1) continue;          // written by its block
+    // the parts that begin before the end of the row tile's rows
+    const int64_t end = tree_end(a, s, (row / rows_per_tile + 1) * rows_per_tile), step = (int64_t)each * a.step;
+    const int n = (int)((end + step - 1) / step);
+    const int64_t first = ((int64_t)cut.first + hk * cut.parts) * a.M + row;
     float mx = -INFINITY;
     for (int i = tid; i < n; i += kThreads) {
       const float m = a.ml[2 * (first + (int64_t)i * a.M)];
@@ -102,35 +105,43 @@ int tree_waves(const Shape& s, int64_t M) {
   return M <= 64 ? 2 : 4;
 }
 
+// How a call is cut: as many workgroups as the chip holds at once, or fewer, with at least
+// kLeast steps each (fewer cost more in partials than they gain). Pairs of one length that
+// nearly fill the chip, and those of any that fill it twice, stay whole.
+constexpr int kLeast = 4;
+
 struct TreePlan {
-  int rw, mtiles, splits, rows_per_tile;
-  int64_t tiles, step;
+  int rw, mtiles, rows_per_tile, step, parts, units;
 };
 
 TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
   TreePlan p;
-  const int64_t M = nodes * s.G, units = (int64_t)s.B * s.Hkv;
+  const int64_t M = nodes * s.G, pairs = (int64_t)s.B * s.Hkv;
   p.rw = tree_waves(s, M);
   p.rows_per_tile = flash_rows(esize(s), p.rw);
   p.mtiles = (int)ceil_div(M, p.rows_per_tile);
-  const int ntg = flash_tile(esize(s), p.rw);
-  const int64_t steps = ceil_div(t + nodes, ntg), blocks = units * p.mtiles;
-  int64_t n = (slots() * (ragged ? kFiner : 1) + blocks / 2) / blocks;
-  n = std::max<int64_t>(1, std::min(n, steps));
-  if (steps <= 4) n = 1;
-  p.tiles = ceil_div(steps, n);
-  p.splits = (int)ceil_div(steps, p.tiles);
-  p.step = p.tiles * ntg;
+  p.step = flash_tile(esize(s), p.rw);
+  const int64_t blocks = pairs * p.mtiles, steps = ceil_div(t + nodes, p.step);
+  p.units = 0;
+  if (ragged && steps > kLeast && blocks <= 2 * slots() && pairs * steps < (1ll << 31)) {
+    // (a pair's last part is shorter: as many more parts as there are pairs, at most)
+    const int64_t units = std::max<int64_t>(1, slots() / p.mtiles);
+    p.parts = 0;
+    p.units = (int)std::max(units - pairs, (units + 1) / 2);
+  } else {
+    p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(slots() / blocks, ceil_div(steps, kLeast)));
+    // (as many of one length)
+    p.parts = (int)ceil_div(steps, ceil_div(steps, p.parts));
+  }
   return p;
 }
 
-// Partial rows of every call with at most these nodes and t: blocks of more than one split
-// are at most 3/2 of the slots (two splits where rounding gives them), with min(M, 128)
-// rows each; and no more than one for each 32 rows.
+// Partial rows of every call with at most these nodes and t: of slots / mtiles parts (or
+// one), and where lengths differ one more for each of 2 slots / mtiles pairs at most, in
+// mtiles tiles of min(M, 128) rows; and no more than one for each step of 32 rows, and one.
 int64_t most_partials(const Shape& s, int64_t nodes, int64_t t) {
-  const int64_t M = nodes * s.G, units = (int64_t)s.B * s.Hkv;
-  const int64_t by_slots = (int64_t)slots() * kFiner * 3 / 2 * std::min<int64_t>(M, 128);
-  return std::min(by_slots, units * ceil_div(t + nodes, 32) * M);
+  const int64_t M = nodes * s.G, pairs = (int64_t)s.B * s.Hkv;
+  return std::min(4ll * slots() * std::min<int64_t>(M, 128), (long long)(pairs * (ceil_div(t + nodes, 32) + 1) * M));
 }
 struct TreeWs {
   size_t acc, ml, total;
@@ -190,7 +201,7 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, con
   if (t < 0 || t > s.cap || (!lens && nodes > s.cap - t)) return RADAR_ECAPACITY;
   const TreeWs w = tree_ws(s, nodes, t);
   if (bad16(workspace) || workspace_bytes < w.total) return RADAR_EWORKSPACE;
-  const TreePlan p = plan_tree(s, nodes, t, lens != nullptr);
+  const TreePlan p = plan_tree(s, nodes, t, lens || counts);
   TreeArgs a{};
   a.q = q->data; a.q_seq = q->seq; a.q_node = q->token; a.q_head = q->head;
   a.out = out->data; a.o_seq = out->seq; a.o_node = out->token; a.o_head = out->head;
@@ -198,7 +209,8 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, con
   a.qscale = kLog2e / std::sqrt((float)s.d);
   a.K = K; a.V = V; a.lens = lens; a.counts = counts; a.t = t; a.cap = s.cap;
   a.nodes = (int)nodes; a.parent = parent; a.parent_shared = parent_shared != 0;
-  a.splits = p.splits; a.mtiles = p.mtiles; a.M = (int)(nodes * s.G); a.tiles = p.tiles;
+  a.mtiles = p.mtiles; a.M = (int)(nodes * s.G);
+  a.parts = p.parts; a.units = p.units; a.least = kLeast; a.step = p.step;
   a.acc = static_cast<float*>(workspace);
   a.ml = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + w.ml);
   if (s.dt == RADAR_BF16) {
@@ -209,17 +221,19 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, con
     else launch_tree_f32_128(a, p.rw, stream);
   }
   r = launch_status();
-  if (r != RADAR_OK || p.splits == 1) return r;
+  if (r != RADAR_OK || p.parts == 1) return r;
   const int64_t rows = (int64_t)s.B * s.Hq * nodes;
+  // (the heads of a sequence have as many each: 1 / Hkv of all, and one, at most)
+  const bool few = (p.parts ? p.parts : p.units / s.Hkv + 1) <= kFew;
   auto merge = [&](auto tag, auto d) {
     typedef decltype(tag) T;
     constexpr int D = decltype(d)::value;
-    if (p.splits <= kWave && rows > 4 * num_cu())
+    if (few && rows > 4 * num_cu())
       launch(RADAR_K_COMBINE, k_tree_merge<T, D, 1>, dim3((unsigned)std::min<int64_t>(ceil_div(rows, 4), 1 << 16)),
-             dim3(256), 0, stream, a, p.rows_per_tile, p.step);
+             dim3(256), 0, stream, a, p.rows_per_tile);
     else
       launch(RADAR_K_COMBINE, k_tree_merge<T, D, 4>, dim3((unsigned)std::min<int64_t>(rows, 1 << 16)), dim3(256), 0,
-             stream, a, p.rows_per_tile, p.step);
+             stream, a, p.rows_per_tile);
   };
   if (s.dt == RADAR_BF16) {
     if (s.d == 64) merge(bf16_t{}, std::integral_constant<int, 64>{});

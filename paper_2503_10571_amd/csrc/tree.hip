@@ -87,9 +87,11 @@ __device__ __forceinline__ void tree_bits(const TreeArgs& a, int64_t b, int node
   __syncthreads();
 }
 
-// Workgroups i and i + 8 share an XCD and its L2: an XCD gets a run of the blocks, in
-// which the row tiles of one (b, kv head, split), who read the same rows, follow one
-// another, the last of them, who in a chain attend the most, first.
+// Workgroups i and i + 8 share an XCD and its L2. The units (the parts of all pairs) go round
+// the XCDs, and a unit's row tiles, which read the same rows, follow one another on one, the
+// last of them, which in a chain attends the most, first; the blocks of the last, not whole
+// round are dealt out evenly. An XCD so gets parts of all sequences: each has about an eighth
+// of the card's bandwidth, and one with the longest sequence for itself is waited for.
 template <typename T, int D, int RW>
 __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
   using F = Flash<T, D, RW>;
@@ -99,30 +101,49 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
   __shared__ float wm[F::TW * kRows], wl[F::TW * kRows];
   __shared__ uint32_t bits[kRows * kNodeWords];
   __shared__ int odd;
-  const int total = a.B * a.Hkv * a.splits * a.mtiles, chunk = (total + 7) / 8;
-  const int i = blockIdx.x % 8 * chunk + blockIdx.x / 8;
-  if ((int)(blockIdx.x / 8) >= chunk || i >= total) return;
-  const int unit = i / a.mtiles, mt = a.mtiles - 1 - i % a.mtiles;
-  const int64_t bh = unit / a.splits, sp = unit % a.splits, b = bh / a.Hkv, hk = bh % a.Hkv;
+  const int units = a.parts ? a.B * a.Hkv * a.parts : a.units + a.B * a.Hkv, x = blockIdx.x % 8;
+  int i = blockIdx.x / 8, unit = i / a.mtiles * 8 + x;
+  if (i >= units / 8 * a.mtiles) {         // the last round
+    const int rest = units % 8 * a.mtiles, each = (rest + 7) / 8;
+    i -= units / 8 * a.mtiles;
+    if (i >= each || x * each + i >= rest) return;
+    i += x * each;
+    unit = units / 8 * 8 + i / a.mtiles;
+  }
+  const int mt = a.mtiles - 1 - i % a.mtiles;
+  int b, hk, part;
+  TreeCut cut;
+  if (a.parts) {                           // uniform
+    const int bh = unit / a.parts;
+    part = unit % a.parts;
+    b = bh / a.Hkv;
+    hk = bh % a.Hkv;
+    const int steps = (int)((a.t + a.nodes + a.step - 1) / a.step);
+    cut = {(steps + a.parts - 1) / a.parts, a.parts, 0};
+  } else {
+    cut = tree_cut(a, tree_each(a), true, unit, &b);
+    if (b < 0) return;
+    hk = (unit - cut.first) / cut.parts;
+    part = (unit - cut.first) % cut.parts;
+  }
   const TreeSeq s = tree_seq(a, b);
   const int row0 = mt * kRows, node0 = row0 / a.G;
-  const bool direct = a.splits == 1;
+  const bool direct = cut.parts == 1;
   TreeMask mask;
   mask.g_log2 = 31 - __clz(a.G);
   mask.out = static_cast<unsigned char*>(a.out) +
              (b * a.o_seq + node0 * a.o_node + hk * a.G * a.o_head) * (int64_t)sizeof(T);
   mask.o_node = a.o_node * (int64_t)sizeof(T);
   mask.o_head = a.o_head * (int64_t)sizeof(T);
-  if (s.rows < 0) {
-    if (!direct) return;
-    for (int x = threadIdx.x; x < min(kRows, a.M - row0) * D; x += 256)
-      static_cast<T*>(mask.out_row(x / D))[x % D] = from_f32<T>(__uint_as_float(0x7fc00000u));
+  if (s.rows < 0) {                        // (parts = 1: else the merge does it)
+    for (int y = threadIdx.x; y < min(kRows, a.M - row0) * D; y += 256)
+      static_cast<T*>(mask.out_row(y / D))[y % D] = from_f32<T>(__uint_as_float(0x7fc00000u));
     return;
   }
   const int rows = min(kRows, s.nodes * a.G - row0);
   if (rows <= 0) return;
-  const int64_t end = tree_end(a, s, row0 + rows), step = a.tiles * F::NTG;
-  const int64_t r0 = sp * step, r1 = min(end, r0 + step);
+  const int64_t end = tree_end(a, s, row0 + rows), step = (int64_t)cut.each * F::NTG;
+  const int64_t r0 = part * step, r1 = min(end, r0 + step);
   if (r0 >= end) return;
   mask.from = s.rows + (a.parent ? 0 : node0 + 1);
   mask.rows = s.rows;
@@ -136,7 +157,7 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
     else __syncthreads();
   }
   const T* q = static_cast<const T*>(a.q) + b * a.q_seq + node0 * a.q_node + hk * a.G * a.q_head;
-  const int64_t at = (bh * a.splits + sp) * a.M + row0;
+  const int64_t bh = (int64_t)b * a.Hkv + hk, at = (int64_t)unit * a.M + row0;
   auto block = [&](auto once) {
     F::template block<false, false, decltype(once)::value>(
         static_cast<const T*>(a.K) + bh * a.cap * D, static_cast<const T*>(a.V) + bh * a.cap * D, r0, r1, rows,
@@ -156,7 +177,8 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
 
 template <typename T, int D>
 void launch_tree(const TreeArgs& a, int rw, hipStream_t st) {
-  const dim3 grid((unsigned)(ceil_div((int64_t)a.B * a.Hkv * a.splits * a.mtiles, 8) * 8)), block(256);
+  const int64_t pairs = (int64_t)a.B * a.Hkv, units = a.parts ? pairs * a.parts : a.units + pairs;
+  const dim3 grid((unsigned)(8 * (units / 8 * a.mtiles + ceil_div(units % 8 * a.mtiles, 8)))), block(256);
   if (rw == 1) launch(RADAR_K_ATTEND, k_tree<T, D, 1>, grid, block, 0, st, a);
   else if (rw == 2) launch(RADAR_K_ATTEND, k_tree<T, D, 2>, grid, block, 0, st, a);
   else launch(RADAR_K_ATTEND, k_tree<T, D, 4>, grid, block, 0, st, a);

@@ -6,10 +6,13 @@
 
 namespace radar_impl {
 
-// A call is cut into blocks (b, kv head, split, row tile), one workgroup each: flash_rows
-// of the pair's query rows i G + g (node i, head g of the group) against `tiles` steps of
-// its cache rows. With one split a block leaves the outputs, with more a partial (max, sum,
-// acc[d]) for each row.
+// Query rows i G + g (node i, head g of the group) of a pair (b, kv head) are taken
+// flash_rows at a time, a row tile, over the pair's cache rows in steps of flash_tile. The
+// steps of a pair are cut into parts, a workgroup for each and row tile: as many for each
+// pair (parts > 0), or, for sequences of different lengths (parts = 0), parts of one number
+// of steps, about 1 / units of all, which every workgroup finds by adding up the lengths. A
+// pair of one part gets its outputs there, else each part leaves a partial (max, sum,
+// acc[d]) for each row, in the place of the part among all.
 struct TreeArgs {
   const void* q;             // [B][nodes][Hq][d], strides in elements
   void* out;
@@ -22,9 +25,9 @@ struct TreeArgs {
   int nodes;
   const int* parent;         // [B][nodes], or [nodes] if shared; null: a chain
   int parent_shared;
-  int splits, mtiles, M;     // M = nodes G query rows of a pair
-  int64_t tiles;
-  float *acc, *ml;           // [B Hkv][splits][M][d], [..][M][2]
+  int mtiles, M;             // M = nodes G query rows of a pair
+  int parts, units, least, step;       // least: steps of a part, at least; step: its rows
+  float *acc, *ml;           // [parts of all pairs][M][d], [..][M][2]
 };
 
 // a sequence's rows and nodes; rows < 0: its length or count is invalid
@@ -40,6 +43,54 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& a, int64_t b) {
 // the end of the rows that a tile's query rows, the last of them row1 - 1, attend
 __device__ __forceinline__ int64_t tree_end(const TreeArgs& a, const TreeSeq& s, int row1) {
   return s.rows + (min(row1, s.nodes * a.G) - 1) / a.G + 1;
+}
+
+__device__ __forceinline__ int tree_steps(const TreeArgs& a, const TreeSeq& s) {
+  return s.nodes > 0 ? (int)((s.rows + s.nodes + a.step - 1) / a.step) : 0;
+}
+
+// the sum of x over the lanes up to this one
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);     // row_shr:1 ..
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);     // row_bcast:15
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);     // row_bcast:31
+  return x;
+}
+
+// Where a pair's parts are among all: `each` steps in one, and for one sequence the number
+// of parts of a head, and how many come before its first. (All steps fit 31 bits.)
+struct TreeCut {
+  int each, parts, first;
+};
+// steps of a part of a ragged batch; the same in every wave
+__device__ __forceinline__ int tree_each(const TreeArgs& a) {
+  int total = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kWave) {
+    const int b = b0 + (threadIdx.x & 63);
+    total += __builtin_amdgcn_readlane(wave_scan(b < a.B ? tree_steps(a, tree_seq(a, b)) : 0), kWave - 1);
+  }
+  return max(a.least, (int)(((int64_t)total * a.Hkv + a.units - 1) / a.units));
+}
+// of sequence b; or, by_part, of the one that part x of all lies in, which becomes b (-1: none)
+__device__ __forceinline__ TreeCut tree_cut(const TreeArgs& a, int each, bool by_part, int x, int* b) {
+  int before = 0;
+  for (int b0 = 0; b0 < a.B; b0 += kWave) {
+    const int lane = threadIdx.x & 63, i = b0 + lane;
+    const int own = i < a.B ? (tree_steps(a, tree_seq(a, i)) + each - 1) / each : 0;
+    const int sum = wave_scan(own * a.Hkv);
+    const u64 hit = __ballot(by_part ? x < before + sum : i == *b);
+    if (hit) {                             // uniform
+      const int l = __ffsll(hit) - 1, parts = __builtin_amdgcn_readlane(own, l);
+      *b = b0 + l;
+      return {each, parts, before + __builtin_amdgcn_readlane(sum, l) - parts * a.Hkv};
+    }
+    before += __builtin_amdgcn_readlane(sum, kWave - 1);
+  }
+  *b = -1;
+  return {each, 0, 0};
 }
 
 // tree.hip: rw in {1, 2, 4} row waves
