@@ -15,7 +15,7 @@ template <typename T, int D, int NW>
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_tile) {
   constexpr int kThreads = NW * kWave, kTpp = D / 4, kGroups = kThreads / kTpp;
   constexpr int kPer = 4 / NW, kMost = NW == 1 ? kFew : kSlots + 1;
-  __shared__ float f_lds[kPer][kMost];
+  __shared__ float f_lds[kPer][kMost], l_lds[kPer][kMost];
   __shared__ float red[8];
   __shared__ __attribute__((aligned(16))) f32x4_t acc_lds[256];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
@@ -29,11 +29,11 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
       __syncthreads();
     }
   };
-  const int64_t n_rows = (int64_t)a.B * a.nodes * a.Hq;
-  const int each = a.parts ? (int)((a.t + a.nodes + a.step - 1) / a.step + a.parts - 1) / a.parts : tree_each(a);
-  for (int64_t x = (int64_t)blockIdx.x * kPer + own; x < n_rows; x += (int64_t)gridDim.x * kPer) {
-    const int hq = (int)(x % a.Hq), node = (int)(x / a.Hq % a.nodes), hk = hq / a.G;
-    const int64_t b = x / a.Hq / a.nodes, bh = b * a.Hkv + hk;
+  const int n_rows = a.B * a.nodes * a.Hq;   // below 2^27
+  const int each = a.parts ? ((int)((a.t + a.nodes - 1) >> a.step_log2) + a.parts) / a.parts : tree_each(a);
+  for (int x = blockIdx.x * kPer + own; x < n_rows; x += gridDim.x * kPer) {
+    const int hq = x % a.Hq, node = x / a.Hq % a.nodes, hk = hq >> a.g_log2;
+    const int64_t b = x / a.Hq / a.nodes;
     const TreeSeq s = tree_seq(a, b);
     T* o = static_cast<T*>(a.out) + b * a.o_seq + node * a.o_node + hq * a.o_head;
     if (s.rows < 0) {
@@ -41,19 +41,30 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
       continue;
     }
     if (node >= s.nodes) continue;
-    const int row = node * a.G + hq % a.G;
+    const int row = node * a.G + (hq & (a.G - 1));
     int seq = (int)b;
     const TreeCut cut = a.parts ? TreeCut{each, a.parts, (int)b * a.Hkv * a.parts} : tree_cut(a, each, false, 0, &seq);
     if (cut.parts == 1) continue;          // written by its block
     // the parts that begin before the end of the row tile's rows
-    const int64_t end = tree_end(a, s, (row / rows_per_tile + 1) * rows_per_tile), step = (int64_t)each * a.step;
-    const int n = (int)((end + step - 1) / step);
+    const int64_t end = tree_end(a, s, (row / rows_per_tile + 1) * rows_per_tile);
+    const int n = (int)((uint32_t)((int)((end - 1) >> a.step_log2) + each) / (uint32_t)each);
     const int64_t first = ((int64_t)cut.first + hk * cut.parts) * a.M + row;
+    // the accumulators' first loads go out with those of m and l
+    constexpr int kAhead = 4;
+    const int grp = tid / kTpp, e = tid % kTpp;
+    auto piece = [&](int i) {
+      return *reinterpret_cast<const f32x4_t*>(a.acc + (first + (int64_t)i * a.M) * D + 4 * e);
+    };
+    f32x4_t ahead[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (grp + j * kGroups < n) ahead[j] = piece(grp + j * kGroups);
     float mx = -INFINITY;
     for (int i = tid; i < n; i += kThreads) {
-      const float m = a.ml[2 * (first + (int64_t)i * a.M)];
-      f_lds[own][i] = m;
-      mx = fmaxf(mx, m);
+      const float2 ml = *reinterpret_cast<const float2*>(a.ml + 2 * (first + (int64_t)i * a.M));
+      f_lds[own][i] = ml.x;
+      l_lds[own][i] = ml.y;
+      mx = fmaxf(mx, ml.x);
     }
     mx = wave_max(mx);
     if constexpr (NW > 1) {
@@ -65,7 +76,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
     for (int i = tid; i < n; i += kThreads) {
       const float f = f_lds[own][i] == -INFINITY ? 0.f : fast_exp2(f_lds[own][i] - mx);
       f_lds[own][i] = f;
-      ls = fmaf(a.ml[2 * (first + (int64_t)i * a.M) + 1], f, ls);
+      ls = fmaf(l_lds[own][i], f, ls);
     }
     ls = wave_sum(ls);
     if constexpr (NW > 1) {
@@ -73,15 +84,16 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
     }
     sync();
     if constexpr (NW > 1) ls = (red[4] + red[5]) + (red[6] + red[7]);
-    const int grp = tid / kTpp, e = tid % kTpp;
     f32x4_t v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = grp; i < n; i += kGroups) {
-      const f32x4_t p = *reinterpret_cast<const f32x4_t*>(a.acc + (first + (int64_t)i * a.M) * D + 4 * e);
-      const float f = f_lds[own][i];
+    auto add = [&](const f32x4_t& p, float f) {
 #pragma unroll
       for (int k = 0; k < 4; ++k) v[k] = fmaf(p[k], f, v[k]);
-    }
+    };
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j)
+      if (grp + j * kGroups < n) add(ahead[j], f_lds[own][grp + j * kGroups]);
+#pragma unroll 4
+    for (int i = grp + kAhead * kGroups; i < n; i += kGroups) add(piece(i), f_lds[own][i]);
     acc_lds[threadIdx.x] = v;
     sync();
     const float* y = reinterpret_cast<const float*>(acc_lds + own * kThreads);
@@ -95,6 +107,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
   }
 }
 
+int log2_of(int n) { return n > 1 ? 1 + log2_of(n / 2) : 0; }
 int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
 int slots() { return std::min(kSlots, 2 * num_cu()); }
 
@@ -106,9 +119,11 @@ int tree_waves(const Shape& s, int64_t M) {
 }
 
 // How a call is cut: as many workgroups as the chip holds at once, or fewer, with at least
-// kLeast steps each (fewer cost more in partials than they gain). Pairs of one length that
-// nearly fill the chip, and those of any that fill it twice, stay whole.
-constexpr int kLeast = 4;
+// kLeast rows each (fewer cost more in partials than they gain: four sequences of 2000 rows
+// and 16 nodes, 32 query heads: 21.1 us, with 128 rows 25.9; one of 4096 and 8 nodes: 15.5,
+// with 512 rows 17.4). Pairs of one length that nearly fill the chip, those of any that
+// fill it twice and those of up to kShort steps stay whole.
+constexpr int kLeast = 256, kShort = 4;
 
 struct TreePlan {
   int rw, mtiles, rows_per_tile, step, parts, units;
@@ -123,13 +138,14 @@ TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
   p.step = flash_tile(esize(s), p.rw);
   const int64_t blocks = pairs * p.mtiles, steps = ceil_div(t + nodes, p.step);
   p.units = 0;
-  if (ragged && steps > kLeast && blocks <= 2 * slots() && pairs * steps < (1ll << 31)) {
+  if (ragged && steps > kShort && blocks <= 2 * slots() && pairs * steps < (1ll << 31)) {
     // (a pair's last part is shorter: as many more parts as there are pairs, at most)
     const int64_t units = std::max<int64_t>(1, slots() / p.mtiles);
     p.parts = 0;
     p.units = (int)std::max(units - pairs, (units + 1) / 2);
   } else {
-    p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(slots() / blocks, ceil_div(steps, kLeast)));
+    p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(slots() / blocks, ceil_div(t + nodes, kLeast)));
+    if (steps <= kShort) p.parts = 1;
     // (as many of one length)
     p.parts = (int)ceil_div(steps, ceil_div(steps, p.parts));
   }
@@ -210,7 +226,8 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, con
   a.K = K; a.V = V; a.lens = lens; a.counts = counts; a.t = t; a.cap = s.cap;
   a.nodes = (int)nodes; a.parent = parent; a.parent_shared = parent_shared != 0;
   a.mtiles = p.mtiles; a.M = (int)(nodes * s.G);
-  a.parts = p.parts; a.units = p.units; a.least = kLeast; a.step = p.step;
+  a.parts = p.parts; a.units = p.units; a.least = kLeast / p.step;
+  a.g_log2 = log2_of(s.G); a.step_log2 = log2_of(p.step);
   a.acc = static_cast<float*>(workspace);
   a.ml = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + w.ml);
   if (s.dt == RADAR_BF16) {

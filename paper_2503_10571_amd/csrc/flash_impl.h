@@ -322,8 +322,10 @@ __device__ __forceinline__ void store4(float* o, float a, float b, float c, floa
   *reinterpret_cast<float4*>(o) = make_float4(a, b, c, d);
 }
 __device__ __forceinline__ void store4(bf16_t* o, float a, float b, float c, float d) {
-  *reinterpret_cast<uint2*>(o) =
-      make_uint2(f32_to_bf16(a) | f32_to_bf16(b) << 16, f32_to_bf16(c) | f32_to_bf16(d) << 16);
+  bf16x2v_t lo, hi;                        // one conversion instruction each, to nearest even
+  lo[0] = (__bf16)a; lo[1] = (__bf16)b;
+  hi[0] = (__bf16)c; hi[1] = (__bf16)d;
+  *reinterpret_cast<uint2*>(o) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, hi));
 }
 
 // A workgroup of four waves. RW = 1: every wave takes the same query rows (up to
@@ -361,9 +363,10 @@ struct Flash {
   //
   // With a MASK (kOn) the rows from mask.from on are not for every query row: bit j of
   // mask.word(i, x) says whether row i attends row x + j. Elements of V there that are no
-  // finite numbers would reach the others as 0 times them, so they are zeros in LDS,
-  // counted by mask.found, and mask.settle adds them, in the end, to those who attend
-  // them. mask.finish(i, l) may change a row's sum.
+  // finite numbers would reach the others as 0 times them, so they are zeros in LDS, noted
+  // by mask.found, and make NaN, in the end, of the dims of those who attend them.
+  // mask.finish(i, l) may change a row's sum. With mask.direct the outputs, not the
+  // partials, go to mask.out_row(i).
   template <bool LOG, bool BOTH, bool ONCE, typename RowQ, typename MASK = Unmasked>
   __device__ static __forceinline__ void block(const T* __restrict__ K, const T* __restrict__ V,
                                                int64_t r0, int64_t r1, int rows, float qscale,
@@ -581,14 +584,13 @@ struct Flash {
         if (mask.any_found() && tw == 0) {
 #pragma unroll 1
           for (int64_t r = max(r0, mask.from); r < r1; ++r) {
-            const bool on = mask.word(row_in, r) & 1;
+            if (!(mask.word(row_in, r) & 1)) continue;
+            // (0 times an element: nothing, or NaN)
 #pragma unroll
             for (int db = 0; db < NDB; ++db)
 #pragma unroll
-              for (int i = 0; i < kAccVals; ++i) {
-                const float v = to_f32<T>(V[r * D + O::kDims * db + O::dim_of(i, lane)]);
-                if (on && !__builtin_isfinite(v)) acc[db][i] += v;
-              }
+              for (int i = 0; i < kAccVals; ++i)
+                acc[db][i] = fmaf(to_f32<T>(V[r * D + O::kDims * db + O::dim_of(i, lane)]), 0.f, acc[db][i]);
           }
         }
         l = mask.finish(row_in, l);
@@ -601,12 +603,13 @@ struct Flash {
       if constexpr (MASK::kOn) {
         if (mask.direct) {                       // uniform
           T* o = static_cast<T*>(mask.out_row(row));
+          const float f = 1.f / l;
 #pragma unroll
           for (int db = 0; db < NDB; ++db)
 #pragma unroll
             for (int i = 0; i < kAccVals; i += 4)
-              store4(o + O::kDims * db + O::dim_of(i, lane), acc[db][i] / l, acc[db][i + 1] / l,
-                     acc[db][i + 2] / l, acc[db][i + 3] / l);
+              store4(o + O::kDims * db + O::dim_of(i, lane), acc[db][i] * f, acc[db][i + 1] * f,
+                     acc[db][i + 2] * f, acc[db][i + 3] * f);
           return;
         }
       }
@@ -652,7 +655,8 @@ struct Flash {
         }
         if constexpr (MASK::kOn) {
           if (mask.direct) {                     // uniform
-            store4(static_cast<T*>(mask.out_row(r)) + 4 * c, a.x / L, a.y / L, a.z / L, a.w / L);
+            const float f = 1.f / L;
+            store4(static_cast<T*>(mask.out_row(r)) + 4 * c, a.x * f, a.y * f, a.z * f, a.w * f);
             continue;
           }
         }

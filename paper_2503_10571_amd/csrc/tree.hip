@@ -54,34 +54,50 @@ struct TreeMask {
 };
 
 // The bits of nodes [node0, node0 + n): node i's are its own, its parent's, .. up to a
-// root. A thread walks up from each, and takes a run of nodes that each follow the one
-// before (up to 32, a word's) at once: `runs` marks those nodes.
-__device__ __forceinline__ void tree_bits(const TreeArgs& a, int64_t b, int nodes, int node0, int n,
+// root. A thread walks up from each, over a run of nodes that each follow the one before
+// (up to 32, a word's) at once: of every node LDS holds where its run begins and the parent
+// of that one, plus 2. own: this thread's parents, of nodes tid and tid + 256.
+constexpr int kOwn = RADAR_MAX_TREE / 256;
+__device__ __forceinline__ void tree_bits(const int (&own)[kOwn], int nodes, int node0, int n,
                                           unsigned char* lds, uint32_t* bits) {
-  int* par = reinterpret_cast<int*>(lds);
-  u64* runs = reinterpret_cast<u64*>(lds + RADAR_MAX_TREE * 4);
-  const int tid = threadIdx.x;
-  const int* list = a.parent + (a.parent_shared ? 0 : b * a.nodes);
-  for (int i = tid; i < (nodes + 63) / 64 * 64; i += 256) {
-    const int p = i < nodes ? list[i] : -2;
-    const bool good = p >= -1 && p < i;
-    par[i] = good ? p : -2;
-    const u64 run = __ballot(good && p == i - 1);
-    if ((tid & 63) == 0) runs[i / 64] = run;
+  int* up = reinterpret_cast<int*>(lds);           // parent + 2, then run begin << 16 | its parent + 2
+  const int tid = threadIdx.x, lane = tid & 63;
+  int begin[kOwn];
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) {
+    const int i = tid + 256 * k;
+    const bool good = i < nodes && own[k] >= -1 && own[k] < i;
+    const u64 runs = __ballot(good && own[k] == i - 1);
+    const uint32_t word = (uint32_t)(lane < 32 ? runs : runs >> 32);
+    const uint32_t breaks = ~word & ((2u << (i & 31)) - 1);
+    begin[k] = (i & ~31) + (breaks ? 31 - __clz(breaks) : 0);
+    up[i] = good ? own[k] + 2 : 0;
   }
   __syncthreads();
-  const uint32_t* run = reinterpret_cast<const uint32_t*>(runs);
+  int jump[kOwn];
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) jump[k] = begin[k] << 16 | up[begin[k]];
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < kOwn; ++k) up[tid + 256 * k] = jump[k];
+  __syncthreads();
   for (int k = tid; k < n; k += 256) {
     uint32_t* o = bits + k * kNodeWords;
     o[0] = ~0u;
     for (int i = 1; i < kTreeWords + 3; ++i) o[i] = 0;
-    int p = node0 + k;
+    uint32_t word = 0;
+    int p = node0 + k, at = p >> 5;
     while (p >= 0) {                       // p descends
-      const uint32_t upto = (2u << (p & 31)) - 1, breaks = ~run[p >> 5] & upto;
-      const int s = breaks ? 31 - __clz(breaks) : 0;
-      o[1 + (p >> 5)] |= upto & ~((1u << s) - 1);
-      p = par[(p & ~31) + s];
+      const int j = up[p], s = j >> 16;
+      if (p >> 5 != at) {
+        o[1 + at] = word;
+        word = 0;
+        at = p >> 5;
+      }
+      word |= ((2u << (p & 31)) - 1) & ~((1u << (s & 31)) - 1);
+      p = (j & 0xffff) - 2;
     }
+    o[1 + at] = word;
     o[kTreeWords + 3] = p == -2;
   }
   __syncthreads();
@@ -118,7 +134,7 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
     part = unit % a.parts;
     b = bh / a.Hkv;
     hk = bh % a.Hkv;
-    const int steps = (int)((a.t + a.nodes + a.step - 1) / a.step);
+    const int steps = (int)((a.t + a.nodes - 1) >> a.step_log2) + 1;
     cut = {(steps + a.parts - 1) / a.parts, a.parts, 0};
   } else {
     cut = tree_cut(a, tree_each(a), true, unit, &b);
@@ -126,11 +142,18 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
     hk = (unit - cut.first) / cut.parts;
     part = (unit - cut.first) % cut.parts;
   }
+  int own[kOwn] = {};                      // (asked for along with the lengths)
+  if (a.parent)
+#pragma unroll
+    for (int k = 0; k < kOwn; ++k) {
+      const int i = threadIdx.x + 256 * k;
+      if (i < a.nodes) own[k] = a.parent[(a.parent_shared ? 0 : (int64_t)b * a.nodes) + i];
+    }
   const TreeSeq s = tree_seq(a, b);
-  const int row0 = mt * kRows, node0 = row0 / a.G;
+  const int row0 = mt * kRows, node0 = row0 >> a.g_log2;
   const bool direct = cut.parts == 1;
   TreeMask mask;
-  mask.g_log2 = 31 - __clz(a.G);
+  mask.g_log2 = a.g_log2;
   mask.out = static_cast<unsigned char*>(a.out) +
              (b * a.o_seq + node0 * a.o_node + hk * a.G * a.o_head) * (int64_t)sizeof(T);
   mask.o_node = a.o_node * (int64_t)sizeof(T);
@@ -153,7 +176,7 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
   mask.direct = direct;
   if (r1 > mask.from) {                    // uniform
     if (threadIdx.x == 0) odd = 0;
-    if (a.parent) tree_bits(a, b, s.nodes, node0, (rows + a.G - 1) / a.G, lds, bits);
+    if (a.parent) tree_bits(own, s.nodes, node0, (rows + a.G - 1) >> a.g_log2, lds, bits);
     else __syncthreads();
   }
   const T* q = static_cast<const T*>(a.q) + b * a.q_seq + node0 * a.q_node + hk * a.G * a.q_head;

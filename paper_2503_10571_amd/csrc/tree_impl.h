@@ -26,7 +26,8 @@ struct TreeArgs {
   const int* parent;         // [B][nodes], or [nodes] if shared; null: a chain
   int parent_shared;
   int mtiles, M;             // M = nodes G query rows of a pair
-  int parts, units, least, step;       // least: steps of a part, at least; step: its rows
+  int parts, units, least, g_log2;     // least: steps of a part, at least
+  int step_log2;             // rows of a step
   float *acc, *ml;           // [parts of all pairs][M][d], [..][M][2]
 };
 
@@ -42,11 +43,11 @@ __device__ __forceinline__ TreeSeq tree_seq(const TreeArgs& a, int64_t b) {
 }
 // the end of the rows that a tile's query rows, the last of them row1 - 1, attend
 __device__ __forceinline__ int64_t tree_end(const TreeArgs& a, const TreeSeq& s, int row1) {
-  return s.rows + (min(row1, s.nodes * a.G) - 1) / a.G + 1;
+  return s.rows + ((min(row1, s.nodes * a.G) - 1) >> a.g_log2) + 1;
 }
 
 __device__ __forceinline__ int tree_steps(const TreeArgs& a, const TreeSeq& s) {
-  return s.nodes > 0 ? (int)((s.rows + s.nodes + a.step - 1) / a.step) : 0;
+  return s.nodes > 0 ? (int)((s.rows + s.nodes - 1) >> a.step_log2) + 1 : 0;
 }
 
 // the sum of x over the lanes up to this one
@@ -72,14 +73,15 @@ __device__ __forceinline__ int tree_each(const TreeArgs& a) {
     const int b = b0 + (threadIdx.x & 63);
     total += __builtin_amdgcn_readlane(wave_scan(b < a.B ? tree_steps(a, tree_seq(a, b)) : 0), kWave - 1);
   }
-  return max(a.least, (int)(((int64_t)total * a.Hkv + a.units - 1) / a.units));
+  const uint32_t all = (uint32_t)total * a.Hkv;
+  return max(a.least, (int)((all + a.units - 1) / (uint32_t)a.units));
 }
 // of sequence b; or, by_part, of the one that part x of all lies in, which becomes b (-1: none)
 __device__ __forceinline__ TreeCut tree_cut(const TreeArgs& a, int each, bool by_part, int x, int* b) {
   int before = 0;
   for (int b0 = 0; b0 < a.B; b0 += kWave) {
     const int lane = threadIdx.x & 63, i = b0 + lane;
-    const int own = i < a.B ? (tree_steps(a, tree_seq(a, i)) + each - 1) / each : 0;
+    const int own = i < a.B ? (int)((uint32_t)(tree_steps(a, tree_seq(a, i)) + each - 1) / (uint32_t)each) : 0;
     const int sum = wave_scan(own * a.Hkv);
     const u64 hit = __ballot(by_part ? x < before + sum : i == *b);
     if (hit) {                             // uniform
