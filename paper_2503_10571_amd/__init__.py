@@ -542,7 +542,9 @@ class RadarLayer:
     number of tokens seen from then on. accumulate() and evict() make room in
     a full cache by the weights that its rows get; only accumulate() gathers
     them, by an exact pass over the whole cache (step() and decode() read a few
-    segments and add nothing)."""
+    segments and add nothing). draft() attends drafted tokens, whose rows stay
+    behind the cache's until accept() or keep() takes some of them in or others
+    replace them; fork() copies sequences onto others."""
 
     def __init__(self, cfg: Config, omega, K=None, V=None, t: int = 0,
                  top_k: int = 16, device="cuda", schedule: str = "fixed",
@@ -591,35 +593,101 @@ class RadarLayer:
         if self.t > 0:
             build_index(self.cfg, self.K, self.omega, self.t, self.summaries)
 
-    def prefill(self, k, v, q=None, q_out=None):
-        """A chunk of tokens behind the cache's rows: k, v [B][T][Hkv][d],
-        rotated with rope, and the index of all rows. With q [B][T][Hq][d]
-        returns its rotation too (without rope q itself, or q_out with q's
-        values). The index is built from row 0 every time: few long chunks cost
-        less than many short ones."""
+    def _fill(self, what, k, v, q, q_out, pos):
+        """k, v (and q's rotation) of a chunk into the rows from t on."""
         cfg, T = self.cfg, k.shape[1]
         for x, name in ((k, "k"), (v, "v")):
             if x.dtype != cfg.dtype or x.shape != (cfg.batch, T, cfg.n_kv_heads, cfg.head_dim):
                 raise ValueError(f"{name} must be {cfg.dtype} [{cfg.batch}][T][{cfg.n_kv_heads}]"
                                  f"[{cfg.head_dim}], got {x.dtype} {list(x.shape)}")
         if self.rope is not None:
-            q = rotary_fill(cfg, self.rope, self.K, self.V, k, v, self.t, pos=self.pos,
-                            q=q, q_out=q_out)
+            q = rotary_fill(cfg, self.rope, self.K, self.V, k, v, self.t, pos=pos, q=q, q_out=q_out)
         else:
-            cache_ops._no_gradient("prefill", k, v, self.K, self.V)
+            cache_ops._no_gradient(what, k, v, self.K, self.V)
             if q_out is not None and (q is None or q_out.shape != q.shape or
                                       q_out.dtype != q.dtype):
                 raise ValueError("q_out must have q's shape and type")
             if self.t + T > cfg.capacity:
-                raise RadarError("prefill", 2)
+                raise RadarError(what, 2)
             if q_out is not None:
                 q = q_out.copy_(q)
             self.K[:, :, self.t:self.t + T].copy_(k.transpose(1, 2))
             self.V[:, :, self.t:self.t + T].copy_(v.transpose(1, 2))
+        return q
+
+    def prefill(self, k, v, q=None, q_out=None, pos=None, next_pos: int | None = None):
+        """A chunk of tokens behind the cache's rows: k, v [B][T][Hkv][d],
+        rotated with rope, and the index of all rows. With q [B][T][Hq][d]
+        returns its rotation too (without rope q itself, or q_out with q's
+        values). The index is built from row 0 every time: few long chunks cost
+        less than many short ones. pos: the tokens' positions as rotary() takes
+        them (of several axes, for a picture), the next ones in order if None;
+        next_pos: the position of the token behind the chunk, T more than
+        before it if None."""
+        if self.rope is None and (pos is not None or next_pos is not None):
+            raise ValueError("positions without rope")
+        T = k.shape[1]
+        q = self._fill("prefill", k, v, q, q_out, self.pos if pos is None else pos)
         self.t += T
-        self.pos += T
+        self.pos = self.pos + T if next_pos is None else next_pos
         self._reindex()
         return q
+
+    def draft(self, q, k, v, parent=None, depth=None, out=None):
+        """Exact attention of N drafted tokens over the whole cache and the tokens
+        that each of them follows (attend_tree): q [B][N][Hq][d], k, v
+        [B][N][Hkv][d]; parent as for attend_tree (None: a chain). With rope, depth
+        (int64 [N] or [B][N]; of several axes [axes][B][N]) is how far each token
+        is behind the next position, 0 for the first; a chain needs none. Their
+        rows lie behind the cache's, for accept() or keep(); the cache, its index and its
+        length are as before, and another draft replaces them."""
+        cfg, N = self.cfg, k.shape[1]
+        pos = self.pos
+        if self.rope is not None and depth is not None:
+            pos = depth + self.pos
+            if pos.dim() == 1:
+                pos = pos.expand(cfg.batch, N).contiguous()
+        elif self.rope is not None and parent is not None:
+            raise ValueError("the depth of a tree's tokens is needed with rope")
+        q = self._fill("draft", k, v, q, None, pos)
+        return attend_tree(self.cfg, q, self.K, self.V, self.t, parent=parent, out=out)
+
+    def keep(self, path) -> None:
+        """Takes the last draft's tokens of path (int32 [B][n], every sequence's
+        from its first token down: ascending) into the cache, and completes the
+        index."""
+        n, c, t = path.shape[1], self.cfg.seg_len, self.t
+        keep_path(self.cfg, self.K, self.V, t, path)
+        self.t += n
+        self.pos += n
+        if self.schedule == "sqrt":
+            if self._cfg_at(max(self.t, 1)).seg_len != c:
+                self._reindex()
+                self.restructures += 1
+                return
+            self.cfg = self._cfg_at(max(self.t, 1))
+        extend_index(self.cfg, self.K, self.omega, t, self.t, self.summaries)
+
+    def accept(self, tokens, first, choice, parent=None):
+        """keep() of the last draft's tokens that the model agrees with, as
+        accept_tree() finds them from tokens, first and choice: as many for every
+        sequence as for the one with the fewest (a layer's sequences are of one
+        length; the number is read back from the device). Returns it and the token
+        that follows in each sequence (int64 [B])."""
+        path, found, after = accept_tree(self.cfg, None, None, self.t, tokens, first, choice,
+                                         parent=parent)
+        n = int(found.min())
+        if n < path.shape[1]:
+            then = tokens.gather(1, path[:, n:n + 1].clamp(min=0).long())[:, 0]
+            after = torch.where(found > n, then, after)
+        self.keep(path[:, :n].contiguous())
+        return n, after
+
+    def fork(self, src, first: int = 0) -> None:
+        """Sequence b becomes what sequence src[b] is (int64 [B], see fork()): its
+        rows from `first` on, its weights and its summaries."""
+        fork(self.cfg, self.K, self.V, src, self.t, first=first, mass=self.mass,
+             summaries=self.summaries)
 
     def append(self, k_new, v_new):
         if self.rope is not None:

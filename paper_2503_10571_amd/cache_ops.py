@@ -606,11 +606,14 @@ def accept_tree(cfg: Config, K, V, t: int, tokens, first, choice, parent=None, c
     model agrees with: first (int64 [B]) is what it chose after the sequence,
     choice (int64 [B][N]) what after each node. parent (int32 [N] for all, or
     [B][N]; None: a chain) and counts (int64 [B]) as for attend_tree(). The rows
-    of the path move up to the sequence's end; new_lens (int64 [B], may be lens)
-    receives the new lengths. Returns (path int32 [B][N], -1 behind its nodes;
+    of the path move up to the sequence's end (K and V None: none do); new_lens
+    (int64 [B], may be lens) receives the new lengths. Returns (path int32 [B][N], -1 behind its nodes;
     how many int64 [B]; the model's next token int64 [B]). The summaries do not
     follow: extend_index()."""
-    _cache(cfg, K, V)
+    if (K is None) != (V is None):
+        raise ValueError("K and V come together")
+    if K is not None:
+        _cache(cfg, K, V)
     if tokens.dim() != 2 or tokens.shape[0] != cfg.batch:
         raise ValueError(f"tokens must be [{cfg.batch}][nodes], got {list(tokens.shape)}")
     B, N = tokens.shape

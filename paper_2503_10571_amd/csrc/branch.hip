@@ -124,7 +124,7 @@ __global__ __launch_bounds__(1024) void k_accept(PathArgs a) {
   __syncthreads();
   const int n = n_path;
   for (int i = tid; i < a.nodes; i += blockDim.x) a.path[b * a.nodes + i] = i < n ? path[i] : -1;
-  move_rows(a, b, at, n, [&](int i) { return path[i]; });
+  if (a.K) move_rows(a, b, at, n, [&](int i) { return path[i]; });
 }
 
 // The same move along a given path: the first wave looks it over.
@@ -596,7 +596,7 @@ radar_status radar_accept_tree(const radar_config* cfg, void* K, void* V, int64_
   Shape s;
   const radar_status r = check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
-  if (bad16(K) || bad16(V) || !tokens || !first || !choice || !path || !accepted || !next ||
+  if (odd16(K) || odd16(V) || !K != !V || !tokens || !first || !choice || !path || !accepted || !next ||
       any_off(tokens, first, choice, path, accepted, next, lens, counts, parent, new_lens) || nodes < 1)
     return RADAR_EINVAL;
   if (nodes > kMaxTree) return RADAR_EUNSUPPORTED;

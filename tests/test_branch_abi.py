@@ -105,7 +105,7 @@ def test_accept_refusals(L):
         assert call(**{name: None}) == 1 and call(**{name: OFF}) == 1, name
     for name in ("lens", "counts", "parent", "new"):
         assert call(**{name: OFF}) == 1, name
-    assert call(K=ODD) == 1 and call(tokens=P(0x1004)) == 1
+    assert call(K=ODD) == 1 and call(tokens=P(0x1004)) == 1 and call(V=ODD) == 1
 
 
 def test_keep_refusals(L):
