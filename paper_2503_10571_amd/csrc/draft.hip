@@ -30,11 +30,12 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
     }
   };
   const int n_rows = a.B * a.nodes * a.Hq;   // below 2^27
-  const int each = a.parts ? ((int)((a.t + a.nodes - 1) >> a.step_log2) + a.parts) / a.parts : tree_each(a);
+  const TreeBatch batch(a);
+  const int each = a.parts ? ((int)((a.t + a.nodes - 1) >> a.step_log2) + a.parts) / a.parts : batch.each();
   for (int x = blockIdx.x * kPer + own; x < n_rows; x += gridDim.x * kPer) {
     const int hq = x % a.Hq, node = x / a.Hq % a.nodes, hk = hq >> a.g_log2;
     const int64_t b = x / a.Hq / a.nodes;
-    const TreeSeq s = tree_seq(a, b);
+    const TreeSeq s = batch.seq(__builtin_amdgcn_readfirstlane((int)b));
     T* o = static_cast<T*>(a.out) + b * a.o_seq + node * a.o_node + hq * a.o_head;
     if (s.rows < 0) {
       for (int i = tid; i < D; i += kThreads) o[i] = from_f32<T>(__uint_as_float(0x7fc00000u));
@@ -43,7 +44,7 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
     if (node >= s.nodes) continue;
     const int row = node * a.G + (hq & (a.G - 1));
     int seq = (int)b;
-    const TreeCut cut = a.parts ? TreeCut{each, a.parts, (int)b * a.Hkv * a.parts} : tree_cut(a, each, false, 0, &seq);
+    const TreeCut cut = a.parts ? TreeCut{each, a.parts, (int)b * a.Hkv * a.parts} : batch.cut(each, false, 0, &seq);
     if (cut.parts == 1) continue;          // written by its block
     // the parts that begin before the end of the row tile's rows
     const int64_t end = tree_end(a, s, (row / rows_per_tile + 1) * rows_per_tile);

@@ -129,27 +129,31 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
   const int mt = a.mtiles - 1 - i % a.mtiles;
   int b, hk, part;
   TreeCut cut;
+  TreeSeq s;
   if (a.parts) {                           // uniform
-    const int bh = unit / a.parts;
-    part = unit % a.parts;
+    const int pairs = a.B * a.Hkv, bh = unit % pairs;
+    part = unit / pairs;
+    unit = bh * a.parts + part;
     b = bh / a.Hkv;
     hk = bh % a.Hkv;
     const int steps = (int)((a.t + a.nodes - 1) >> a.step_log2) + 1;
     cut = {(steps + a.parts - 1) / a.parts, a.parts, 0};
+    s = tree_seq(a, b);
   } else {
-    cut = tree_cut(a, tree_each(a), true, unit, &b);
+    const TreeBatch batch(a);
+    cut = batch.cut(batch.each(), true, unit, &b);
     if (b < 0) return;
+    s = batch.seq(b);
     hk = (unit - cut.first) / cut.parts;
     part = (unit - cut.first) % cut.parts;
   }
-  int own[kOwn] = {};                      // (asked for along with the lengths)
+  int own[kOwn] = {};                      // (asked for ahead of what follows)
   if (a.parent)
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) {
       const int i = threadIdx.x + 256 * k;
       if (i < a.nodes) own[k] = a.parent[(a.parent_shared ? 0 : (int64_t)b * a.nodes) + i];
     }
-  const TreeSeq s = tree_seq(a, b);
   const int row0 = mt * kRows, node0 = row0 >> a.g_log2;
   const bool direct = cut.parts == 1;
   TreeMask mask;

@@ -66,34 +66,53 @@ __device__ __forceinline__ int wave_scan(int x) {
 struct TreeCut {
   int each, parts, first;
 };
-// steps of a part of a ragged batch; the same in every wave
-__device__ __forceinline__ int tree_each(const TreeArgs& a) {
-  int total = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kWave) {
-    const int b = b0 + (threadIdx.x & 63);
-    total += __builtin_amdgcn_readlane(wave_scan(b < a.B ? tree_steps(a, tree_seq(a, b)) : 0), kWave - 1);
+
+// The sequences of a ragged batch as a wave sees them, 64 at a time; of up to 64 all at once,
+// each in its lane, asked for once.
+struct TreeBatch {
+  const TreeArgs& a;
+  TreeSeq own;
+  __device__ __forceinline__ explicit TreeBatch(const TreeArgs& args) : a(args), own{-1, 0} {
+    if (a.B <= kWave && lane() < a.B) own = tree_seq(a, lane());
   }
-  const uint32_t all = (uint32_t)total * a.Hkv;
-  return max(a.least, (int)((all + a.units - 1) / (uint32_t)a.units));
-}
-// of sequence b; or, by_part, of the one that part x of all lies in, which becomes b (-1: none)
-__device__ __forceinline__ TreeCut tree_cut(const TreeArgs& a, int each, bool by_part, int x, int* b) {
-  int before = 0;
-  for (int b0 = 0; b0 < a.B; b0 += kWave) {
-    const int lane = threadIdx.x & 63, i = b0 + lane;
-    const int own = i < a.B ? (int)((uint32_t)(tree_steps(a, tree_seq(a, i)) + each - 1) / (uint32_t)each) : 0;
-    const int sum = wave_scan(own * a.Hkv);
-    const u64 hit = __ballot(by_part ? x < before + sum : i == *b);
-    if (hit) {                             // uniform
-      const int l = __ffsll(hit) - 1, parts = __builtin_amdgcn_readlane(own, l);
-      *b = b0 + l;
-      return {each, parts, before + __builtin_amdgcn_readlane(sum, l) - parts * a.Hkv};
+  __device__ __forceinline__ static int lane() { return threadIdx.x & 63; }
+  // steps of sequence b0 + lane
+  __device__ __forceinline__ int steps(int b0) const {
+    if (a.B <= kWave) return tree_steps(a, own);
+    return b0 + lane() < a.B ? tree_steps(a, tree_seq(a, b0 + lane())) : 0;
+  }
+  __device__ __forceinline__ TreeSeq seq(int b) const {            // b: uniform
+    if (a.B > kWave) return tree_seq(a, b);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)(uint32_t)own.rows, b);
+    const uint32_t hi = __builtin_amdgcn_readlane((int)(own.rows >> 32), b);
+    return {(int64_t)((uint64_t)hi << 32 | lo), __builtin_amdgcn_readlane(own.nodes, b)};
+  }
+  // steps of a part; the same in every wave
+  __device__ __forceinline__ int each() const {
+    uint32_t all = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave)
+      all += (uint32_t)__builtin_amdgcn_readlane(wave_scan(steps(b0)), kWave - 1);
+    all *= a.Hkv;
+    return max(a.least, (int)((all + a.units - 1) / (uint32_t)a.units));
+  }
+  // of sequence b; or, by_part, of the one that part x of all lies in, which becomes b (-1: none)
+  __device__ __forceinline__ TreeCut cut(int each, bool by_part, int x, int* b) const {
+    int before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += kWave) {
+      const int own_parts = (int)((uint32_t)(steps(b0) + each - 1) / (uint32_t)each);
+      const int sum = wave_scan(own_parts * a.Hkv);
+      const u64 hit = __ballot(by_part ? x < before + sum : b0 + lane() == *b);
+      if (hit) {                           // uniform
+        const int l = __ffsll(hit) - 1, parts = __builtin_amdgcn_readlane(own_parts, l);
+        *b = b0 + l;
+        return {each, parts, before + __builtin_amdgcn_readlane(sum, l) - parts * a.Hkv};
+      }
+      before += __builtin_amdgcn_readlane(sum, kWave - 1);
     }
-    before += __builtin_amdgcn_readlane(sum, kWave - 1);
+    *b = -1;
+    return {each, 0, 0};
   }
-  *b = -1;
-  return {each, 0, 0};
-}
+};
 
 // tree.hip: rw in {1, 2, 4} row waves
 void launch_tree_bf16_64(const TreeArgs& a, int rw, hipStream_t st);
