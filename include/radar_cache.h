@@ -226,7 +226,7 @@ size_t radar_attend_tree_workspace_bytes(const radar_config* cfg, int64_t nodes,
  * [batch]) how many, next (int64 [batch]) the last choice, which no node held.
  * The rows of K and V that the path's nodes have move to len, len + 1, ..; no
  * other row changes, and none does with K and V NULL. new_lens (nullable, int64 [batch]) receives len + accepted;
- * it may be lens itself, and next first. 1 <= nodes <= RADAR_MAX_TREE, else as
+ * it may be lens itself, and next first (no other two share memory). 1 <= nodes <= RADAR_MAX_TREE, else as
  * above; a sequence with an invalid length or count keeps its rows and gets an
  * empty path, next -1 and new_lens its lens[b]. A node with an invalid parent is
  * never met. The summaries of the index are not touched: radar_extend_index

@@ -550,6 +550,10 @@ template <typename T>
 bool off(const T* p) { return reinterpret_cast<uintptr_t>(p) % sizeof(T) != 0; }
 template <typename... T>
 bool any_off(const T*... p) { return (off(p) || ...); }
+// two lists of n, given, share memory without being one
+bool meet(const int64_t* p, const int64_t* q, int n) {
+  return p && q && p != q && std::abs((intptr_t)p - (intptr_t)q) < (intptr_t)n * 8;
+}
 int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
 
 // the index's fields of the config, with radar.h's limits
@@ -597,7 +601,8 @@ radar_status radar_accept_tree(const radar_config* cfg, void* K, void* V, int64_
   const radar_status r = check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
   if (odd16(K) || odd16(V) || !K != !V || !tokens || !first || !choice || !path || !accepted || !next ||
-      any_off(tokens, first, choice, path, accepted, next, lens, counts, parent, new_lens) || nodes < 1)
+      any_off(tokens, first, choice, path, accepted, next, lens, counts, parent, new_lens) || nodes < 1 ||
+      meet(new_lens, lens, s.B) || meet(next, first, s.B))
     return RADAR_EINVAL;
   if (nodes > kMaxTree) return RADAR_EUNSUPPORTED;
   if (t < 0 || t > s.cap || (!lens && nodes > s.cap - t)) return RADAR_ECAPACITY;
@@ -617,7 +622,8 @@ radar_status radar_keep_path(const radar_config* cfg, void* K, void* V, int64_t 
   Shape s;
   const radar_status r = check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
-  if (bad16(K) || bad16(V) || n < 0 || (n > 0 && !path) || any_off(path, lens, counts, new_lens))
+  if (bad16(K) || bad16(V) || n < 0 || (n > 0 && !path) || any_off(path, lens, counts, new_lens) ||
+      meet(new_lens, lens, s.B))
     return RADAR_EINVAL;
   if (t < 0 || t > s.cap || n > s.cap) return RADAR_ECAPACITY;
   PathArgs a = path_args(s, K, V, t, lens, n, counts, new_lens);
@@ -673,7 +679,8 @@ radar_status radar_fork(const radar_config* cfg, void* K, void* V, float* mass, 
   const radar_status r = summaries ? check_index(cfg, &s) : check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
   if (bad16(K) || bad16(V) || odd16(mass) || odd16(summaries) || !src ||
-      any_off(src, lens, new_lens) || src == new_lens || first < 0)
+      any_off(src, lens, new_lens) || src == new_lens || meet(new_lens, src, s.B) || meet(new_lens, lens, s.B) ||
+      first < 0)
     return RADAR_EINVAL;
   if (t < 0 || t > s.cap) return RADAR_ECAPACITY;
   if (s.B > RADAR_MAX_FORK) return RADAR_EUNSUPPORTED;

@@ -101,11 +101,13 @@ def test_accept_refusals(L):
     assert call(nodes=0) == 1 and call(nodes=513) == 3
     assert call(t=-1) == 2 and call(t=4097) == 2 and call(t=4090) == 2
     assert call(t=4097, lens=GOOD) == 2
-    for name in ("K", "V", "tokens", "first", "choice", "path", "accepted", "nxt"):
+    for name in ("tokens", "first", "choice", "path", "accepted", "nxt"):
         assert call(**{name: None}) == 1 and call(**{name: OFF}) == 1, name
     for name in ("lens", "counts", "parent", "new"):
         assert call(**{name: OFF}) == 1, name
     assert call(K=ODD) == 1 and call(tokens=P(0x1004)) == 1 and call(V=ODD) == 1
+    assert call(K=None, V=GOOD) == 1 and call(V=None) == 1
+    assert call(lens=GOOD, new=ODD) == 1 and call(nxt=ODD) == 1
 
 
 def test_keep_refusals(L):
@@ -120,6 +122,7 @@ def test_keep_refusals(L):
     for name in ("lens", "counts", "new"):
         assert call(**{name: OFF}) == 1, name
     assert call(V=ODD) == 1
+    assert call(lens=GOOD, new=P(0x1038)) == 1 and call(lens=P(0x1038), new=GOOD) == 1   # over a part of the other
 
 
 def test_extend_index_refusals(L):
@@ -161,6 +164,7 @@ def test_fork_refusals(L):
         assert call(**{name: OFF}) == 1, name
     assert call(K=ODD) == 1 and call(mass=ODD) == 1 and call(summ=ODD) == 1
     assert call(new=GOOD) == 1                                   # the new lengths over the map
+    assert call(new=ODD) == 1 and call(src=P(0x2000), lens=GOOD, new=P(0x1038)) == 1     # or over a part of a list
 
 
 def test_binding_refuses_host_tensors(L):
