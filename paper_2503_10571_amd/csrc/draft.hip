@@ -137,15 +137,29 @@ TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
   p.rows_per_tile = flash_rows(esize(s), p.rw);
   p.mtiles = (int)ceil_div(M, p.rows_per_tile);
   p.step = flash_tile(esize(s), p.rw);
-  const int64_t blocks = pairs * p.mtiles, steps = ceil_div(t + nodes, p.step);
+  const int64_t blocks = pairs * p.mtiles;
+  int room = slots();
+  // Two groups of four waves to a workgroup, whose accumulators meet in LDS: half as many
+  // workgroups and partials, but groups in step. For sequences of one length where each CU
+  // has four steps and more to do and a pair at most two row tiles (32 nodes over 32K rows:
+  // 44.5 us, 41.8; four sequences of 2000 and 64 nodes: 31.1, 29.1; but one of 4096 and 64:
+  // 21.7, 22.5, one of 64K and 128: 169, 177), or is whole then (four of 4000 and 200 nodes:
+  // 97, 85); not at head dim 64, where the vector ALUs bound (eight of 8000 and 64: 65, 69).
+  if (p.rw == 4 && s.dt == RADAR_BF16 && s.d == 128 && !ragged && 2 * blocks <= room &&
+      (p.mtiles <= 2 || 4 * blocks > room) && blocks * ceil_div(t + nodes, 2 * p.step) >= 4 * (room / 2)) {
+    p.rw = 8;
+    p.step *= 2;
+    room /= 2;
+  }
+  const int64_t steps = ceil_div(t + nodes, p.step);
   p.units = 0;
-  if (ragged && steps > kShort && blocks <= 2 * slots() && pairs * steps < (1ll << 31)) {
+  if (ragged && steps > kShort && blocks <= 2 * room && pairs * steps < (1ll << 31)) {
     // (a pair's last part is shorter: as many more parts as there are pairs, at most)
-    const int64_t units = std::max<int64_t>(1, slots() / p.mtiles);
+    const int64_t units = std::max<int64_t>(1, room / p.mtiles);
     p.parts = 0;
     p.units = (int)std::max(units - pairs, (units + 1) / 2);
   } else {
-    p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(slots() / blocks, ceil_div(t + nodes, kLeast)));
+    p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(room / blocks, ceil_div(t + nodes, kLeast)));
     if (steps <= kShort) p.parts = 1;
     // (as many of one length)
     p.parts = (int)ceil_div(steps, ceil_div(steps, p.parts));

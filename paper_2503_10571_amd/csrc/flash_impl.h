@@ -332,23 +332,24 @@ __device__ __forceinline__ void store4(bf16_t* o, float a, float b, float c, flo
 // kRows) and tiles of its own, in its own part of the LDS, with no barrier in the
 // loop: what memory bounds. RW = 2 or 4: RW waves with 32 rows each, and 4 / RW
 // such groups that share the tokens of a tile.
-template <typename T, int D, int RW>
+template <typename T, int D, int RW, int WAVES = 4>
 struct Flash {
   using O = Ops<T, D, RW>;
   using Vec = typename O::Vec;
-  static constexpr int TW = 4 / RW;              // groups with tokens of their own
-  static constexpr int NTG = flash_tile(sizeof(T), RW);   // tokens of a workgroup's step
-  static constexpr int NT = RW == 1 ? NTG / 4 : NTG;      // of one tile in LDS
-  static constexpr int NTHR = RW == 1 ? 64 : 256;         // threads that load it
+  static constexpr int kThreads = WAVES * 64;
+  static constexpr int TW = WAVES / RW;          // groups with tokens of their own
+  static constexpr int NTG = flash_tile(sizeof(T), RW) * (WAVES / 4);   // tokens of a workgroup's step
+  static constexpr int NT = RW == 1 ? NTG / WAVES : NTG;  // of one tile in LDS
+  static constexpr int NTHR = RW == 1 ? 64 : kThreads;    // threads that load it
   static constexpr int kSub = NTG / TW / O::kTok;         // steps of a wave in it
   static constexpr int kBytes = NT * D * (int)sizeof(T);  // of K, and of V
   static constexpr int NCH = kBytes / 16 / NTHR; // chunks of each per thread
   static constexpr int NDB = O::NDB;
   // two buffers save the barrier before a tile is written
-  static constexpr int kBuf = RW > 1 && 4 * kBytes <= (64 << 10) ? 2 : 1;
-  static constexpr int kTiles = (RW == 1 ? 4 : kBuf) * 2 * kBytes;
+  static constexpr int kBuf = RW > 1 && 4 * kBytes <= (64 << 10) * (WAVES / 4) ? 2 : 1;
+  static constexpr int kTiles = (RW == 1 ? WAVES : kBuf) * 2 * kBytes;
   // the groups' accumulators are added in LDS
-  static constexpr int kMerge = TW > 1 ? 4 * O::kRows * D * 4 : 0;
+  static constexpr int kMerge = TW > 1 ? WAVES * O::kRows * D * 4 : 0;
   static constexpr int kLds = kTiles > kMerge ? kTiles : kMerge;
 
   // Rows [r0, r1) of K and V (r1 > r0) for the query rows of this workgroup:
@@ -638,7 +639,7 @@ struct Flash {
         if (first) { wm[tw][row] = m; wl[tw][row] = l; }
       }
       __syncthreads();
-      for (int x = tid; x < rows * (D / 4); x += 256) {
+      for (int x = tid; x < rows * (D / 4); x += kThreads) {
         const int r = x / (D / 4), c = x % (D / 4);
         float M = wm[0][r];
 #pragma unroll

@@ -56,16 +56,17 @@ struct TreeMask {
 // The bits of nodes [node0, node0 + n): node i's are its own, its parent's, .. up to a
 // root. A thread walks up from each, over a run of nodes that each follow the one before
 // (up to 32, a word's) at once: of every node LDS holds where its run begins and the parent
-// of that one, plus 2. own: this thread's parents, of nodes tid and tid + 256.
-constexpr int kOwn = RADAR_MAX_TREE / 256;
-__device__ __forceinline__ void tree_bits(const int (&own)[kOwn], int nodes, int node0, int n,
-                                          unsigned char* lds, uint32_t* bits) {
+// of that one, plus 2. own: this thread's parents, of nodes tid, tid + THREADS, ..
+template <int THREADS>
+__device__ __forceinline__ void tree_bits(const int (&own)[RADAR_MAX_TREE / THREADS], int nodes, int node0,
+                                          int n, unsigned char* lds, uint32_t* bits) {
+  constexpr int kOwn = RADAR_MAX_TREE / THREADS;
   int* up = reinterpret_cast<int*>(lds);           // parent + 2, then run begin << 16 | its parent + 2
   const int tid = threadIdx.x, lane = tid & 63;
   int begin[kOwn];
 #pragma unroll
   for (int k = 0; k < kOwn; ++k) {
-    const int i = tid + 256 * k;
+    const int i = tid + THREADS * k;
     const bool good = i < nodes && own[k] >= -1 && own[k] < i;
     const u64 runs = __ballot(good && own[k] == i - 1);
     const uint32_t word = (uint32_t)(lane < 32 ? runs : runs >> 32);
@@ -79,9 +80,9 @@ __device__ __forceinline__ void tree_bits(const int (&own)[kOwn], int nodes, int
   for (int k = 0; k < kOwn; ++k) jump[k] = begin[k] << 16 | up[begin[k]];
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < kOwn; ++k) up[tid + 256 * k] = jump[k];
+  for (int k = 0; k < kOwn; ++k) up[tid + THREADS * k] = jump[k];
   __syncthreads();
-  for (int k = tid; k < n; k += 256) {
+  for (int k = tid; k < n; k += THREADS) {
     uint32_t* o = bits + k * kNodeWords;
     o[0] = ~0u;
     for (int i = 1; i < kTreeWords + 3; ++i) o[i] = 0;
@@ -108,9 +109,9 @@ __device__ __forceinline__ void tree_bits(const int (&own)[kOwn], int nodes, int
 // last of them, which in a chain attends the most, first; the blocks of the last, not whole
 // round are dealt out evenly. An XCD so gets parts of all sequences: each has about an eighth
 // of the card's bandwidth, and one with the longest sequence for itself is waited for.
-template <typename T, int D, int RW>
-__global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
-  using F = Flash<T, D, RW>;
+template <typename T, int D, int RW, int WAVES>
+__global__ __launch_bounds__(WAVES * 64, 2) void k_tree(TreeArgs a) {
+  using F = Flash<T, D, RW, WAVES>;
   constexpr int kRows = F::O::kRows * RW;
   using RowArray = float (*)[kRows];
   __shared__ __attribute__((aligned(16))) unsigned char lds[F::kLds];
@@ -147,11 +148,12 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
     hk = (unit - cut.first) / cut.parts;
     part = (unit - cut.first) % cut.parts;
   }
+  constexpr int kOwn = RADAR_MAX_TREE / (WAVES * 64);
   int own[kOwn] = {};                      // (asked for ahead of what follows)
   if (a.parent)
 #pragma unroll
     for (int k = 0; k < kOwn; ++k) {
-      const int i = threadIdx.x + 256 * k;
+      const int i = threadIdx.x + WAVES * 64 * k;
       if (i < a.nodes) own[k] = a.parent[(a.parent_shared ? 0 : (int64_t)b * a.nodes) + i];
     }
   const int row0 = mt * kRows, node0 = row0 >> a.g_log2;
@@ -163,7 +165,7 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
   mask.o_node = a.o_node * (int64_t)sizeof(T);
   mask.o_head = a.o_head * (int64_t)sizeof(T);
   if (s.rows < 0) {                        // (parts = 1: else the merge does it)
-    for (int y = threadIdx.x; y < min(kRows, a.M - row0) * D; y += 256)
+    for (int y = threadIdx.x; y < min(kRows, a.M - row0) * D; y += WAVES * 64)
       static_cast<T*>(mask.out_row(y / D))[y % D] = from_f32<T>(__uint_as_float(0x7fc00000u));
     return;
   }
@@ -180,7 +182,7 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
   mask.direct = direct;
   if (r1 > mask.from) {                    // uniform
     if (threadIdx.x == 0) odd = 0;
-    if (a.parent) tree_bits(own, s.nodes, node0, (rows + a.G - 1) >> a.g_log2, lds, bits);
+    if (a.parent) tree_bits<WAVES * 64>(own, s.nodes, node0, (rows + a.G - 1) >> a.g_log2, lds, bits);
     else __syncthreads();
   }
   const T* q = static_cast<const T*>(a.q) + b * a.q_seq + node0 * a.q_node + hk * a.G * a.q_head;
@@ -205,10 +207,11 @@ __global__ __launch_bounds__(256, 2) void k_tree(TreeArgs a) {
 template <typename T, int D>
 void launch_tree(const TreeArgs& a, int rw, hipStream_t st) {
   const int64_t pairs = (int64_t)a.B * a.Hkv, units = a.parts ? pairs * a.parts : a.units + pairs;
-  const dim3 grid((unsigned)(8 * (units / 8 * a.mtiles + ceil_div(units % 8 * a.mtiles, 8)))), block(256);
-  if (rw == 1) launch(RADAR_K_ATTEND, k_tree<T, D, 1>, grid, block, 0, st, a);
-  else if (rw == 2) launch(RADAR_K_ATTEND, k_tree<T, D, 2>, grid, block, 0, st, a);
-  else launch(RADAR_K_ATTEND, k_tree<T, D, 4>, grid, block, 0, st, a);
+  const dim3 grid((unsigned)(8 * (units / 8 * a.mtiles + ceil_div(units % 8 * a.mtiles, 8))));
+  if (rw == 1) launch(RADAR_K_ATTEND, k_tree<T, D, 1, 4>, grid, dim3(256), 0, st, a);
+  else if (rw == 2) launch(RADAR_K_ATTEND, k_tree<T, D, 2, 4>, grid, dim3(256), 0, st, a);
+  else if (rw == 4) launch(RADAR_K_ATTEND, k_tree<T, D, 4, 4>, grid, dim3(256), 0, st, a);
+  else if constexpr (sizeof(T) == 2) launch(RADAR_K_ATTEND, k_tree<T, D, 4, 8>, grid, dim3(512), 0, st, a);
 }
 
 }  // namespace

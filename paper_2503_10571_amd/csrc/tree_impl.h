@@ -87,7 +87,9 @@ struct TreeBatch {
     const uint32_t hi = __builtin_amdgcn_readlane((int)(own.rows >> 32), b);
     return {(int64_t)((uint64_t)hi << 32 | lo), __builtin_amdgcn_readlane(own.nodes, b)};
   }
-  // steps of a part; the same in every wave
+  // Steps of a part; the same in every wave. With 1 / units of all there are at most units
+  // parts and a shorter one for each pair. (To look here for the fewest steps whose parts
+  // just fill the chip gains nothing.)
   __device__ __forceinline__ int each() const {
     uint32_t all = 0;
     for (int b0 = 0; b0 < a.B; b0 += kWave)
