@@ -151,13 +151,19 @@ TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
     p.step *= 2;
     room /= 2;
   }
+  // Up to 32 query rows a pair in bf16, whose waves have tiles of their own: one workgroup a
+  // CU asks for as much as two, with half the partials (8 nodes over 64K rows: 56 us, 51;
+  // 32 sequences of 1000 rows, whole: 38, 29; but one token each, 16 sequences of 4000:
+  // 53.5, 56).
+  const bool one = p.rw == 1 && s.dt == RADAR_BF16;
+  if (one) room /= 2;
   const int64_t steps = ceil_div(t + nodes, p.step);
   p.units = 0;
   if (ragged && steps > kShort && blocks <= 2 * room && pairs * steps < (1ll << 31)) {
     // (a pair's last part is shorter: as many more parts as there are pairs, at most)
     const int64_t units = std::max<int64_t>(1, room / p.mtiles);
     p.parts = 0;
-    p.units = (int)std::max(units - pairs, (units + 1) / 2);
+    p.units = (int)std::max(units - (one ? pairs / 2 : pairs), (units + 1) / 2);
   } else {
     p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(room / blocks, ceil_div(t + nodes, kLeast)));
     if (steps <= kShort) p.parts = 1;
