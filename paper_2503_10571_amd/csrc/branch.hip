@@ -61,7 +61,8 @@ __device__ __forceinline__ void move_rows(const PathArgs& a, int64_t b, int64_t 
 // A workgroup per sequence. Its first wave holds the nodes, U to a lane, and walks
 // down: of the nodes behind the current one whose parent it is and whose token is the
 // one wanted, the lowest, by a ballot for each 64 (a step is some 100 cycles; the
-// loads, all at once, are most of the kernel's time). All waves then move the rows.
+// loads, all at once, are most of the kernel's time: 2.4 us for 26 nodes, 3.5 for 64
+// sequences of 63). All waves then move the rows.
 // The sequence's length is read by the first wave only and before anything is
 // written, so that the new length may take its place.
 template <int U>
@@ -192,6 +193,11 @@ __device__ __forceinline__ int64_t fork_len(const ForkArgs& a, int64_t s) {
 // Each workgroup makes the list of the moves once: those whose destination no move
 // still has to read come first, then those that this sets free, and so on; what is
 // left are cycles, whose first sequence is saved.
+//
+// Memory bounds it, by the streams that are open at once: one sequence to one 5.6 TB/s (268
+// MB each way: 96 us), to seven 4.65 (16411 rows of 8 heads: 116 us), to 31 4.2; any map of 16
+// 4.6 (12001 rows of 16 heads: 559 us). A workgroup's start, with the list, is some 5 us (16
+// sequences of 30 rows: 8 us).
 constexpr int kInFlight = 8, kForkThreads = 256;
 // a move is dst << 16 | src; kNone as dst: src is saved; kSaved in src: src as it was saved;
 // kZero as src: zeros

@@ -9,7 +9,8 @@ constexpr int kSlots = 512;                // workgroups that the chip holds at 
 constexpr int kFew = 128;                  // partials of a row that one wave merges
 
 // A query row's output from its partials by NW waves: D / 4 lanes on four dims each of one
-// partial, the others on the next.
+// partial, the others on the next. One wave a row where there are enough rows to fill the
+// chip (8192 rows of up to 13 partials, 29 MB: 10 us; 1024 of 63: 5.5 with four).
 //   out = sum_i acc_i 2^(m_i - m) / sum_i l_i 2^(m_i - m),  m = max_i m_i
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_tile) {
