@@ -366,6 +366,56 @@ def test_fork_most_sequences():
     assert e.value.status == 3
 
 
+@pytest.mark.parametrize("src", [[1, 2, 0, 0], [3, 4, 0, 1, 5, 6, 3, 2]])
+def test_fork_past_the_caches(src):
+    """More than the Infinity Cache holds."""
+    B = len(src)
+    _check_fork(src, [64000 // B - 1000 * b for b in range(B)], 64000 // B, 7, "bf16", Hkv=8, d=128, c=512)
+
+
+@DTYPES
+def test_fork_behind_2_31_elements(dtype):
+    """Sequences and rows that lie past 32-bit offsets; only the last rows move."""
+    t = (1 << 25) + 40 if dtype == "bf16" else (1 << 24) + 40
+    K = torch.zeros(2, 1, t, 64, dtype=DT[dtype], device="cuda")
+    V = torch.zeros_like(K)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for x in (K, V):
+        x[:, :, -100:] = torch.randn(2, 1, 100, 64, generator=g, device="cuda").to(DT[dtype])
+    want = [x[:, :, -100:].flip(0) for x in (K, V)]
+    radar.fork(_cfg(2, 1, 64, t, dtype), K, V, _int([1, 0]), t, first=t - 60)
+    for x, w, in zip((K, V), want):
+        assert torch.equal(x[:, :, -60:], w[:, :, -60:])
+        assert torch.equal(x[:, :, -100:-60], w[:, :, :40].flip(0)) and not bool(x[:, :, :1000].any())
+    lens = _int([t - 50, t - 9])
+    before = [x[:, :, -100:].clone() for x in (K, V)]
+    radar.keep_path(_cfg(2, 1, 64, t, dtype), K, V, t, _int([[1, 3, 8], [0, 2, 8]], torch.int32), lens=lens, new_lens=lens)
+    for x, w in zip((K, V), before):
+        w[0, :, 50:53] = w[0][:, [51, 53, 58]]
+        w[1, :, 91:94] = w[1][:, [91, 93, 99]]
+        assert torch.equal(x[:, :, -100:], w)
+    assert lens.tolist() == [t - 47, t - 6]
+
+
+def test_paths_in_a_host_cache():
+    K, V = (torch.randn(2, 3, 30, 64).pin_memory() for _ in range(2))
+    want = [x.clone() for x in (K, V)]
+    for w in want:
+        w[:, :, 10:12] = w[:, :, [10, 13]]
+    cfg = _cfg(2, 3, 64, 30, "f32")
+    tokens = _int([[1, 2, 3, 4]] * 2)
+    path, n, token = radar.accept_tree(cfg, K, V, 10, tokens, _int([1, 1]), _int([[4, 0, 0, 9]] * 2),
+                                       parent=_int([-1, 0, 0, 0], torch.int32))
+    torch.cuda.synchronize()
+    assert path.tolist() == [[0, 3, -1, -1]] * 2 and token.tolist() == [9, 9]
+    assert torch.equal(K, want[0]) and torch.equal(V, want[1])
+    for w in want:
+        w[:, :, 12:14] = w[:, :, [14, 17]]
+    radar.keep_path(cfg, K, V, 12, _int([[2, 5]] * 2, torch.int32))
+    torch.cuda.synchronize()
+    assert torch.equal(K, want[0]) and torch.equal(V, want[1])
+
+
 def test_fork_host_cache():
     K, V = (torch.randn(3, 2, 30, 64).pin_memory() for _ in range(2))
     want = [_forked(x, [1, 2, 2], [25] * 3, 0, [25] * 3) for x in (K, V)]

@@ -77,6 +77,10 @@ def _check(out, q, K, V, parents, lens, counts, dtype, Hkv, worst=None):
 
 def _run(B, Hq, Hkv, d, t, N, lens, counts, spread, dtype, shared=False, qscale=2.0, check=None, seed=None):
     print(f"[case] tree B{B} Hq{Hq}/{Hkv} d{d} t{t} N{N} spread{spread} {lens} {counts} {dtype}", flush=True)
+    if lens == "ragged":
+        lens = [t * ((7 * b) % B) // B for b in range(B)]
+    if counts == "ragged":
+        counts = [(5 * b) % (N + 1) for b in range(B)]
     L, C = lens or [t] * B, counts or [N] * B
     q, K, V = _inputs(B, Hq, Hkv, d, t, N, L, C, dtype, seed=t + N if seed is None else seed, qscale=qscale)
     parents = [_tree(N, 0 if shared else b, spread) for b in range(B)]
@@ -125,6 +129,12 @@ CASES = [  # B, Hq, Hkv, d, t, N, lens, counts, spread
     (1, 4, 1, 64, 1000, 700, None, None, 0),
     (1, 1, 1, 128, 5, 1500, None, None, 0),
     (40, 4, 2, 64, 50, 6, None, None, 2),                   # more pairs than a wave of blocks needs
+    (1, 32, 8, 128, 8161, 33, None, None, 6),               # two groups of waves to a workgroup
+    (2, 16, 4, 128, 9000, 40, None, None, 0),
+    (17, 8, 8, 128, 1100, 66, None, None, 9),               # the same, whole
+    (70, 2, 1, 64, 3000, 5, "ragged", None, 2),             # more lengths than lanes
+    (130, 1, 1, 128, 700, 20, "ragged", "ragged", 3),
+    (150, 4, 4, 64, 600, 3, "ragged", None, 1),             # more pairs than parts
 ]
 
 
@@ -163,7 +173,7 @@ def test_sharp_and_flat(N, dtype):
 
 @DTYPES
 @pytest.mark.parametrize("chain", [False, True])
-@pytest.mark.parametrize("N,t", [(6, 40), (30, 1000), (90, 2500)])
+@pytest.mark.parametrize("N,t", [(6, 40), (30, 1000), (90, 2500), (40, 17000)])
 def test_other_branches_do_not_matter(N, t, chain, dtype):
     """NaN and infinities in the rows of some nodes: those who attend them get values
     that are no finite numbers in those dims, the others what they get without."""
@@ -271,6 +281,30 @@ def test_host_cache():
     want = radar.attend_tree(cfg, q, K, V, 400, parent=P)
     got = radar.attend_tree(cfg, q, K.cpu().pin_memory(), V.cpu().pin_memory(), 400, parent=P)
     assert torch.equal(got, want)
+
+
+@DTYPES
+@pytest.mark.parametrize("N", [1, 20, 100])
+def test_rows_behind_2_31_elements(N, dtype):
+    """A cache whose rows lie past 32-bit offsets: one of the first rows and one of the
+    last take all the weight of a query each, and its value is their mean."""
+    d, G = 64, 2
+    t = (1 << 25) + 77 if dtype == "bf16" else (1 << 24) + 77
+    K = torch.zeros(1, 1, t + N, d, dtype=DT[dtype], device="cuda")
+    V = torch.zeros_like(K)
+    g = torch.Generator(device="cuda").manual_seed(N)
+    q = torch.randn(1, N, G, d, generator=g, device="cuda").sign().to(DT[dtype])
+    at = [3, t - 5]
+    K[0, 0, at] = q[0, 0, 0] * 8                           # logits of 64 for the first query row
+    V[0, 0, at] = torch.randn(2, d, generator=g, device="cuda").to(DT[dtype])
+    V[0, 0, t:] = 5.0
+    cfg = _cfg(1, G, 1, d, t + N, dtype)
+    out = radar.attend_tree(cfg, q, K, V, t)
+    # the others' weights together: 2^25 e^-64 of a row's
+    want = V[0, 0, at].double().mean(0)
+    half = 2.0 ** -8 if dtype == "bf16" else 0.0
+    lim = (2 * half + 1e-5) * V[0, 0, at].double().abs().sum(0) + 1e-18
+    assert bool(((out[0, 0, 0].double() - want).abs() <= lim).all())
 
 
 @DTYPES
