@@ -333,13 +333,15 @@ struct ForkStep {
   }
 };
 
-// Every tile of a plane, a step ahead.
+// Every tile of the planes of a kind, a step ahead. The workgroups take them in turn from
+// number `turn` of all on, where the kind before has left off; returns the next turn.
 template <typename V, int COLS, bool MASS, bool NT>
-__device__ __forceinline__ void fork_plane(ForkPlane p, const ForkList& l, int64_t planes) {
+__device__ __forceinline__ int64_t fork_planes(ForkPlane p, const ForkList& l, int64_t planes, int64_t turn) {
   using Step = ForkStep<V, COLS, MASS, NT>;
   p.tiles = (p.units + Step::kTile - 1) / Step::kTile;
   const int64_t all = planes * p.tiles;
-  int64_t i = (int64_t)blockIdx.x - gridDim.x;
+  const int late = (int)((blockIdx.x + gridDim.x - turn % gridDim.x) % gridDim.x);
+  int64_t i = (int64_t)late - gridDim.x;
   int e1 = l.n;
   u64 rest = 0;
   V saved[COLS];
@@ -365,7 +367,7 @@ __device__ __forceinline__ void fork_plane(ForkPlane p, const ForkList& l, int64
     return true;
   };
   Step a, b;
-  if (!next(a, b)) return;
+  if (!next(a, b)) return turn + all;
   for (;;) {
     const bool more_b = next(b, a);
     a.store(saved);
@@ -374,22 +376,23 @@ __device__ __forceinline__ void fork_plane(ForkPlane p, const ForkList& l, int64
     b.store(saved);
     if (!more_a) break;
   }
+  return turn + all;
 }
 
 template <int COLS, bool NT>
 __device__ __forceinline__ void fork_all(const ForkArgs& a, const ForkList& l) {
   const ForkPlane kv{a.K + a.first * a.row_bytes, a.V - a.K, a.cap * a.row_bytes, a.Hkv * a.cap * a.row_bytes,
                      a.units[0], a.first, 0, 1, a.row_bytes / 16, 0};
-  fork_plane<u32x4_t, COLS, false, NT>(kv, l, 2 * a.Hkv);
+  int64_t turn = fork_planes<u32x4_t, COLS, false, NT>(kv, l, 2 * a.Hkv, 0);
   if (a.units[1]) {
     const ForkPlane mass{a.mass, 0, a.cap * 4, a.Hkv * a.cap * 4, a.units[1], 0, 0, 1, 1, 0};
-    fork_plane<uint32_t, COLS, true, false>(mass, l, a.Hkv);
+    turn = fork_planes<uint32_t, COLS, true, false>(mass, l, a.Hkv, turn);
   }
   if (a.units[2]) {
     const int64_t seg0 = max((int64_t)0, a.first - a.n_sink) / a.c;
     const ForkPlane summ{a.summ + seg0 * a.summ_bytes, 0, a.summ_rows * a.summ_bytes,
                          a.Hkv * a.summ_rows * a.summ_bytes, a.units[2], seg0, a.n_sink, a.c, a.summ_bytes / 16, 0};
-    fork_plane<u32x4_t, COLS, false, false>(summ, l, a.Hkv);
+    fork_planes<u32x4_t, COLS, false, false>(summ, l, a.Hkv, turn);
   }
 }
 
