@@ -128,7 +128,7 @@ int tree_waves(const Shape& s, int64_t M) {
 constexpr int kLeast = 256, kShort = 4;
 
 struct TreePlan {
-  int rw, mtiles, rows_per_tile, step, parts, units;
+  int rw, waves, mtiles, rows_per_tile, step, parts, units;
 };
 
 TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
@@ -140,15 +140,17 @@ TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
   p.step = flash_tile(esize(s), p.rw);
   const int64_t blocks = pairs * p.mtiles;
   int room = slots();
-  // Two groups of four waves to a workgroup, whose accumulators meet in LDS: half as many
-  // workgroups and partials, but groups in step. For sequences of one length where each CU
-  // has four steps and more to do and a pair at most two row tiles (32 nodes over 32K rows:
-  // 44.5 us, 41.8; four sequences of 2000 and 64 nodes: 31.1, 29.1; but one of 4096 and 64:
-  // 21.7, 22.5, one of 64K and 128: 169, 177), or is whole then (four of 4000 and 200 nodes:
-  // 97, 85); not at head dim 64, where the vector ALUs bound (eight of 8000 and 64: 65, 69).
-  if (p.rw == 4 && s.dt == RADAR_BF16 && s.d == 128 && !ragged && 2 * blocks <= room &&
+  // Eight waves to a workgroup, whose accumulators meet in LDS: half as many workgroups and
+  // partials, but all waves in step. For sequences of one length where each CU has four
+  // steps and more to do and a pair at most two row tiles (16 nodes over 16K rows: 28.5 us,
+  // 25.5, eight sequences of 9000: 62, 59.5; 32 nodes over 32K rows: 44.5, 41.8; four of 2000
+  // and 64 nodes: 31.1, 29.1; but one of 4096 and 64: 21.7, 22.5, one of 64K and 128: 169,
+  // 177), or is whole then (four of 4000 and 200 nodes: 97, 85); not at head dim 64, where
+  // the vector ALUs bound (eight of 8000 and 64: 65, 69).
+  p.waves = 4;
+  if (p.rw > 1 && s.dt == RADAR_BF16 && s.d == 128 && !ragged && 2 * blocks <= room &&
       (p.mtiles <= 2 || 4 * blocks > room) && blocks * ceil_div(t + nodes, 2 * p.step) >= 4 * (room / 2)) {
-    p.rw = 8;
+    p.waves = 8;
     p.step *= 2;
     room /= 2;
   }
@@ -253,11 +255,11 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, con
   a.acc = static_cast<float*>(workspace);
   a.ml = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + w.ml);
   if (s.dt == RADAR_BF16) {
-    if (s.d == 64) launch_tree_bf16_64(a, p.rw, stream);
-    else launch_tree_bf16_128(a, p.rw, stream);
+    if (s.d == 64) launch_tree_bf16_64(a, p.rw, p.waves, stream);
+    else launch_tree_bf16_128(a, p.rw, p.waves, stream);
   } else {
-    if (s.d == 64) launch_tree_f32_64(a, p.rw, stream);
-    else launch_tree_f32_128(a, p.rw, stream);
+    if (s.d == 64) launch_tree_f32_64(a, p.rw, p.waves, stream);
+    else launch_tree_f32_128(a, p.rw, p.waves, stream);
   }
   r = launch_status();
   if (r != RADAR_OK || p.parts == 1) return r;

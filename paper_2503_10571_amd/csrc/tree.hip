@@ -212,25 +212,31 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_tree(TreeArgs a) {
 }
 
 template <typename T, int D>
-void launch_tree(const TreeArgs& a, int rw, hipStream_t st) {
+void launch_tree(const TreeArgs& a, int rw, int waves, hipStream_t st) {
   const int64_t pairs = (int64_t)a.B * a.Hkv, units = a.parts ? pairs * a.parts : a.units + pairs;
   const dim3 grid((unsigned)(8 * (units / 8 * a.mtiles + ceil_div(units % 8 * a.mtiles, 8))));
+  if constexpr (sizeof(T) == 2 && D == 128) {
+    if (waves == 8) {
+      if (rw == 2) launch(RADAR_K_ATTEND, k_tree<T, D, 2, 8>, grid, dim3(512), 0, st, a);
+      else launch(RADAR_K_ATTEND, k_tree<T, D, 4, 8>, grid, dim3(512), 0, st, a);
+      return;
+    }
+  }
   if (rw == 1) launch(RADAR_K_ATTEND, k_tree<T, D, 1, 4>, grid, dim3(256), 0, st, a);
   else if (rw == 2) launch(RADAR_K_ATTEND, k_tree<T, D, 2, 4>, grid, dim3(256), 0, st, a);
-  else if (rw == 4) launch(RADAR_K_ATTEND, k_tree<T, D, 4, 4>, grid, dim3(256), 0, st, a);
-  else if constexpr (sizeof(T) == 2) launch(RADAR_K_ATTEND, k_tree<T, D, 4, 8>, grid, dim3(512), 0, st, a);
+  else launch(RADAR_K_ATTEND, k_tree<T, D, 4, 4>, grid, dim3(256), 0, st, a);
 }
 
 }  // namespace
 
 #if RADAR_ATTEND_F32 && RADAR_ATTEND_D == 64
-void launch_tree_f32_64(const TreeArgs& a, int rw, hipStream_t st) { launch_tree<float, 64>(a, rw, st); }
+void launch_tree_f32_64(const TreeArgs& a, int rw, int waves, hipStream_t st) { launch_tree<float, 64>(a, rw, waves, st); }
 #elif RADAR_ATTEND_F32
-void launch_tree_f32_128(const TreeArgs& a, int rw, hipStream_t st) { launch_tree<float, 128>(a, rw, st); }
+void launch_tree_f32_128(const TreeArgs& a, int rw, int waves, hipStream_t st) { launch_tree<float, 128>(a, rw, waves, st); }
 #elif RADAR_ATTEND_D == 64
-void launch_tree_bf16_64(const TreeArgs& a, int rw, hipStream_t st) { launch_tree<bf16_t, 64>(a, rw, st); }
+void launch_tree_bf16_64(const TreeArgs& a, int rw, int waves, hipStream_t st) { launch_tree<bf16_t, 64>(a, rw, waves, st); }
 #else
-void launch_tree_bf16_128(const TreeArgs& a, int rw, hipStream_t st) { launch_tree<bf16_t, 128>(a, rw, st); }
+void launch_tree_bf16_128(const TreeArgs& a, int rw, int waves, hipStream_t st) { launch_tree<bf16_t, 128>(a, rw, waves, st); }
 #endif
 
 }  // namespace radar_impl

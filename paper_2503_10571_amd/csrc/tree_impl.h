@@ -116,10 +116,10 @@ struct TreeBatch {
   }
 };
 
-// tree.hip: rw in {1, 2, 4} row waves
-void launch_tree_bf16_64(const TreeArgs& a, int rw, hipStream_t st);
-void launch_tree_bf16_128(const TreeArgs& a, int rw, hipStream_t st);
-void launch_tree_f32_64(const TreeArgs& a, int rw, hipStream_t st);
-void launch_tree_f32_128(const TreeArgs& a, int rw, hipStream_t st);
+// tree.hip: rw in {1, 2, 4} row waves, in workgroups of 4 waves or (bf16, d = 128, rw > 1) 8
+void launch_tree_bf16_64(const TreeArgs& a, int rw, int waves, hipStream_t st);
+void launch_tree_bf16_128(const TreeArgs& a, int rw, int waves, hipStream_t st);
+void launch_tree_f32_64(const TreeArgs& a, int rw, int waves, hipStream_t st);
+void launch_tree_f32_128(const TreeArgs& a, int rw, int waves, hipStream_t st);
 
 }  // namespace radar_impl

@@ -129,7 +129,8 @@ CASES = [  # B, Hq, Hkv, d, t, N, lens, counts, spread
     (1, 4, 1, 64, 1000, 700, None, None, 0),
     (1, 1, 1, 128, 5, 1500, None, None, 0),
     (40, 4, 2, 64, 50, 6, None, None, 2),                   # more pairs than a wave of blocks needs
-    (1, 32, 8, 128, 8161, 33, None, None, 6),               # two groups of waves to a workgroup
+    (1, 32, 8, 128, 8161, 33, None, None, 6),               # eight waves to a workgroup
+    (2, 32, 16, 128, 4100, 20, None, None, 4),              # the same, of 40 rows
     (2, 16, 4, 128, 9000, 40, None, None, 0),
     (17, 8, 8, 128, 1100, 66, None, None, 9),               # the same, whole
     (70, 2, 1, 64, 3000, 5, "ragged", None, 2),             # more lengths than lanes
@@ -173,7 +174,7 @@ def test_sharp_and_flat(N, dtype):
 
 @DTYPES
 @pytest.mark.parametrize("chain", [False, True])
-@pytest.mark.parametrize("N,t", [(6, 40), (30, 1000), (90, 2500), (40, 17000)])
+@pytest.mark.parametrize("N,t", [(6, 40), (30, 1000), (90, 2500), (40, 17000), (12, 33000)])
 def test_other_branches_do_not_matter(N, t, chain, dtype):
     """NaN and infinities in the rows of some nodes: those who attend them get values
     that are no finite numbers in those dims, the others what they get without."""
