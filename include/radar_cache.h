@@ -14,11 +14,12 @@
  * K and V may lie in pinned host memory mapped for the device. Of the
  * radar_config these calls read batch, n_q_heads, n_kv_heads, head_dim,
  * capacity, kv_dtype and n_sink, with radar.h's limits; the fields of the
- * index and the selection are not read but where a call says so. Workspaces: contents on entry do not
- * matter, and one workspace must not be used by two calls at the same time
- * (two graphs that hold the same one must not be replayed concurrently). The
- * lists of numbers of radar_rotary_axes (axis, pos) and of the calls for drafted
- * tokens and forking lie on their elements' size instead of 16 bytes.
+ * index and the selection are not read but where a call says so. Workspaces:
+ * contents on entry do not matter, and one workspace must not be used by two
+ * calls at the same time (two graphs that hold the same one must not be replayed
+ * concurrently). The lists of numbers of radar_rotary_axes (axis, pos) and of the
+ * calls for drafted tokens and forking lie on their elements' size instead of 16
+ * bytes.
  *
  * The measurement hook of radar.h books their kernels under the kinds that it
  * has: rotations and what moves rows (eviction, acceptance, forking) as
@@ -202,9 +203,10 @@ size_t radar_evict_workspace_bytes(const radar_config* cfg, int64_t t,
  * node of a sequence with lens[b] outside [0, t], counts[b] outside [0, nodes]
  * or len + N_b above the capacity. Requires 1 <= nodes (at most RADAR_MAX_TREE
  * with parent), 0 <= t, t + nodes <= capacity where lens is NULL, t <= capacity
- * where it is not; batch * nodes * n_q_heads < 2^27. With a bf16 cache the weights enter the product with V in 16
- * bits where a kv head has at most 16 query rows (nodes n_q_heads / n_kv_heads),
- * and rounded to bf16 where it has more; everything else is fp32. */
+ * where it is not; batch * nodes * n_q_heads < 2^27. With a bf16 cache the weights
+ * enter the product with V in 16 bits where a kv head has at most 16 query rows
+ * (nodes n_q_heads / n_kv_heads), and rounded to bf16 where it has more;
+ * everything else is fp32. */
 radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q,
                                const void* K, const void* V, int64_t t,
                                const int64_t* lens, int64_t nodes,
@@ -225,12 +227,12 @@ size_t radar_attend_tree_workspace_bytes(const radar_config* cfg, int64_t nodes,
  * [batch][nodes]) receives the nodes met, -1 behind them, accepted (int64
  * [batch]) how many, next (int64 [batch]) the last choice, which no node held.
  * The rows of K and V that the path's nodes have move to len, len + 1, ..; no
- * other row changes, and none does with K and V NULL. new_lens (nullable, int64 [batch]) receives len + accepted;
- * it may be lens itself, and next first (no other two share memory). 1 <= nodes <= RADAR_MAX_TREE, else as
- * above; a sequence with an invalid length or count keeps its rows and gets an
- * empty path, next -1 and new_lens its lens[b]. A node with an invalid parent is
- * never met. The summaries of the index are not touched: radar_extend_index
- * follows. */
+ * other row changes, and none does with K and V NULL. new_lens (nullable, int64
+ * [batch]) receives len + accepted; it may be lens itself, and next first (no
+ * other two share memory). 1 <= nodes <= RADAR_MAX_TREE, else as above; a sequence
+ * with an invalid length or count keeps its rows and gets an empty path, next -1
+ * and new_lens its lens[b]. A node with an invalid parent is never met. The
+ * summaries of the index are not touched: radar_extend_index follows. */
 radar_status radar_accept_tree(const radar_config* cfg, void* K, void* V,
                                int64_t t, const int64_t* lens, int64_t nodes,
                                const int64_t* counts, const int32_t* parent,
@@ -277,7 +279,8 @@ size_t radar_extend_index_workspace_bytes(const radar_config* cfg, int64_t most)
  * new_lens (nullable, int64 [batch]) receives the new lengths and may be lens
  * itself. A src[b] outside [-1, batch) changes nothing of b but its new length,
  * -1; a src[b] whose length is outside [0, t] gives b that length alone. batch
- * at most RADAR_MAX_FORK; 0 <= first, 0 <= t <= capacity. */
+ * at most RADAR_MAX_FORK; 0 <= first, 0 <= t <= capacity; K, V, mass and summaries
+ * share no memory (else RADAR_EINVAL, as for K and V above). */
 #define RADAR_MAX_FORK 2048
 radar_status radar_fork(const radar_config* cfg, void* K, void* V, float* mass,
                         float* summaries, const int64_t* src, int64_t first,

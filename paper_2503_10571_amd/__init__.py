@@ -657,6 +657,8 @@ class RadarLayer:
         from its first token down: ascending) into the cache, and completes the
         index."""
         n, c, t = path.shape[1], self.cfg.seg_len, self.t
+        if t + n > self.cfg.capacity:
+            raise RadarError("keep", 2)
         keep_path(self.cfg, self.K, self.V, t, path)
         self.t += n
         self.pos += n

@@ -564,6 +564,24 @@ bool meet(const int64_t* p, const int64_t* q, int n) {
   return p && q && p != q && std::abs((intptr_t)p - (intptr_t)q) < (intptr_t)n * 8;
 }
 int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
+// what a call moves in place has its own memory
+struct Plane {
+  const void* p;
+  int64_t bytes;
+};
+bool overlap(std::initializer_list<Plane> planes) {
+  for (const Plane& x : planes)
+    for (const Plane& y : planes)
+      if (&x != &y && x.p && y.p && (uintptr_t)x.p <= (uintptr_t)y.p &&
+          (uintptr_t)y.p - (uintptr_t)x.p < (uintptr_t)x.bytes)
+        return true;
+  return false;
+}
+int64_t cache_rows(const Shape& s) { return (int64_t)s.B * s.Hkv * s.cap; }
+bool caches_overlap(const Shape& s, const void* K, const void* V) {
+  const int64_t bytes = cache_rows(s) * s.d * esize(s);
+  return overlap({{K, bytes}, {V, bytes}});
+}
 
 // the index's fields of the config, with radar.h's limits
 radar_status check_index(const radar_config* cfg, Shape* s) {
@@ -615,6 +633,7 @@ radar_status radar_accept_tree(const radar_config* cfg, void* K, void* V, int64_
     return RADAR_EINVAL;
   if (nodes > kMaxTree) return RADAR_EUNSUPPORTED;
   if (t < 0 || t > s.cap || (!lens && nodes > s.cap - t)) return RADAR_ECAPACITY;
+  if (caches_overlap(s, K, V)) return RADAR_EINVAL;
   PathArgs a = path_args(s, K, V, t, lens, nodes, counts, new_lens);
   a.parent = parent; a.parent_shared = parent_shared != 0;
   a.tokens = tokens; a.first = first; a.choice = choice;
@@ -635,6 +654,7 @@ radar_status radar_keep_path(const radar_config* cfg, void* K, void* V, int64_t 
       meet(new_lens, lens, s.B))
     return RADAR_EINVAL;
   if (t < 0 || t > s.cap || n > s.cap) return RADAR_ECAPACITY;
+  if (caches_overlap(s, K, V)) return RADAR_EINVAL;
   PathArgs a = path_args(s, K, V, t, lens, n, counts, new_lens);
   a.given = path;
   launch(RADAR_K_APPEND, k_keep, dim3((unsigned)s.B), dim3((unsigned)path_threads(s)), 0, stream, a);
@@ -693,6 +713,12 @@ radar_status radar_fork(const radar_config* cfg, void* K, void* V, float* mass, 
     return RADAR_EINVAL;
   if (t < 0 || t > s.cap) return RADAR_ECAPACITY;
   if (s.B > RADAR_MAX_FORK) return RADAR_EUNSUPPORTED;
+  const int64_t kv_bytes = cache_rows(s) * s.d * esize(s);
+  if (overlap({{K, kv_bytes},
+               {V, kv_bytes},
+               {mass, cache_rows(s) * 4},
+               {summaries, (int64_t)s.B * s.Hkv * std::max<int64_t>(1, s.s_cap) * s.n * 4}}))
+    return RADAR_EINVAL;
   const bool in_place = new_lens && new_lens == lens;
   ForkArgs a{};
   a.K = static_cast<unsigned char*>(K); a.V = static_cast<unsigned char*>(V);

@@ -167,6 +167,23 @@ def test_fork_refusals(L):
     assert call(new=ODD) == 1 and call(src=P(0x2000), lens=GOOD, new=P(0x1038)) == 1     # or over a part of a list
 
 
+def test_what_moves_in_place_shares_no_memory(L):
+    """Caches, masses or summaries over one another, by one address or by the last 16
+    bytes: refused, before a lane is sent over them."""
+    n = 8 * 8 * 4096                                             # rows; 128 bf16 each
+    far = 0x1000 + n * 256
+    accept = dict(t=100, tail=(None, 9, None, GOOD, 0, GOOD, GOOD, GOOD, GOOD, GOOD, GOOD, None, None))
+    for K, V in ((0x1000, 0x1000), (0x1000, far - 16), (far - 16, 0x1000)):
+        assert L.radar_accept_tree(by(_cfg()), P(K), P(V), accept["t"], *accept["tail"]) == 1
+        assert L.radar_keep_path(by(_cfg()), P(K), P(V), 100, None, GOOD, 9, None, None, None) == 1
+        assert L.radar_fork(by(_cfg()), P(K), P(V), None, None, GOOD, 0, 100, None, None, None) == 1
+    end = far + n * 256                                          # of V
+    summ = 8 * 8 * 16 * 256 * 4
+    for mass, at in ((0x1000, None), (far, None), (end - 16, None), (None, 0x1000), (None, end - 16), (end, end),
+                     (end, end + n * 4 - 16), (end + summ - 16, end)):
+        assert L.radar_fork(by(_cfg()), P(0x1000), P(far), P(mass), P(at), GOOD, 0, 100, None, None, None) == 1, (mass, at)
+
+
 def test_binding_refuses_host_tensors(L):
     cfg = radar.Config(1, 1, 1, 64, 64, 16, 16, 32)
     K = torch.zeros(1, 1, 32, 64, dtype=torch.bfloat16)

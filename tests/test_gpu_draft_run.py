@@ -127,6 +127,10 @@ def test_layer_drafts(dtype, rope, schedule):
     assert layer.t == t + 1 and torch.equal(layer.K[:, :, t], K1)
     with pytest.raises(radar.RadarError):
         layer.draft(rand(B, 90, Hq, d), rand(B, 90, Hkv, d), rand(B, 90, Hkv, d))
+    t, pos = layer.t, layer.pos
+    with pytest.raises(radar.RadarError):                      # more than the cache has room for
+        layer.keep(torch.arange(160 - t + 1, dtype=torch.int32, device="cuda").expand(B, -1).contiguous())
+    assert (layer.t, layer.pos) == (t, pos)
 
 
 def test_layer_with_axes():
