@@ -64,7 +64,8 @@ def declare(L) -> None:
         getattr(L, fn).restype = sz
     for fn in ("radar_rotary", "radar_rotary_fill", "radar_rotary_axes", "radar_rotary_fill_axes",
                "radar_attend_prefix", "radar_attend_accumulate", "radar_evict",
-               "radar_attend_tree", "radar_accept_tree", "radar_keep_path", "radar_extend_index", "radar_fork"):
+               "radar_attend_tree", "radar_accept_tree", "radar_keep_path", "radar_extend_index",
+               "radar_fork"):
         getattr(L, fn).restype = ctypes.c_int
 
 
@@ -592,9 +593,13 @@ def attend_tree(cfg: Config, q, K, V, t: int, parent=None, counts=None, out=None
     return out
 
 
-def _given_or_new(x, name, dtype, shape, device):
+def _given_or_new(x, name, dtype, shape, like):
+    """x, or a new tensor of this shape on the device of `like` (of its shape too where
+    that is it: 0.6 us less)."""
     if x is None:
-        return torch.empty(shape, dtype=dtype, device=device)
+        if like.shape == shape:
+            return torch.empty_like(like, dtype=dtype)
+        return torch.empty(shape, dtype=dtype, device=like.device)
     _need(x, dtype, name, math.prod(shape))
     return x
 
@@ -607,9 +612,9 @@ def accept_tree(cfg: Config, K, V, t: int, tokens, first, choice, parent=None, c
     choice (int64 [B][N]) what after each node. parent (int32 [N] for all, or
     [B][N]; None: a chain) and counts (int64 [B]) as for attend_tree(). The rows
     of the path move up to the sequence's end (K and V None: none do); new_lens
-    (int64 [B], may be lens) receives the new lengths. Returns (path int32 [B][N], -1 behind its nodes;
-    how many int64 [B]; the model's next token int64 [B]). The summaries do not
-    follow: extend_index()."""
+    (int64 [B], may be lens) receives the new lengths. Returns (path int32 [B][N],
+    -1 behind its nodes; how many int64 [B]; the model's next token int64 [B]).
+    The summaries do not follow: extend_index()."""
     if (K is None) != (V is None):
         raise ValueError("K and V come together")
     if K is not None:
@@ -624,10 +629,9 @@ def accept_tree(cfg: Config, K, V, t: int, tokens, first, choice, parent=None, c
     lens = _lens_of(lens, B)
     if new_lens is not None:
         _need(new_lens, torch.int64, "new_lens", B)
-    dev = tokens.device
-    path = _given_or_new(path, "path", torch.int32, (B, N), dev)
-    accepted = _given_or_new(accepted, "accepted", torch.int64, (B,), dev)
-    next_token = _given_or_new(next_token, "next_token", torch.int64, (B,), dev)
+    path = _given_or_new(path, "path", torch.int32, (B, N), tokens)
+    accepted = _given_or_new(accepted, "accepted", torch.int64, (B,), first)
+    next_token = _given_or_new(next_token, "next_token", torch.int64, (B,), first)
     _one_device(tokens, first, choice, parent, counts, lens, new_lens, path, accepted, next_token,
                 K, V)
     _call("radar_accept_tree", tokens, ctypes.byref(cfg.c_struct()), _ptr(K), _ptr(V), t, _ptr(lens),
