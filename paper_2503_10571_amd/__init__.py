@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
 import os
 
 import torch
@@ -73,6 +74,11 @@ class Config:
                        self.head_dim, self.n_features, self.seg_len,
                        self.window, self.capacity, codes[self.dtype], self.n_sink,
                        self.gqa_mode, codes[self.omega_dtype])
+
+    @functools.cached_property
+    def _c(self) -> _Config:
+        """c_struct(), made once (0.4 us of a call): read only."""
+        return self.c_struct()
 
     @property
     def summary_rows(self) -> int:

@@ -243,13 +243,14 @@ def _positions(pos, B, T, name="pos", rope=None):
     if isinstance(pos, int):
         return pos, None, 0
     _need(pos, torch.int64, name)
-    if pos.dim() == 1 and pos.numel() == B:
+    shape = pos.shape
+    if shape == (B,):
         return 0, pos, 0
-    if tuple(pos.shape) == (B, T):
+    if shape == (B, T):
         return 0, pos, 1
     if rope is not None and rope.axis is not None:
-        if pos.dim() == 3 and tuple(pos.shape[1:]) == (B, T) and pos.shape[0] > 0:
-            return 0, pos, -pos.shape[0]
+        if len(shape) == 3 and shape[1:] == (B, T) and shape[0] > 0:
+            return 0, pos, -shape[0]
         raise ValueError(f"{name} must be an int or int64 [B], [B][T] or [axes][B][T]")
     raise ValueError(f"{name} must be an int, int64 [B] or int64 [B][T]")
 
@@ -409,10 +410,10 @@ def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_ou
     lens = _lens_of(lens, B)
     _one_device(k, v, q, rows, p, lens, rope.inv_freq, K, V)
     if T and each < 0:
-        _call("radar_rotary_fill_axes", k, by(cfg.c_struct()), by(rope._c), -each, _ptr(rope.axis),
+        _call("radar_rotary_fill_axes", k, by(cfg._c), by(rope._c), -each, _ptr(rope.axis),
               T, rq, qo, by(rk), by(rv), _ptr(K), _ptr(V), r0, _ptr(rows), _ptr(p), _ptr(lens))
     elif T:
-        _call("radar_rotary_fill", k, by(cfg.c_struct()), by(rope._c), T, rq, qo, by(rk), by(rv),
+        _call("radar_rotary_fill", k, by(cfg._c), by(rope._c), T, rq, qo, by(rk), by(rv),
               _ptr(K), _ptr(V), r0, _ptr(rows), p0, _ptr(p), each, _ptr(lens))
     return q_out
 
@@ -420,13 +421,13 @@ def rotary_fill(cfg: Config, rope: Rope, K, V, k, v, row, pos=None, q=None, q_ou
 # ---- attention over a shared prefix, and with accumulated weights --------------
 def attend_prefix_workspace_bytes(cfg: Config, prefix_len: int, t: int) -> int:
     """Scratch for every call with this config, at most this prefix_len and t."""
-    return int(lib().radar_attend_prefix_workspace_bytes(ctypes.byref(cfg.c_struct()),
+    return int(lib().radar_attend_prefix_workspace_bytes(ctypes.byref(cfg._c),
                                                          prefix_len, t))
 
 
 def attend_accumulate_workspace_bytes(cfg: Config, t: int) -> int:
     """Scratch for every call with this config and at most this t."""
-    return int(lib().radar_attend_accumulate_workspace_bytes(ctypes.byref(cfg.c_struct()), t))
+    return int(lib().radar_attend_accumulate_workspace_bytes(ctypes.byref(cfg._c), t))
 
 
 def _workspace(given, nbytes, device):
@@ -471,7 +472,7 @@ def attend_prefix(cfg: Config, q, Kp, Vp, prefix_len: int, K=None, V=None, t: in
             raise ValueError("K and V are needed with t > 0")
         _cache(cfg, K, V)
     _one_device(q, Kp, Vp, K, V, out, lens, workspace)
-    c = ctypes.byref(cfg.c_struct())
+    c = ctypes.byref(cfg._c)
     need = lib().radar_attend_prefix_workspace_bytes(c, prefix_len, t) if workspace is None else 0
     workspace, n = _workspace(workspace, need, q.device)
     _call("radar_attend_prefix", q, c, _ptr(q), _ptr(Kp), _ptr(Vp), prefix_len, prefix_cap,
@@ -500,7 +501,7 @@ def attend_accumulate(cfg: Config, q, K, V, mass, t: int, out=None, lens=None,
     _cache(cfg, K, V)
     _mass(cfg, mass)
     _one_device(q, K, V, mass, out, lens, workspace)
-    c = ctypes.byref(cfg.c_struct())
+    c = ctypes.byref(cfg._c)
     need = lib().radar_attend_accumulate_workspace_bytes(c, t) if workspace is None else 0
     workspace, n = _workspace(workspace, need, q.device)
     _call("radar_attend_accumulate", q, c, _ptr(q), _ptr(K), _ptr(V), _ptr(mass), t,
@@ -512,7 +513,7 @@ def attend_accumulate(cfg: Config, q, K, V, mass, t: int, out=None, lens=None,
 def evict_workspace_bytes(cfg: Config, t: int, heavy: int, recent: int) -> int:
     """Scratch for every call with this config, at most this t and at most as
     many kept rows."""
-    return int(lib().radar_evict_workspace_bytes(ctypes.byref(cfg.c_struct()), t, heavy,
+    return int(lib().radar_evict_workspace_bytes(ctypes.byref(cfg._c), t, heavy,
                                                  recent))
 
 
@@ -534,7 +535,7 @@ def evict(cfg: Config, K, V, mass, t: int, heavy: int, recent: int, lens=None,
     if kept is not None:
         _need(kept, torch.int32, "kept", cfg.batch * cfg.n_kv_heads * n)
     _one_device(mass, K, V, lens, new_lens, kept, workspace)
-    c = ctypes.byref(cfg.c_struct())
+    c = ctypes.byref(cfg._c)
     need = (lib().radar_evict_workspace_bytes(c, t, heavy, recent)
             if workspace is None else 0)
     workspace, size = _workspace(workspace, need, mass.device)
@@ -550,7 +551,7 @@ def _nodes(cfg, parent, counts, N):
     if parent is not None:
         _need(parent, torch.int32, "parent")
         shared = 1 if parent.dim() == 1 else 0
-        if tuple(parent.shape) not in ((N,), (cfg.batch, N)):
+        if parent.shape != ((N,) if shared else (cfg.batch, N)):
             raise ValueError(f"parent must be [{N}] or [{cfg.batch}][{N}], got {list(parent.shape)}")
     if counts is not None:
         _need(counts, torch.int64, "counts", cfg.batch)
@@ -560,7 +561,7 @@ def _nodes(cfg, parent, counts, N):
 def attend_tree_workspace_bytes(cfg: Config, nodes: int, t: int) -> int:
     """Scratch for every call with this config, at most this many nodes and at most
     this t."""
-    return int(lib().radar_attend_tree_workspace_bytes(ctypes.byref(cfg.c_struct()), nodes, t))
+    return int(lib().radar_attend_tree_workspace_bytes(ctypes.byref(cfg._c), nodes, t))
 
 
 def attend_tree(cfg: Config, q, K, V, t: int, parent=None, counts=None, out=None, lens=None,
@@ -585,7 +586,7 @@ def attend_tree(cfg: Config, q, K, V, t: int, parent=None, counts=None, out=None
     out, ro = _out_rows(q, out, "out", counts)
     _one_device(q, K, V, parent, counts, lens, out, workspace)
     by = ctypes.byref
-    c = by(cfg.c_struct())
+    c = by(cfg._c)
     need = lib().radar_attend_tree_workspace_bytes(c, N, t) if workspace is None else 0
     workspace, n = _workspace(workspace, need, q.device)
     _call("radar_attend_tree", q, c, by(rq), _ptr(K), _ptr(V), t, _ptr(lens), N, _ptr(counts),
@@ -634,7 +635,7 @@ def accept_tree(cfg: Config, K, V, t: int, tokens, first, choice, parent=None, c
     next_token = _given_or_new(next_token, "next_token", torch.int64, (B,), first)
     _one_device(tokens, first, choice, parent, counts, lens, new_lens, path, accepted, next_token,
                 K, V)
-    _call("radar_accept_tree", tokens, ctypes.byref(cfg.c_struct()), _ptr(K), _ptr(V), t, _ptr(lens),
+    _call("radar_accept_tree", tokens, ctypes.byref(cfg._c), _ptr(K), _ptr(V), t, _ptr(lens),
           N, _ptr(counts), _ptr(parent), shared, _ptr(tokens), _ptr(first), _ptr(choice), _ptr(path),
           _ptr(accepted), _ptr(next_token), _ptr(new_lens))
     return path, accepted, next_token
@@ -654,13 +655,13 @@ def keep_path(cfg: Config, K, V, t: int, path, counts=None, lens=None, new_lens=
         if x is not None:
             _need(x, torch.int64, name, cfg.batch)
     _one_device(path, counts, lens, new_lens, K, V)
-    _call("radar_keep_path", path, ctypes.byref(cfg.c_struct()), _ptr(K), _ptr(V), t, _ptr(lens),
+    _call("radar_keep_path", path, ctypes.byref(cfg._c), _ptr(K), _ptr(V), t, _ptr(lens),
           _ptr(path), path.shape[1], _ptr(counts), _ptr(new_lens))
 
 
 def extend_index_workspace_bytes(cfg: Config, most: int) -> int:
     """Scratch for every call with this config and at most this `most`."""
-    return int(lib().radar_extend_index_workspace_bytes(ctypes.byref(cfg.c_struct()), most))
+    return int(lib().radar_extend_index_workspace_bytes(ctypes.byref(cfg._c), most))
 
 
 def extend_index(cfg: Config, K, omega, t0: int, t: int, summaries, lens0=None, lens=None,
@@ -678,7 +679,7 @@ def extend_index(cfg: Config, K, omega, t0: int, t: int, summaries, lens0=None, 
         _need(lens0, torch.int64, "lens0", cfg.batch)
         _need(lens, torch.int64, "lens", cfg.batch)
     _one_device(summaries, K, omega, lens0, lens, workspace)
-    c, n = ctypes.byref(cfg.c_struct()), 0
+    c, n = ctypes.byref(cfg._c), 0
     if most is None:
         most = t - t0
     if lens is not None:
@@ -707,5 +708,5 @@ def fork(cfg: Config, K, V, src, t: int, first: int = 0, lens=None, new_lens=Non
     if summaries is not None:
         _summ(cfg, summaries)
     _one_device(src, K, V, lens, new_lens, mass, summaries)
-    _call("radar_fork", src, ctypes.byref(cfg.c_struct()), _ptr(K), _ptr(V), _ptr(mass),
+    _call("radar_fork", src, ctypes.byref(cfg._c), _ptr(K), _ptr(V), _ptr(mass),
           _ptr(summaries), _ptr(src), first, t, _ptr(lens), _ptr(new_lens))
