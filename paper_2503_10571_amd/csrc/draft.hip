@@ -121,15 +121,30 @@ int tree_waves(const Shape& s, int64_t M) {
 }
 
 // How a call is cut: as many workgroups as the chip holds at once, or fewer, with at least
-// kLeast rows each (fewer cost more in partials than they gain: four sequences of 2000 rows
-// and 16 nodes, 32 query heads: 21.1 us, with 128 rows 25.9; one of 4096 and 8 nodes: 15.5,
-// with 512 rows 17.4). Pairs of one length that nearly fill the chip, those of any that
-// fill it twice and those of up to kShort steps stay whole.
-constexpr int kLeast = 256, kShort = 4;
+// 256 rows each in bf16 (fewer cost more in partials than they gain: four sequences of 2000
+// rows and 16 nodes, 32 query heads: 21.1 us, with 128 rows 25.9; one of 4096 and 8 nodes:
+// 15.5, with 512 rows 17.4) and 64 in fp32, whose products take eight times as long (16 nodes
+// over 1000 rows: 19.7 us, with 256 rows 33; 121 over 400: 43, 52). Pairs of one length that
+// nearly fill the chip, those of any that fill it twice and those of up to four steps (in
+// fp32: of one) stay whole.
+int least_rows(const Shape& s) { return esize(s) == 4 ? 64 : 256; }
+int short_steps(const Shape& s) { return esize(s) == 4 ? 1 : 4; }
 
 struct TreePlan {
   int rw, waves, mtiles, rows_per_tile, step, parts, units;
 };
+
+// Whether cutting a pair's steps into so many parts saves more than the merge takes: steps of
+// 64 and 128 query rows, of 0.8 and 1.1 us in bf16 at head dim 128, against 3 us and the
+// partials there and back at 5 TB/s (chunks of 500 tokens, 32 / 8 heads: behind 250, whole 25
+// us, cut 32; behind 1000, 40.7 and 37.2).
+bool worth(const Shape& s, const TreePlan& p, int64_t steps, int64_t parts, int64_t M) {
+  if (p.rw == 1) return true;
+  double step_ns = (p.rw == 4 ? 1100. : 800.) * s.d / 128 * (p.waves / 4);
+  if (esize(s) == 4) step_ns = 3500. * s.d / 128;
+  const double saved = step_ns * (double)(steps - ceil_div(steps, parts));
+  return saved > 3000. + (double)s.B * s.Hkv * M * parts * s.d * 4 * 2 / 5000;
+}
 
 TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
   TreePlan p;
@@ -154,22 +169,26 @@ TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
     p.step *= 2;
     room /= 2;
   }
-  // Up to 32 query rows a pair in bf16, whose waves have tiles of their own: one workgroup a
-  // CU asks for as much as two, with half the partials (8 nodes over 64K rows: 56 us, 51;
-  // 32 sequences of 1000 rows, whole: 38, 29; but one token each, 16 sequences of 4000:
-  // 53.5, 56).
-  const bool one = p.rw == 1 && s.dt == RADAR_BF16;
+  // Up to 32 query rows a pair in bf16 (16 in fp32), whose waves have tiles of their own: one
+  // workgroup a CU asks for as much as two, with half the partials (8 nodes over 64K rows: 56
+  // us, 51; 32 sequences of 1000 rows, whole: 38, 29; in fp32 4 nodes over 16000: 33, 29.5;
+  // but one token each, 16 sequences of 4000: 53.5, 56). And more than 48 in fp32, where the
+  // matrix cores bound and one workgroup keeps them busy (32 nodes over 4000: 38.3, 34.5; 60
+  // and 30 over 1500 and 750, 16 heads: 41.9, 35.4).
+  const bool one = p.rw > 1 ? esize(s) == 4 : p.mtiles == 1;
   if (one) room /= 2;
   const int64_t steps = ceil_div(t + nodes, p.step);
   p.units = 0;
-  if (ragged && steps > kShort && blocks <= 2 * room && pairs * steps < (1ll << 31)) {
+  const int64_t least = least_rows(s);
+  if (ragged && steps > short_steps(s) && blocks <= 2 * room && pairs * steps < (1ll << 31)) {
     // (a pair's last part is shorter: as many more parts as there are pairs, at most)
     const int64_t units = std::max<int64_t>(1, room / p.mtiles);
     p.parts = 0;
     p.units = (int)std::max(units - (one ? pairs / 2 : pairs), (units + 1) / 2);
+    if (!worth(s, p, steps, std::min(p.units / pairs + 2, ceil_div(t + nodes, least)), M)) p.parts = 1;
   } else {
-    p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(room / blocks, ceil_div(t + nodes, kLeast)));
-    if (steps <= kShort) p.parts = 1;
+    p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(room / blocks, ceil_div(t + nodes, least)));
+    if (steps <= short_steps(s) || !worth(s, p, steps, p.parts, M)) p.parts = 1;
     // (as many of one length)
     p.parts = (int)ceil_div(steps, ceil_div(steps, p.parts));
   }
@@ -250,7 +269,7 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, con
   a.K = K; a.V = V; a.lens = lens; a.counts = counts; a.t = t; a.cap = s.cap;
   a.nodes = (int)nodes; a.parent = parent; a.parent_shared = parent_shared != 0;
   a.mtiles = p.mtiles; a.M = (int)(nodes * s.G);
-  a.parts = p.parts; a.units = p.units; a.least = kLeast / p.step;
+  a.parts = p.parts; a.units = p.units; a.least = std::max(1, least_rows(s) / p.step);
   a.g_log2 = log2_of(s.G); a.step_log2 = log2_of(p.step);
   a.acc = static_cast<float*>(workspace);
   a.ml = reinterpret_cast<float*>(static_cast<unsigned char*>(workspace) + w.ml);

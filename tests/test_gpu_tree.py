@@ -136,6 +136,11 @@ CASES = [  # B, Hq, Hkv, d, t, N, lens, counts, spread
     (70, 2, 1, 64, 3000, 5, "ragged", None, 2),             # more lengths than lanes
     (130, 1, 1, 128, 700, 20, "ragged", "ragged", 3),
     (150, 4, 4, 64, 600, 3, "ragged", None, 1),             # more pairs than parts
+    (3, 16, 4, 128, 2100, 40, [2100, 900, 5], [40, 31, 40], 5),      # cut, with row tiles
+    (3, 32, 8, 128, 500, 130, [500, 17, 0], [130, 128, 129], 0),     # whole: the merge would cost more
+    (2, 32, 8, 128, 400, 250, None, None, 0),
+    (1, 8, 2, 128, 100, 30, None, None, 3),                 # parts of few steps in 32 bits
+    (4, 4, 2, 64, 200, 8, "ragged", None, 2),
 ]
 
 
