@@ -181,7 +181,6 @@ struct ForkArgs {
   int row_bytes;
   int c, n_sink, summ_bytes;         // of a summary
   int64_t summ_rows;
-  int64_t units[3];        // columns of K (and V), masses and summaries, per head
 };
 
 __device__ __forceinline__ int64_t fork_len(const ForkArgs& a, int64_t s) {
@@ -379,19 +378,22 @@ __device__ __forceinline__ int64_t fork_planes(ForkPlane p, const ForkList& l, i
   return turn + all;
 }
 
+// (rows: of the longest sequence that a move reads; all: or writes)
 template <int COLS, bool NT>
-__device__ __forceinline__ void fork_all(const ForkArgs& a, const ForkList& l) {
-  const ForkPlane kv{a.K + a.first * a.row_bytes, a.V - a.K, a.cap * a.row_bytes, a.Hkv * a.cap * a.row_bytes,
-                     a.units[0], a.first, 0, 1, a.row_bytes / 16, 0};
+__device__ __forceinline__ void fork_all(const ForkArgs& a, const ForkList& l, int rows, int all) {
+  ForkPlane kv{a.K + a.first * a.row_bytes, a.V - a.K, a.cap * a.row_bytes, a.Hkv * a.cap * a.row_bytes,
+               0, a.first, 0, 1, a.row_bytes / 16, 0};
+  kv.units = kv.columns(rows);
   int64_t turn = fork_planes<u32x4_t, COLS, false, NT>(kv, l, 2 * a.Hkv, 0);
-  if (a.units[1]) {
-    const ForkPlane mass{a.mass, 0, a.cap * 4, a.Hkv * a.cap * 4, a.units[1], 0, 0, 1, 1, 0};
+  if (a.mass) {
+    const ForkPlane mass{a.mass, 0, a.cap * 4, a.Hkv * a.cap * 4, all, 0, 0, 1, 1, 0};
     turn = fork_planes<uint32_t, COLS, true, false>(mass, l, a.Hkv, turn);
   }
-  if (a.units[2]) {
+  if (a.summ) {
     const int64_t seg0 = max((int64_t)0, a.first - a.n_sink) / a.c;
-    const ForkPlane summ{a.summ + seg0 * a.summ_bytes, 0, a.summ_rows * a.summ_bytes,
-                         a.Hkv * a.summ_rows * a.summ_bytes, a.units[2], seg0, a.n_sink, a.c, a.summ_bytes / 16, 0};
+    ForkPlane summ{a.summ + seg0 * a.summ_bytes, 0, a.summ_rows * a.summ_bytes,
+                   a.Hkv * a.summ_rows * a.summ_bytes, 0, seg0, a.n_sink, a.c, a.summ_bytes / 16, 0};
+    summ.units = summ.columns(rows);
     fork_planes<u32x4_t, COLS, false, false>(summ, l, a.Hkv, turn);
   }
 }
@@ -445,10 +447,12 @@ __global__ __launch_bounds__(kForkThreads) void k_fork(ForkArgs a) {
   uint32_t* list = reinterpret_cast<uint32_t*>(len + lds_b);   // dst << 16 | src
   __shared__ int n_list;
   __shared__ u64 moved;                    // rows of K
+  __shared__ int longest[2];               // rows of a sequence that is read; or written
   const int tid = threadIdx.x;
   if (tid == 0) {
     n_list = 0;
     moved = 0;
+    longest[0] = longest[1] = 0;
   }
   auto kind = [&](int64_t s, int b) {
     return s >= 0 && s < a.B && s != b && len[s] >= 0 ? (int)s : s == -1 ? kFreed : kStay;
@@ -515,21 +519,30 @@ __global__ __launch_bounds__(kForkThreads) void k_fork(ForkArgs a) {
   if (n == 0) return;
   // past the caches, of 256 MB, where the call moves more than they hold
   int64_t rows = 0;
+  int most = 0, most_old = 0;
   for (int e = tid; e < n; e += kForkThreads) {
-    const uint32_t from = list[e] & 0x7fffu;
-    rows += from == kZero ? 0 : max((int64_t)0, len[from] - a.first);
+    const uint32_t from = list[e] & 0x7fffu, dst = list[e] >> 16;
+    if (from != kZero) {
+      rows += max((int64_t)0, len[from] - a.first);
+      most = max(most, len[from]);
+    }
+    if (dst != kNone) most_old = max(most_old, len[dst]);
   }
-  atomicAdd(&moved, (u64)rows);
+  if (tid < n) {
+    atomicAdd(&moved, (u64)rows);
+    atomicMax(&longest[0], most);
+    atomicMax(&longest[1], max(most, most_old));
+  }
   __syncthreads();
   const bool past = 4 * a.Hkv * (int64_t)moved * a.row_bytes > (256 << 20);
   const ForkList l{list, len, n};
   // few moves: two columns of each in flight
   if (n <= 4) {
-    if (past) fork_all<2, true>(a, l);
-    else fork_all<2, false>(a, l);
+    if (past) fork_all<2, true>(a, l, longest[0], longest[1]);
+    else fork_all<2, false>(a, l, longest[0], longest[1]);
   } else {
-    if (past) fork_all<1, true>(a, l);
-    else fork_all<1, false>(a, l);
+    if (past) fork_all<1, true>(a, l, longest[0], longest[1]);
+    else fork_all<1, false>(a, l, longest[0], longest[1]);
   }
 }
 
@@ -727,16 +740,15 @@ radar_status radar_fork(const radar_config* cfg, void* K, void* V, float* mass, 
   a.B = s.B; a.Hkv = s.Hkv; a.t = t; a.first = std::min(first, t); a.cap = s.cap;
   a.row_bytes = s.d * esize(s);
   a.n_sink = s.n_sink;
-  a.units[0] = (t - a.first) * (a.row_bytes / 16);
-  if (mass) a.units[1] = t;
+  int64_t units[3] = {(t - a.first) * (a.row_bytes / 16), mass ? t : 0, 0};      // columns of a head, at most
   if (summaries) {
     a.c = s.c; a.summ_bytes = s.n * 4; a.summ_rows = std::max<int64_t>(1, s.s_cap);
     const int64_t seg0 = std::max<int64_t>(0, a.first - s.n_sink) / s.c;
     const int64_t seg1 = std::max<int64_t>(0, t - s.n_sink) / s.c;
-    a.units[2] = (seg1 - seg0) * (a.summ_bytes / 16);
+    units[2] = (seg1 - seg0) * (a.summ_bytes / 16);
   }
-  const int64_t items = s.Hkv * (2 * ceil_div(a.units[0], kForkThreads) + ceil_div(a.units[1], kForkThreads) +
-                                 ceil_div(a.units[2], kForkThreads));
+  const int64_t items = s.Hkv * (2 * ceil_div(units[0], kForkThreads) + ceil_div(units[1], kForkThreads) +
+                                 ceil_div(units[2], kForkThreads));
   // three words a sequence (of a wave's, at least), and up to 3/2 in the list
   const size_t lds = (size_t)std::max(s.B, kWave) * 18;
   const unsigned grid = (unsigned)std::max<int64_t>(1, std::min<int64_t>(items, 4 * num_cu()));
