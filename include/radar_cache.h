@@ -188,17 +188,22 @@ size_t radar_evict_workspace_bytes(const radar_config* cfg, int64_t t,
  * its nodes (counts, nullable device int64 [batch], 0 .. nodes; else nodes).
  * parent names the node that each one follows, always one before it, or -1: it
  * follows the sequence's last row (device int32, [batch][nodes], or one list
- * [nodes] for all with parent_shared). parent NULL: a chain, node i follows
+ * [nodes] for all with parent_shared or that flag). parent NULL: a chain, node i follows
  * node i - 1. */
 #define RADAR_MAX_TREE 512      /* most nodes where a parent list is given */
+
+/* flags of radar_attend_tree: parent is one list for all sequences; the outputs of
+ * nodes from N_b on become 0 */
+#define RADAR_TREE_SHARED 1
+#define RADAR_TREE_ZERO 2
 
 /* Query row (b, i, q head) attends rows [0, len) of K and V and the rows of node
  * i and of the nodes above it (its parent, the parent's, ..): exact softmax
  * attention with the scale 1/sqrt(head_dim). q and out are rows [batch][nodes]
  * [n_q_heads][head_dim] (see radar_rows); out may be q (the same address and
- * strides), there is no other overlap. Nodes from N_b on are
- * neither read nor written, and what the rows hold that a node does not attend,
- * NaN and infinities too, does not matter to it. A node whose list of parents leaves the tree
+ * strides), there is no other overlap. Nodes from N_b on are neither read nor,
+ * without RADAR_TREE_ZERO in flags, written, and what the rows hold that a node
+ * does not attend, NaN and infinities too, does not matter to it. A node whose list of parents leaves the tree
  * (a parent below -1 or not before its child) gets NaN outputs; so does every
  * node of a sequence with lens[b] outside [0, t], counts[b] outside [0, nodes]
  * or len + N_b above the capacity. Requires 1 <= nodes (at most RADAR_MAX_TREE
@@ -211,7 +216,7 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q,
                                const void* K, const void* V, int64_t t,
                                const int64_t* lens, int64_t nodes,
                                const int64_t* counts, const int32_t* parent,
-                               int32_t parent_shared, const radar_rows* out,
+                               int32_t flags, const radar_rows* out,
                                void* workspace, size_t workspace_bytes,
                                hipStream_t stream);
 

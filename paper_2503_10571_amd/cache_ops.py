@@ -583,14 +583,15 @@ def attend_tree(cfg: Config, q, K, V, t: int, parent=None, counts=None, out=None
     _cache(cfg, K, V)
     parent, shared, counts = _nodes(cfg, parent, counts, N)
     lens = _lens_of(lens, B)
-    out, ro = _out_rows(q, out, "out", counts)
+    flags = shared if out is not None else shared | 2          # RADAR_TREE_ZERO
+    out, ro = _out_rows(q, out, "out", None)
     _one_device(q, K, V, parent, counts, lens, out, workspace)
     by = ctypes.byref
     c = by(cfg._c)
     need = lib().radar_attend_tree_workspace_bytes(c, N, t) if workspace is None else 0
     workspace, n = _workspace(workspace, need, q.device)
     _call("radar_attend_tree", q, c, by(rq), _ptr(K), _ptr(V), t, _ptr(lens), N, _ptr(counts),
-          _ptr(parent), shared, by(ro), _ptr(workspace), n)
+          _ptr(parent), flags, by(ro), _ptr(workspace), n)
     return out
 
 

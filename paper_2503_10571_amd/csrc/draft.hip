@@ -38,8 +38,9 @@ __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_til
     const int64_t b = x / a.Hq / a.nodes;
     const TreeSeq s = batch.seq(__builtin_amdgcn_readfirstlane((int)b));
     T* o = static_cast<T*>(a.out) + b * a.o_seq + node * a.o_node + hq * a.o_head;
-    if (s.rows < 0) {
-      for (int i = tid; i < D; i += kThreads) o[i] = from_f32<T>(__uint_as_float(0x7fc00000u));
+    if (s.rows < 0 || (a.zero && node >= s.nodes)) {
+      const T x = from_f32<T>(s.rows < 0 ? __uint_as_float(0x7fc00000u) : 0.f);
+      for (int i = tid; i < D; i += kThreads) o[i] = x;
       continue;
     }
     if (node >= s.nodes) continue;
@@ -246,14 +247,14 @@ size_t radar_attend_tree_workspace_bytes(const radar_config* cfg, int64_t nodes,
 radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, const void* K,
                                const void* V, int64_t t, const int64_t* lens, int64_t nodes,
                                const int64_t* counts, const int32_t* parent,
-                               int32_t parent_shared, const radar_rows* out, void* workspace,
+                               int32_t flags, const radar_rows* out, void* workspace,
                                size_t workspace_bytes, hipStream_t stream) {
   Shape s;
   radar_status r = check_cache(cfg, &s);
   if (r != RADAR_OK) return r;
   const int esz = esize(s);
   if (!good_rows(q, esz) || !good_rows(out, esz) || bad16(K) || bad16(V) || off(lens) || off(counts) ||
-      off(parent))
+      off(parent) || (flags & ~(RADAR_TREE_SHARED | RADAR_TREE_ZERO)))
     return RADAR_EINVAL;
   r = check_nodes(s, nodes, parent != nullptr);
   if (r != RADAR_OK) return r;
@@ -267,7 +268,7 @@ radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q, con
   a.B = s.B; a.Hq = s.Hq; a.Hkv = s.Hkv; a.G = s.G;
   a.qscale = kLog2e / std::sqrt((float)s.d);
   a.K = K; a.V = V; a.lens = lens; a.counts = counts; a.t = t; a.cap = s.cap;
-  a.nodes = (int)nodes; a.parent = parent; a.parent_shared = parent_shared != 0;
+  a.nodes = (int)nodes; a.parent = parent; a.parent_shared = flags & RADAR_TREE_SHARED; a.zero = (flags & RADAR_TREE_ZERO) && counts;
   a.mtiles = p.mtiles; a.M = (int)(nodes * s.G);
   a.parts = p.parts; a.units = p.units; a.least = std::max(1, least_rows(s) / p.step);
   a.g_log2 = log2_of(s.G); a.step_log2 = log2_of(p.step);

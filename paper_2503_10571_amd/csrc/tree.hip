@@ -177,6 +177,9 @@ __global__ __launch_bounds__(WAVES * 64, 2) void k_tree(TreeArgs a) {
     return;
   }
   const int rows = min(kRows, s.nodes * a.G - row0);
+  if (a.zero && a.parts == 1)              // uniform (parts = 0: the merge does it)
+    for (int y = 4 * threadIdx.x + max(rows, 0) * D; y < min(kRows, a.M - row0) * D; y += 4 * WAVES * 64)
+      store4(static_cast<T*>(mask.out_row(y / D)) + y % D, 0.f, 0.f, 0.f, 0.f);
   if (rows <= 0) return;
   const int64_t end = tree_end(a, s, row0 + rows), step = (int64_t)cut.each * F::NTG;
   const int64_t r0 = part * step, r1 = min(end, r0 + step);

@@ -24,7 +24,7 @@ struct TreeArgs {
   int64_t t, cap;
   int nodes;
   const int* parent;         // [B][nodes], or [nodes] if shared; null: a chain
-  int parent_shared;
+  int parent_shared, zero;   // zero: outputs of nodes behind a sequence's own become 0
   int mtiles, M;             // M = nodes G query rows of a pair
   int parts, units, least, g_log2;     // least: steps of a part, at least
   int step_log2;             // rows of a step

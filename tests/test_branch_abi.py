@@ -90,6 +90,17 @@ def test_tree_refusals(L):
     assert L.radar_attend_tree_workspace_bytes(by(_cfg(head_dim=96)), 9, 100) == 0
 
 
+def test_tree_flags(L):
+    """Shared, zeros behind the nodes, both; no others."""
+    rows = by(cache_ops._Rows(0x1000, 32768, 4096, 128))
+    for flags in (4, 8, 7, -1, 1 << 31 - 1):
+        assert L.radar_attend_tree(by(_cfg()), rows, GOOD, GOOD, 100, None, 9, None, GOOD, flags, rows, GOOD, 1 << 30,
+                                   None) == 1, flags
+    for flags in (0, 1, 2, 3):                                   # (as far as the workspace)
+        assert L.radar_attend_tree(by(_cfg()), rows, GOOD, GOOD, 100, None, 9, None, GOOD, flags, rows, GOOD, 0,
+                                   None) == 5, flags
+
+
 def test_accept_refusals(L):
     def call(cfg=_cfg(), K=GOOD, V=GOOD, t=100, lens=None, nodes=9, counts=None, parent=GOOD, tokens=GOOD, first=GOOD,
              choice=GOOD, path=GOOD, accepted=GOOD, nxt=GOOD, new=None):

@@ -166,6 +166,28 @@ def test_where_the_drafted_rows_begin(t, dtype):
 
 
 @DTYPES
+@pytest.mark.parametrize("t,N,G", [(5, 1, 1), (40, 9, 4), (900, 9, 4), (900, 30, 4), (30, 130, 4), (2500, 130, 1)])
+def test_zeros_behind_the_nodes(t, N, G, dtype):
+    """A new out where another tensor was: zeros from the counts on, of sequences with
+    none too, whether blocks or the merge write the outputs."""
+    B, Hkv, d = 5, 2, 128
+    counts = torch.tensor([N, 0, N // 2, 1, max(0, N - 1)], device="cuda")
+    lens = torch.tensor([t, t, t // 2, 0, 1], device="cuda")
+    q, K, V = _inputs(B, Hkv * G, Hkv, d, t, N, lens.tolist(), [N] * B, dtype)
+    cfg = _cfg(B, Hkv * G, Hkv, d, K.shape[2], dtype)
+    ws = torch.empty(radar.attend_tree_workspace_bytes(cfg, N, t), dtype=torch.uint8, device="cuda")
+    given = torch.full_like(q, 5.0)
+    radar.attend_tree(cfg, q, K, V, t, lens=lens, counts=counts, workspace=ws, out=given)
+    old = torch.full_like(q, float("nan"))
+    at = old.data_ptr()
+    del old
+    out = radar.attend_tree(cfg, q, K, V, t, lens=lens, counts=counts, workspace=ws)
+    assert out.data_ptr() == at
+    for b, n in enumerate(counts.tolist()):
+        assert torch.equal(out[b, :n], given[b, :n]) and bool((out[b, n:] == 0).all()) and bool((given[b, n:] == 5).all())
+
+
+@DTYPES
 def test_shared_tree(dtype):
     _run(3, 8, 2, 64, 100, 20, [100, 50, 0], [20, 7, 19], 4, dtype, shared=True)
 
