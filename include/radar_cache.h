@@ -210,8 +210,8 @@ size_t radar_evict_workspace_bytes(const radar_config* cfg, int64_t t,
  * with parent), 0 <= t, t + nodes <= capacity where lens is NULL, t <= capacity
  * where it is not; batch * nodes * n_q_heads < 2^27. With a bf16 cache the weights
  * enter the product with V in 16 bits where a kv head has at most 16 query rows
- * (nodes n_q_heads / n_kv_heads), and rounded to bf16 where it has more;
- * everything else is fp32. */
+ * (nodes n_q_heads / n_kv_heads), and are rounded to bf16 in most of the rows
+ * where it has more; everything else is fp32. */
 radar_status radar_attend_tree(const radar_config* cfg, const radar_rows* q,
                                const void* K, const void* V, int64_t t,
                                const int64_t* lens, int64_t nodes,

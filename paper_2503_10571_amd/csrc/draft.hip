@@ -6,11 +6,12 @@ namespace radar_impl {
 namespace {
 
 constexpr int kSlots = 512;                // workgroups that the chip holds at once
-constexpr int kFew = 128;                  // partials of a row that one wave merges
+constexpr int kFew = 256;                  // partials of a row that one wave merges
 
 // A query row's output from its partials by NW waves: D / 4 lanes on four dims each of one
 // partial, the others on the next. One wave a row where there are enough rows to fill the
-// chip (8192 rows of up to 13 partials, 29 MB: 10 us; 1024 of 63: 5.5 with four).
+// chip (8192 rows of up to 13 partials, 29 MB: 10 us; 1024 of 63: 5.5 with four; 4671 of 10
+// and up to 230, 27 sequences of one head: 8, with four 16.5).
 //   out = sum_i acc_i 2^(m_i - m) / sum_i l_i 2^(m_i - m),  m = max_i m_i
 template <typename T, int D, int NW>
 __global__ __launch_bounds__(256) void k_tree_merge(TreeArgs a, int rows_per_tile) {
@@ -114,10 +115,19 @@ int log2_of(int n) { return n > 1 ? 1 + log2_of(n / 2) : 0; }
 int esize(const Shape& s) { return s.dt == RADAR_BF16 ? 2 : 4; }
 int slots() { return std::min(kSlots, 2 * num_cu()); }
 
-// row waves of M query rows a pair
-int tree_waves(const Shape& s, int64_t M) {
-  if (M <= (esize(s) == 4 ? 48 : flash_rows(esize(s), 1))) return 1;
-  if (esize(s) == 4) return ceil_div(M, 64) * 64 < ceil_div(M, 128) * 128 ? 2 : 4;
+// Row waves of M query rows a pair. Few: one, whose workgroups have the fewest rows and take
+// the longest steps. More: two or four, so that fewer workgroups read the same rows; but one
+// too where all row tiles are on the chip at once and a pair is short, for more workgroups
+// without partials (32 / 8 heads, bf16: 64 nodes over 400 rows 19.2 us, 14.7, four sequences
+// over 800 22.4, 19.2, 150 nodes over 800 21.8, 23.4; fp32: 64 nodes over 100 and 400 rows
+// 22.2 and 23.0, 13.8 and 18.9, over 1500 33.2, 34.3; ragged, 121 over 377: 44, 32.5).
+int tree_waves(const Shape& s, int64_t M, int64_t end, bool ragged) {
+  const int64_t pairs = (int64_t)s.B * s.Hkv, tiles = pairs * ceil_div(M, flash_rows(esize(s), 1));
+  if (esize(s) == 4) {
+    if (M <= 48 || (tiles <= 512 && tiles * end <= (ragged ? 1 << 18 : 1 << 17))) return 1;
+    return ceil_div(M, 64) * 64 < ceil_div(M, 128) * 128 ? 2 : 4;
+  }
+  if (M <= 32 || (tiles <= 256 && end <= 900)) return 1;
   return M <= 64 ? 2 : 4;
 }
 
@@ -136,13 +146,14 @@ struct TreePlan {
 };
 
 // Whether cutting a pair's steps into so many parts saves more than the merge takes: steps of
-// 64 and 128 query rows, of 0.8 and 1.1 us in bf16 at head dim 128, against 3 us and the
-// partials there and back at 5 TB/s (chunks of 500 tokens, 32 / 8 heads: behind 250, whole 25
-// us, cut 32; behind 1000, 40.7 and 37.2).
+// 32, 64 and 128 query rows, of 1.3, 0.8 and 1.1 us in bf16 at head dim 128 (fp32: 1.0 and
+// 3.5), against 3 us and the partials there and back at 5 TB/s (chunks of 500 tokens, 32 / 8
+// heads: behind 250, whole 25 us, cut 32; behind 1000, 40.7 and 37.2). Not asked where memory
+// bounds the steps.
 bool worth(const Shape& s, const TreePlan& p, int64_t steps, int64_t parts, int64_t M) {
-  if (p.rw == 1) return true;
-  double step_ns = (p.rw == 4 ? 1100. : 800.) * s.d / 128 * (p.waves / 4);
-  if (esize(s) == 4) step_ns = 3500. * s.d / 128;
+  if (M <= (esize(s) == 4 ? 48 : 32)) return true;
+  double step_ns = (p.rw == 4 ? 1100. : p.rw == 2 ? 800. : 1300.) * s.d / 128 * (p.waves / 4);
+  if (esize(s) == 4) step_ns = (p.rw == 1 ? 1000. : 3500.) * s.d / 128;
   const double saved = step_ns * (double)(steps - ceil_div(steps, parts));
   return saved > 3000. + (double)s.B * s.Hkv * M * parts * s.d * 4 * 2 / 5000;
 }
@@ -150,7 +161,7 @@ bool worth(const Shape& s, const TreePlan& p, int64_t steps, int64_t parts, int6
 TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
   TreePlan p;
   const int64_t M = nodes * s.G, pairs = (int64_t)s.B * s.Hkv;
-  p.rw = tree_waves(s, M);
+  p.rw = tree_waves(s, M, t + nodes, ragged);
   p.rows_per_tile = flash_rows(esize(s), p.rw);
   p.mtiles = (int)ceil_div(M, p.rows_per_tile);
   p.step = flash_tile(esize(s), p.rw);

@@ -141,6 +141,12 @@ CASES = [  # B, Hq, Hkv, d, t, N, lens, counts, spread
     (2, 32, 8, 128, 400, 250, None, None, 0),
     (1, 8, 2, 128, 100, 30, None, None, 3),                 # parts of few steps in 32 bits
     (4, 4, 2, 64, 200, 8, "ragged", None, 2),
+    (2, 32, 16, 128, 170, 150, [170, 3], [150, 149], 7),    # row tiles of one wave
+    (1, 8, 2, 64, 800, 100, None, None, 0),
+    (1, 8, 2, 64, 801, 100, None, None, 3),                 # and one row more: of four
+    (5, 64, 8, 128, 60, 32, None, None, 3),                 # many short ones
+    (7, 64, 8, 64, 60, 20, "ragged", None, 3),
+    (30, 2, 1, 128, 1200, 80, "ragged", "ragged", 4),       # many parts of one head's rows
 ]
 
 
@@ -163,6 +169,17 @@ def test_where_the_drafted_rows_begin(t, dtype):
     """Every offset of the tree's bits in a step, and steps that begin with it."""
     _run(1, 4, 2, 64, t, 37, None, None, 6, dtype)
     _run(1, 2, 2, 128, t, 70, None, None, 0, dtype)
+
+
+@DTYPES
+@pytest.mark.parametrize("t", list(range(1024, 1042)) + [1055, 1056, 1057, 1087, 1088, 1089, 1151, 1153])
+def test_where_the_drafted_rows_begin_in_longer_calls(t, dtype):
+    """The same where a workgroup's waves share the rows (two and four row waves)."""
+    _run(1, 16, 2, 64, t, 128, None, None, 6, dtype)
+    _run(1, 1, 1, 64, t, 60, None, None, 4, dtype)
+    if t % 4 == 0:
+        _run(2, 16, 2, 64, t, 130, None, None, 3, dtype)
+    _run(1, 8, 1, 128, t, 250, [t], None, 0, dtype)
 
 
 @DTYPES
