@@ -145,17 +145,16 @@ struct TreePlan {
   int rw, waves, mtiles, rows_per_tile, step, parts, units;
 };
 
-// Whether cutting a pair's steps into so many parts saves more than the merge takes: steps of
-// 32, 64 and 128 query rows, of 1.3, 0.8 and 1.1 us in bf16 at head dim 128 (fp32: 1.0 and
-// 3.5), against 3 us and the partials there and back at 5 TB/s (chunks of 500 tokens, 32 / 8
-// heads: behind 250, whole 25 us, cut 32; behind 1000, 40.7 and 37.2). Not asked where memory
-// bounds the steps.
+// Whether cutting the pairs, so that the longest has so many steps less in one part, saves
+// more than the merge of so many parts takes: steps of 32, 64 and 128 query rows, of 1.3, 0.8
+// and 1.1 us in bf16 at head dim 128 (fp32: 1.0 and 3.5), against 3 us and the partials there
+// and back at 5 TB/s (chunks of 500 tokens, 32 / 8 heads: behind 250, whole 25 us, cut 32;
+// behind 1000, 40.7 and 37.2). Not asked where memory bounds the steps.
 bool worth(const Shape& s, const TreePlan& p, int64_t steps, int64_t parts, int64_t M) {
   if (M <= (esize(s) == 4 ? 48 : 32)) return true;
   double step_ns = (p.rw == 4 ? 1100. : p.rw == 2 ? 800. : 1300.) * s.d / 128 * (p.waves / 4);
   if (esize(s) == 4) step_ns = (p.rw == 1 ? 1000. : 3500.) * s.d / 128;
-  const double saved = step_ns * (double)(steps - ceil_div(steps, parts));
-  return saved > 3000. + (double)s.B * s.Hkv * M * parts * s.d * 4 * 2 / 5000;
+  return step_ns * (double)steps > 3000. + (double)(parts * M * s.d) * 4 * 2 / 5000;
 }
 
 TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
@@ -197,10 +196,12 @@ TreePlan plan_tree(const Shape& s, int64_t nodes, int64_t t, bool ragged) {
     const int64_t units = std::max<int64_t>(1, room / p.mtiles);
     p.parts = 0;
     p.units = (int)std::max(units - (one ? pairs / 2 : pairs), (units + 1) / 2);
-    if (!worth(s, p, steps, std::min(p.units / pairs + 2, ceil_div(t + nodes, least)), M)) p.parts = 1;
+    // (as if all were of t rows)
+    const int64_t each = std::max<int64_t>(std::max<int64_t>(1, least / p.step), ceil_div(steps * pairs, p.units));
+    if (!worth(s, p, steps - each, std::min<int64_t>(p.units, pairs * ceil_div(steps, each)) + pairs, M)) p.parts = 1;
   } else {
     p.parts = ragged ? 1 : (int)std::max<int64_t>(1, std::min(room / blocks, ceil_div(t + nodes, least)));
-    if (steps <= short_steps(s) || !worth(s, p, steps, p.parts, M)) p.parts = 1;
+    if (steps <= short_steps(s) || !worth(s, p, steps - ceil_div(steps, p.parts), pairs * p.parts, M)) p.parts = 1;
     // (as many of one length)
     p.parts = (int)ceil_div(steps, ceil_div(steps, p.parts));
   }
