@@ -194,7 +194,7 @@ __device__ __forceinline__ int64_t fork_len(const ForkArgs& a, int64_t s) {
 // left are cycles, whose first sequence is saved.
 //
 // Memory bounds it, by the streams that are open at once: one sequence to one 5.6 TB/s (268
-// MB each way: 96 us), to seven 4.65 (16411 rows of 8 heads: 116 us), to 31 4.2; any map of 16
+// MB each way: 96 us), to seven 4.65 (16411 rows of 8 heads: 115 us), to 31 4.2; any map of 16
 // 4.6 (12001 rows of 16 heads: 559 us). A workgroup's start, with the list, is some 5 us (16
 // sequences of 30 rows: 8 us).
 constexpr int kInFlight = 8, kForkThreads = 256;
