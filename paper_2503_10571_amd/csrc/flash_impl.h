@@ -411,19 +411,17 @@ struct Flash {
     auto load = [&](int64_t at) {
       const bool own = BOTH && at >= own_at;
       const int64_t row = own ? at - own_at : at;
-      const unsigned char* kb = reinterpret_cast<const unsigned char*>((own ? own_K : K) + row * D);
-      const unsigned char* vb = reinterpret_cast<const unsigned char*>((own ? own_V : V) + row * D);
-      auto get = [](const unsigned char* p) {
-        const u32x4_t* v = reinterpret_cast<const u32x4_t*>(p);
-        return ONCE ? __builtin_nontemporal_load(v) : *v;
+      // (buffers of the tile's rows: no address in vector registers, and zeros behind them)
+      const int bytes = (int)min<int64_t>(NT, rows_left(at)) * kRowBytes, lt = here(ltid);
+      auto buffer = [&](const T* p) {
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p + row * D), 0, bytes, 0x00027000);
       };
-      const int last = (int)min<int64_t>(NT, rows_left(at)) - 1, lt = here(ltid);
+      const __amdgpu_buffer_rsrc_t kb = buffer(own ? own_K : K), vb = buffer(own ? own_V : V);
 #pragma unroll
       for (int i = 0; i < NCH; ++i) {
-        const int x = i * NTHR + lt, r = x / O::CPR;
-        const uint32_t off = min(r, last) * kRowBytes + x % O::CPR * 16;
-        kr[i] = get(kb + off);
-        vr[i] = get(vb + off);
+        const int off = (i * NTHR + lt) * 16;
+        kr[i] = __builtin_amdgcn_raw_buffer_load_b128(kb, off, 0, ONCE ? 2 : 0);
+        vr[i] = __builtin_amdgcn_raw_buffer_load_b128(vb, off, 0, ONCE ? 2 : 0);
       }
     };
     auto sync = [] {
