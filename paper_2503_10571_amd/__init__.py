@@ -552,6 +552,9 @@ class RadarLayer:
     behind the cache's until accept() or keep() takes some of them in or others
     replace them; fork() copies sequences onto others."""
 
+    _drafted = 0               # tokens of the last draft, whose rows lie from t on
+    _found = None              # accept()'s path, which keep() need not look over
+
     def __init__(self, cfg: Config, omega, K=None, V=None, t: int = 0,
                  top_k: int = 16, device="cuda", schedule: str = "fixed",
                  rope: Rope | None = None):
@@ -634,6 +637,7 @@ class RadarLayer:
             raise ValueError("positions without rope")
         T = k.shape[1]
         q = self._fill("prefill", k, v, q, q_out, self.pos if pos is None else pos)
+        self._drafted = 0
         self.t += T
         self.pos = self.pos + T if next_pos is None else next_pos
         self._reindex()
@@ -656,16 +660,29 @@ class RadarLayer:
         elif self.rope is not None and parent is not None:
             raise ValueError("the depth of a tree's tokens is needed with rope")
         q = self._fill("draft", k, v, q, None, pos)
-        return attend_tree(self.cfg, q, self.K, self.V, self.t, parent=parent, out=out)
+        self._drafted = 0
+        out = attend_tree(self.cfg, q, self.K, self.V, self.t, parent=parent, out=out)
+        self._drafted = N
+        return out
 
     def keep(self, path) -> None:
         """Takes the last draft's tokens of path (int32 [B][n], every sequence's
         from its first token down: ascending) into the cache, and completes the
-        index."""
-        n, c, t = path.shape[1], self.cfg.seg_len, self.t
-        if t + n > self.cfg.capacity:
+        index. A path that does not ascend, or has tokens that were not drafted since
+        the cache last grew or was cut, is refused before anything changes (whether it
+        is one is read back from the device)."""
+        n, N = path.shape[1], self._drafted
+        if self.t + n > self.cfg.capacity:
             raise RadarError("keep", 2)
+        if n > N:
+            raise ValueError(f"a path of {n} tokens, of {N} drafted ones")
+        if n and path is not self._found and bool(
+                (path[:, 1:] <= path[:, :-1]).any() | (path[:, 0] < 0).any() | (path[:, -1] >= N).any()):
+            raise ValueError(f"every sequence's path must ascend, in the {N} drafted tokens")
+        c, t = self.cfg.seg_len, self.t
         keep_path(self.cfg, self.K, self.V, t, path)
+        if n:
+            self._drafted = 0
         self.t += n
         self.pos += n
         if self.schedule == "sqrt":
@@ -684,11 +701,17 @@ class RadarLayer:
         that follows in each sequence (int64 [B])."""
         path, found, after = accept_tree(self.cfg, None, None, self.t, tokens, first, choice,
                                          parent=parent)
+        if path.shape[1] > self._drafted:
+            raise ValueError(f"{path.shape[1]} tokens, of {self._drafted} drafted ones")
         n = int(found.min())
         if n < path.shape[1]:
             then = tokens.gather(1, path[:, n:n + 1].clamp(min=0).long())[:, 0]
             after = torch.where(found > n, then, after)
-        self.keep(path[:, :n].contiguous())
+        self._found = path[:, :n].contiguous()
+        try:
+            self.keep(self._found)
+        finally:
+            self._found = None
         return n, after
 
     def fork(self, src, first: int = 0) -> None:
@@ -702,6 +725,7 @@ class RadarLayer:
             k_new = rotary(self.rope, k_new, self.pos)
         append(self.cfg, self.K, self.V, k_new, v_new, self.omega, self.t,
                self.summaries)
+        self._drafted = 0
         self.t += 1
         self.pos += 1
         if self.schedule == "sqrt":
@@ -731,6 +755,7 @@ class RadarLayer:
         if self.schedule == "sqrt":
             self.cfg = self._cfg_at(self.t + 1)
         self._fit_workspace()
+        self._drafted = 0
         self.t += 1
         self.pos += 1
         return append_decode(self.cfg, q, self.K, self.V, k_new, v_new,
@@ -754,6 +779,7 @@ class RadarLayer:
         if self.mass is None:
             raise RuntimeError("evict() needs the weights that accumulate() gathers")
         self.t = evict(self.cfg, self.K, self.V, self.mass, self.t, heavy, recent, kept=kept)
+        self._drafted = 0
         self._reindex()
 
     def _fit_workspace(self):
