@@ -716,9 +716,11 @@ class RadarLayer:
 
     def fork(self, src, first: int = 0) -> None:
         """Sequence b becomes what sequence src[b] is (int64 [B], see fork()): its
-        rows from `first` on, its weights and its summaries."""
-        fork(self.cfg, self.K, self.V, src, self.t, first=first, mass=self.mass,
-             summaries=self.summaries)
+        rows from `first` on, those of a draft that nothing was taken of among them, its
+        weights and its summaries."""
+        # (the weights behind the cache's rows are all 0, and no one reads the summaries there)
+        fork(self.cfg, self.K, self.V, src, self.t + self._drafted, first=min(first, self.t),
+             mass=self.mass, summaries=self.summaries)
 
     def append(self, k_new, v_new):
         if self.rope is not None:

@@ -111,3 +111,15 @@ def test_accept(layer, monkeypatch):
     assert n == 2 and after.tolist() == [7, 7] and layer.t == T + 2
     assert seen == [[[0, 2], [1, 2]]] and layer.calls == ["keep_path", "extend_index"]
     _refused(layer, _path([0, 0], [0, 1]), "path")
+
+
+def test_fork_takes_a_draft_along(layer, monkeypatch):
+    seen = []
+    monkeypatch.setattr(radar, "fork", lambda cfg, K, V, src, t, first=0, **kw: seen.append((t, first)))
+    layer.fork("src")
+    _draft(layer, 5)
+    layer.fork("src", first=3)
+    layer.fork("src", first=T + 2)       # rows below `first`: the cache's at most
+    layer.keep(_path([0, 4], [1, 2]))
+    layer.fork("src")
+    assert seen == [(T, 0), (T + 5, 3), (T + 5, T), (T + 2, 0)]
