@@ -203,7 +203,11 @@ size_t radar_evict_workspace_bytes(const radar_config* cfg, int64_t t,
  * [n_q_heads][head_dim] (see radar_rows); out may be q (the same address and
  * strides), there is no other overlap. Nodes from N_b on are neither read nor,
  * without RADAR_TREE_ZERO in flags, written, and what the rows hold that a node
- * does not attend, NaN and infinities too, does not matter to it. A node whose list of parents leaves the tree
+ * does not attend, NaN and infinities too, does not matter to it. An infinity in a
+ * row of V that it does attend makes that dim of its output the same infinity (NaN
+ * beside one of the other sign, and where its weight is 0: by a logit of -infinity,
+ * or in the rows [0, len) and between parts of a call by one too small for 32 bits).
+ * A node whose list of parents leaves the tree
  * (a parent below -1 or not before its child) gets NaN outputs; so does every
  * node of a sequence with lens[b] outside [0, t], counts[b] outside [0, nodes]
  * or len + N_b above the capacity. Requires 1 <= nodes (at most RADAR_MAX_TREE

@@ -88,6 +88,17 @@ template <int D, int RW> struct Ops<bf16_t, D, RW> : Wide {
     for (int ks = 0; ks < D / 16; ++ks)
       q[ks] = *reinterpret_cast<const bf16x8v_t*>(row + ks * 16 + (lane >> 5) * 8);
   }
+  // this lane's part of its row's logit of one token
+  __device__ __forceinline__ float logit_part(const bf16_t* k, int lane) const {
+    float s = 0.f;
+#pragma unroll
+    for (int ks = 0; ks < D / 16; ++ks) {
+      const bf16x8v_t a = *reinterpret_cast<const bf16x8v_t*>(k + ks * 16 + (lane >> 5) * 8);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) s = fmaf((float)a[i], (float)q[ks][i], s);
+    }
+    return s;
+  }
   // logits of tokens tok0 .. tok0 + 31 of the tile
   __device__ __forceinline__ Vec logits(const unsigned char* k, int tok0, int lane) const {
     const int row = tok0 + (lane & 31), h = lane >> 5;
@@ -194,6 +205,16 @@ template <int D, int RW> struct Ops<float, D, RW> : Wide {
       q[4 * j] = x.x; q[4 * j + 1] = x.y; q[4 * j + 2] = x.z; q[4 * j + 3] = x.w;
     }
   }
+  __device__ __forceinline__ float logit_part(const float* k, int lane) const {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 8; ++j) {
+      const float4 x = *reinterpret_cast<const float4*>(k + 8 * j + 4 * (lane >> 5));
+      s = fmaf(x.x, q[4 * j], s); s = fmaf(x.y, q[4 * j + 1], s);
+      s = fmaf(x.z, q[4 * j + 2], s); s = fmaf(x.w, q[4 * j + 3], s);
+    }
+    return s;
+  }
   __device__ __forceinline__ Vec logits(const unsigned char* k, int tok0, int lane) const {
     const int row = tok0 + (lane & 31), h = lane >> 5;
     Vec s = {};
@@ -241,6 +262,16 @@ template <int D> struct Ops<float, D, 1> : Narrow {
       const float4 x = *reinterpret_cast<const float4*>(row + 16 * j + 4 * (lane >> 4));
       q[4 * j] = x.x; q[4 * j + 1] = x.y; q[4 * j + 2] = x.z; q[4 * j + 3] = x.w;
     }
+  }
+  __device__ __forceinline__ float logit_part(const float* k, int lane) const {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 16; ++j) {
+      const float4 x = *reinterpret_cast<const float4*>(k + 16 * j + 4 * (lane >> 4));
+      s = fmaf(x.x, q[4 * j], s); s = fmaf(x.y, q[4 * j + 1], s);
+      s = fmaf(x.z, q[4 * j + 2], s); s = fmaf(x.w, q[4 * j + 3], s);
+    }
+    return s;
   }
   __device__ __forceinline__ Vec logits(const unsigned char* k, int tok0, int lane) const {
     const int row = tok0 + (lane & 15), g = lane >> 4;
@@ -365,7 +396,8 @@ struct Flash {
   // With a MASK (kOn) the rows from mask.from on are not for every query row: bit j of
   // mask.word(i, x) says whether row i attends row x + j. Elements of V there that are no
   // finite numbers would reach the others as 0 times them, so they are zeros in LDS, noted
-  // by mask.found, and make NaN, in the end, of the dims of those who attend them.
+  // by mask.found, and added in the end for those who attend them: an infinity as itself,
+  // whatever its weight, or as NaN where that is 0 by a logit of -infinity.
   // mask.finish(i, l) may change a row's sum. With mask.direct the outputs, not the
   // partials, go to mask.out_row(i).
   template <bool LOG, bool BOTH, bool ONCE, typename RowQ, typename MASK = Unmasked>
@@ -581,15 +613,21 @@ struct Flash {
     if constexpr (MASK::kOn) {
       if (r1 > mask.from) {                      // uniform
         if (mask.any_found() && tw == 0) {
+          const int ln = here(lane);
 #pragma unroll 1
           for (int64_t r = max(r0, mask.from); r < r1; ++r) {
+            const float s = O::row_total(ops.logit_part(K + r * D, ln));
             if (!(mask.word(row_in, r) & 1)) continue;
-            // (0 times an element: nothing, or NaN)
+            // (its weight is that of another group, which this one's partial must not lose)
+            if (m == -INFINITY && s > -INFINITY) m = s * qscale - 1.f;
+            const float weighs = s == -INFINITY ? 0.f : 1.f;
 #pragma unroll
             for (int db = 0; db < NDB; ++db)
 #pragma unroll
-              for (int i = 0; i < kAccVals; ++i)
-                acc[db][i] = fmaf(to_f32<T>(V[r * D + O::kDims * db + O::dim_of(i, lane)]), 0.f, acc[db][i]);
+              for (int i = 0; i < kAccVals; ++i) {
+                const float x = to_f32<T>(V[r * D + O::kDims * db + O::dim_of(i, ln)]);
+                if (!(fabsf(x) < INFINITY)) acc[db][i] = fmaf(x, weighs, acc[db][i]);
+              }
           }
         }
         l = mask.finish(row_in, l);
