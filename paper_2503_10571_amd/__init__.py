@@ -10,7 +10,6 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
-import functools
 import os
 
 import torch
@@ -46,6 +45,18 @@ class _Config(ctypes.Structure):
                 ("gqa_mode", ctypes.c_int32), ("omega_dtype", ctypes.c_int32)]
 
 
+class _MadeOnce:
+    """A config's c_struct(), read only: left in the config's own dict, where it is found
+    first from then on (0.4 us of a call less, and 0.1 more for a config made for one call;
+    functools.cached_property, which takes a lock then, 0.4 more)."""
+
+    def __get__(self, cfg, owner=None):
+        if cfg is None:
+            return self
+        made = cfg.__dict__["_c"] = cfg.c_struct()
+        return made
+
+
 @dataclasses.dataclass(frozen=True)
 class Config:
     """Shape of one Radar layer (mirrors radar_config). n_sink: leading
@@ -67,6 +78,7 @@ class Config:
     n_sink: int = 0
     gqa_mode: int = GQA_UNION
     omega_dtype: torch.dtype = torch.float32
+    _c = _MadeOnce()
 
     def c_struct(self) -> _Config:
         codes = {torch.float32: RADAR_F32, torch.bfloat16: RADAR_BF16}
@@ -74,11 +86,6 @@ class Config:
                        self.head_dim, self.n_features, self.seg_len,
                        self.window, self.capacity, codes[self.dtype], self.n_sink,
                        self.gqa_mode, codes[self.omega_dtype])
-
-    @functools.cached_property
-    def _c(self) -> _Config:
-        """c_struct(), made once (0.4 us of a call): read only."""
-        return self.c_struct()
 
     @property
     def summary_rows(self) -> int:

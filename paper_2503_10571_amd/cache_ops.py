@@ -255,15 +255,10 @@ def _positions(pos, B, T, name="pos", rope=None):
     raise ValueError(f"{name} must be an int, int64 [B] or int64 [B][T]")
 
 
-def _rotate(rope, x, B, T, d, first, second, p0, p, each, lens, inverse):
-    """radar_rotary, or radar_rotary_axes where the positions are of axes."""
-    by, head = ctypes.byref, (B, T, d, _DTYPES[x.dtype], *first, *second)
-    inverse = 1 if inverse else 0
-    if each < 0:
-        _call("radar_rotary_axes", x, by(rope._c), -each, _ptr(rope.axis), *head, _ptr(p),
-              _ptr(lens), inverse)
-    else:
-        _call("radar_rotary", x, by(rope._c), *head, p0, _ptr(p), each, _ptr(lens), inverse)
+def _rotate_axes(rope, x, B, T, d, first, second, p, each, lens, inverse):
+    """radar_rotary_axes of (heads, rows, their outputs) twice."""
+    _call("radar_rotary_axes", x, ctypes.byref(rope._c), -each, _ptr(rope.axis), B, T, d,
+          _DTYPES[x.dtype], *first, *second, _ptr(p), _ptr(lens), 1 if inverse else 0)
 
 
 def _lens_of(lens, B):
@@ -345,7 +340,11 @@ def rotary(rope: Rope, x, pos, out=None, inverse: bool = False, lens=None):
     _one_device(x, p, lens, rope.inv_freq)
     if x.numel():
         by = ctypes.byref
-        _rotate(rope, x, B, T, d, (H, by(rx), by(ro)), (0, None, None), p0, p, each, lens, inverse)
+        if each < 0:
+            _rotate_axes(rope, x, B, T, d, (H, by(rx), by(ro)), (0, None, None), p, each, lens, inverse)
+        else:
+            _call("radar_rotary", x, by(rope._c), B, T, d, _DTYPES[x.dtype], H, by(rx), by(ro),
+                  0, None, None, p0, _ptr(p), each, _ptr(lens), 1 if inverse else 0)
     return out
 
 
@@ -374,7 +373,11 @@ def rotary_qk(rope: Rope, q, k, pos, q_out=None, k_out=None, inverse: bool = Fal
             first, second = second, first
         if not second[0]:
             second = (0, None, None)
-        _rotate(rope, q, B, T, d, first, second, p0, p, each, lens, inverse)
+        if each < 0:
+            _rotate_axes(rope, q, B, T, d, first, second, p, each, lens, inverse)
+        else:
+            _call("radar_rotary", q, by(rope._c), B, T, d, _DTYPES[q.dtype], *first, *second,
+                  p0, _ptr(p), each, _ptr(lens), 1 if inverse else 0)
     return q_out, k_out
 
 
