@@ -265,8 +265,10 @@ radar_status radar_keep_path(const radar_config* cfg, void* K, void* V, int64_t 
  * own code (0 <= t0 <= t <= capacity); with lens0 and lens (both or neither,
  * device int64 [batch]) rows [lens0[b], lens[b]) of each sequence, at most `most`
  * of them (those behind are left out; an invalid pair, negative or above t,
- * completes nothing). Reads the index's fields of the config too. The workspace
- * is needed with lens only. */
+ * completes nothing; t0 is not read). Then it is a launch of the index build for
+ * each seg_len of `most`, whatever the lengths are: ask for the rows that a step may
+ * have added, not for all that there may be. Reads the index's fields of the config
+ * too. The workspace is needed with lens only. */
 radar_status radar_extend_index(const radar_config* cfg, const void* K,
                                 const void* omega, int64_t t0, int64_t t,
                                 const int64_t* lens0, const int64_t* lens,

@@ -672,20 +672,25 @@ def extend_index(cfg: Config, K, omega, t0: int, t: int, summaries, lens0=None, 
                  most: int | None = None, workspace=None) -> None:
     """radar_extend_index: the summaries of the segments that rows [t0, t) of K
     complete; or, with lens0 and lens (int64 [B], at most t), rows [lens0[b],
-    lens[b]) of every sequence, of which there are `most` at most (t - t0 if
-    None)."""
+    lens[b]) of every sequence, of which there are `most` at most (those behind are
+    left out; all, if it is None, which with lens needs t0 = 0). With lens that is
+    one launch of the index build for each seg_len of `most`, whatever the lengths
+    are."""
+    if (lens0 is None) != (lens is None):
+        raise ValueError("lens0 and lens come together")
+    if most is None:
+        if lens is not None and t0 != 0:
+            raise ValueError("most is needed with lens: the longest [lens0[b], lens[b]) may have "
+                             "more rows than [t0, t)")
+        most = t - t0
     _cache(cfg, K)
     _omega(cfg, omega)
     _summ(cfg, summaries)
-    if (lens0 is None) != (lens is None):
-        raise ValueError("lens0 and lens come together")
     if lens is not None:
         _need(lens0, torch.int64, "lens0", cfg.batch)
         _need(lens, torch.int64, "lens", cfg.batch)
     _one_device(summaries, K, omega, lens0, lens, workspace)
     c, n = ctypes.byref(cfg._c), 0
-    if most is None:
-        most = t - t0
     if lens is not None:
         need = lib().radar_extend_index_workspace_bytes(c, most) if workspace is None else 0
         workspace, n = _workspace(workspace, need, summaries.device)
