@@ -435,15 +435,15 @@ struct Flash {
 
     u32x4_t kr[NCH], vr[NCH];
     constexpr int kRowBytes = D * (int)sizeof(T);
-    // rows behind the last are read as the last; with BOTH the own rows begin behind
-    // the prefix's last step
+    // with BOTH the own rows begin behind the prefix's last step
     const int64_t own_at = BOTH ? (r1 + NTG - 1) / NTG * NTG : 0;
     const int64_t end = BOTH ? own_at + own_r1 : r1;
     auto rows_left = [&](int64_t at) { return (BOTH && at < own_at ? r1 : end) - at; };
     auto load = [&](int64_t at) {
       const bool own = BOTH && at >= own_at;
       const int64_t row = own ? at - own_at : at;
-      // (buffers of the tile's rows: no address in vector registers, and zeros behind them)
+      // Buffers of the tile's rows: no address in vector registers, and zeros behind them (a
+      // weight of 0 there takes an infinity of V for NaN).
       const int bytes = (int)min<int64_t>(NT, rows_left(at)) * kRowBytes, lt = here(ltid);
       auto buffer = [&](const T* p) {
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(p + row * D), 0, bytes, 0x00027000);
@@ -489,18 +489,6 @@ struct Flash {
         const int x = i * NTHR + pt, r = x / O::CPR, c = x % O::CPR;
         *reinterpret_cast<u32x4_t*>(kl + (r * O::CPR + O::k_place(r, c)) * 16) = kr[i];
         *reinterpret_cast<u32x4_t*>(vl + (r * O::CPR + O::v_place(r, c)) * 16) = vr[i];
-      }
-      // V's rows behind the last become zeros here (their weight is 0, which an
-      // infinity would turn into NaN); done where they are loaded, it would wait
-      // for one load after the other
-      if (len < NT) {                            // uniform
-        const int lt = here(ltid);
-#pragma unroll
-        for (int i = 0; i < NCH; ++i) {
-          const int x = i * NTHR + lt, r = x / O::CPR, c = x % O::CPR;
-          if (r >= len)
-            *reinterpret_cast<u32x4_t*>(vl + (r * O::CPR + O::v_place(r, c)) * 16) = u32x4_t{0, 0, 0, 0};
-        }
       }
       if constexpr (MASK::kOn) {
         if (at + len > mask.from) {              // uniform
