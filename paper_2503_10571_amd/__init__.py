@@ -655,7 +655,8 @@ class RadarLayer:
         that each of them follows (attend_tree): q [B][N][Hq][d], k, v
         [B][N][Hkv][d]; parent as for attend_tree (None: a chain). With rope, depth
         (int64 [N] or [B][N]; of several axes [axes][B][N]) is how far each token
-        is behind the next position, 0 for the first; a chain needs none. Their
+        is behind the next position, 0 for the first; a chain needs none (and without rope
+        no position matters). Their
         rows lie behind the cache's, for accept() or keep(); the cache, its index and its
         length are as before, and another draft replaces them."""
         cfg, N = self.cfg, k.shape[1]
@@ -705,7 +706,8 @@ class RadarLayer:
         accept_tree() finds them from tokens, first and choice: as many for every
         sequence as for the one with the fewest (a layer's sequences are of one
         length; the number is read back from the device). Returns it and the token
-        that follows in each sequence (int64 [B])."""
+        that follows in each sequence (int64 [B]). The choices are of exact attention;
+        steps, which read selected segments, might have chosen others."""
         path, found, after = accept_tree(self.cfg, None, None, self.t, tokens, first, choice,
                                          parent=parent)
         if path.shape[1] > self._drafted:

@@ -22,9 +22,10 @@ struct PathArgs {
 };
 
 // Rows len + path(i) of a sequence's heads to len + i, i < n, in place: path(i) >= i
-// ascends, so rows read later are not among those written, and of kRows rows at a time
-// all are read before one is written. A wave per head; a row's 16-byte chunks on the
-// lanes.
+// ascends, so rows read later are not among those written, and of kPasses passes' rows at a
+// time all are read before one is written. A wave per head, one after the other down the
+// path: 8 rows of each of 8 heads 3.4 us, 512 rows 49, 4096 550; a row's 16-byte chunks on
+// the lanes.
 template <typename PathOf>
 __device__ __forceinline__ void move_rows(const PathArgs& a, int64_t b, int64_t len, int n,
                                           PathOf&& path) {
@@ -195,8 +196,11 @@ __device__ __forceinline__ int64_t fork_len(const ForkArgs& a, int64_t s) {
 //
 // Memory bounds it, by the streams that are open at once: one sequence to one 5.6 TB/s (268
 // MB each way: 96 us), to seven 4.65 (16411 rows of 8 heads: 115 us), to 31 4.2; any map of 16
-// 4.6 (12001 rows of 16 heads: 559 us). A workgroup's start, with the list, is some 5 us (16
-// sequences of 30 rows: 8 us).
+// 4.6 (12001 rows of 16 heads: 559 us). A workgroup's start, with the list, is some 5 us for up
+// to 16 sequences (of 30 rows: 8 us). The list takes a round for each link of a chain and above
+// 64 sequences, where a whole workgroup makes it, barriers in each; there every member of a
+// cycle walks all of it (rows of one head, 16 a sequence, all moves: 64 sequences as pairs 37 us,
+// a cycle 32, a chain 35; 65: 33, 38, 60; 256: 100, 119, 217; 2048: 741, 1600, 3330).
 constexpr int kInFlight = 8, kForkThreads = 256;
 // a move is dst << 16 | src; kNone as dst: src is saved; kSaved in src: src as it was saved;
 // kZero as src: zeros

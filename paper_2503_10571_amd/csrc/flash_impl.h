@@ -9,12 +9,13 @@
 // four consecutive tokens at a time, which are its k-slots of P^T if the rows of
 // V are taken in the same order: no value of P crosses lanes.
 //
-// Up to 32 query rows per kv head (16 in fp32) memory bounds it: 6.4 TB/s of the
-// 7.2 that one pass of loads over 2 GiB and more reaches (32000 own rows of 8 x 8 pairs, head dim 128: 162 us). Above,
+// Up to 64 query rows per kv head (16 in fp32) memory bounds it, and at 128 nearly: 6.5 TB/s of the
+// 7.2 that one pass of loads over 2 GiB and more reaches (32000 own rows of 8 x 8 pairs, head dim 128, 4 query rows:
+// 161 us); at the margin 6.9 with 32 rows, 7.4 with 64, 6.0 with 128 (a tree's nodes over 131072). Above,
 // the matrix cores, the exponentials and the LDS reads of their operands share
-// the time: 0.8 PFLOP/s of the 1.28 that a large library product reaches (512
-// rows per kv head over a prefix of 100000: 265 us, at a clock of 1.8 GHz). In fp32 the matrix cores' 32-bit
-// rate.
+// the time: 0.8 to 0.9 PFLOP/s of the 1.28 that a large library product reaches (512
+// rows per kv head over a prefix of 100000: 230 us at 2.0 GHz, 265 in a long run, whose clock falls). In fp32 the
+// matrix cores' 32-bit rate.
 //
 // K and V come to LDS through registers, the next tile's loads in flight while
 // this one is computed. Rows are stored whole, their 16-byte chunks at places
@@ -119,7 +120,8 @@ template <int D, int RW> struct Ops<bf16_t, D, RW> : Wide {
   // own rounding, 1.62e-3. Otherwise p is rounded to bf16, half a step of 2^-8 each, and
   // both roundings together are 1.93e-3 at 20 query rows, 2.17e-3 at 64, 2.27e-3 at 512,
   // where the output's alone is 1.66e-3; the second product that more bits would take is
-  // half of the kernel's matrix work again.
+  // half of the kernel's matrix work again. (For 17 to 32 rows, where memory bounds it, a
+  // second product takes 2-9% more up to 900 cache rows and 2-3% above, for 1.7e-3.)
   __device__ static __forceinline__ bf16x8v_t p_operand(const Vec& p, int ks, bool twice, bool low) {
     constexpr float kTiny = 1.17549435e-38f;     // smallest normal number
     bf16x8v_t b;

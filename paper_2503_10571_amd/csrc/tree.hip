@@ -3,10 +3,12 @@
 // over the rows is flash_impl.h's: a pair's query rows are those of all its nodes, and
 // only the steps that hold drafted rows look at who attends which.
 //
-// Up to 128 query rows a pair memory bounds it: at the margin 6.0 to 7.4 TB/s of the 7.2 that
+// Up to 64 query rows a pair memory bounds it, and at 128 nearly: at the margin 6.0 to 7.4 TB/s of the 7.2 that
 // a pass of loads reaches (8, 16, 32 nodes of 32 / 8 heads of 128 over 131072 rows, bf16: 83, 85, 102
-// us); above, matrix cores, exponentials and LDS in turn, 0.94 PFLOP/s of the 1.35 of a large
-// library product (64 nodes over 131072 rows: 161 us; a chunk of 1500 tokens behind 8000: 265).
+// us; one token 80); above, matrix cores, exponentials and LDS in turn, 0.94 PFLOP/s of the 1.35 of a large
+// library product (64 nodes over 131072 rows: 161 us). A chunk of 1500 tokens behind 8000, 265 us, is 376
+// row tiles for 256 CUs, of which 120 take two: 32% of the cycles are of matrix instructions, 43%
+// where every CU has two (2048 tokens, 314 us; the clock is 2.08 and 1.94 GHz).
 // Start and end are 5 to 14 us: the lengths, the parents and the first rows one after the
 // other, 2 us each, the bits, and the partials of a full chip.
 #include "flash_impl.h"
