@@ -644,7 +644,8 @@ class RadarLayer:
             raise ValueError("positions without rope")
         T = k.shape[1]
         q = self._fill("prefill", k, v, q, q_out, self.pos if pos is None else pos)
-        self._drafted = 0
+        if T:
+            self._drafted = 0
         self.t += T
         self.pos = self.pos + T if next_pos is None else next_pos
         self._reindex()
@@ -789,8 +790,10 @@ class RadarLayer:
         others with the most accumulated weight, and rebuilds the index."""
         if self.mass is None:
             raise RuntimeError("evict() needs the weights that accumulate() gathers")
-        self.t = evict(self.cfg, self.K, self.V, self.mass, self.t, heavy, recent, kept=kept)
-        self._drafted = 0
+        t = evict(self.cfg, self.K, self.V, self.mass, self.t, heavy, recent, kept=kept)
+        if t != self.t:
+            self._drafted = 0
+        self.t = t
         self._reindex()
 
     def _fit_workspace(self):

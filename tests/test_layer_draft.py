@@ -82,6 +82,8 @@ def test_keep_needs_a_draft(layer):
         layer.prefill(x[:1], x[:1])
     with pytest.raises(radar.RadarError):
         _draft(layer, CAP)
+    layer.evict(layer.t - 8, 8)          # nothing to cut, and a chunk of no tokens
+    layer.prefill(x[:, :0], x[:, :0])
     layer.keep(one)
     _draft(layer, 3)
     with pytest.raises(radar.RadarError):        # no room in the cache at all
